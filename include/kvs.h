@@ -377,10 +377,154 @@ KVS_API kvs_status kvs_project_qkv(const kvs_shape *shape, int32_t hidden, const
                                    void *q_out, void *k_out, void *v_out, void *stream);
 
 /*
+ * kvs_rotary -- rotary positions of Q and K rows: what a layer applies to fresh rows, and what a reused key needs when it
+ * takes another position in the new request than it had in the one it was computed for (its K then has to be turned by the
+ * difference; V carries no position).
+ *
+ * The first rotary_dim channels of every head form rotary_dim/2 pairs, pair j = channels (j, j + rotary_dim/2) in the
+ * KVS_ROTARY_HALF layout and (2j, 2j + 1) in the KVS_ROTARY_INTERLEAVED one; the other channels pass through.  With
+ * a = (pos[i] - pos_from[i]) * f_j a pair (u, v) of row i becomes
+ *     magnitude * (u cos a - v sin a),   magnitude * (v cos a + u sin a)
+ * in fp32, rounded once.  Angles are formed in fp64 (a position of 10^6 keeps them to 1e-7).  f_j, before scaling, is
+ * base^(-2j / rotary_dim); the scalings for contexts longer than `original`, the length that a model was trained on, are
+ *     KVS_ROTARY_PLAIN       f_j
+ *     KVS_ROTARY_LINEAR      f_j / factor                         (position interpolation)
+ *     KVS_ROTARY_NTK         base * factor^(rotary_dim / (rotary_dim - 2)) in place of base; rotary_dim > 2
+ *     KVS_ROTARY_RAMP        f_j (1 - w) + f_j / factor * w, w rising from 0 to 1 over the pairs from floor(at(high)) to
+ *                            ceil(at(low)), at(t) = rotary_dim * ln(original / (2 pi t)) / (2 ln base): pairs that turn more
+ *                            than `high` times within the original length keep their frequency, those under `low` turns are
+ *                            interpolated (YaRN, arXiv 2309.00071; its magnitude 0.1 ln(factor) + 1 is the caller's)
+ *     KVS_ROTARY_WAVELENGTH  f_j w + f_j / factor * (1 - w), w rising from 0 to 1 with the turns original * f_j / (2 pi)
+ *                            from `low` to `high`
+ * factor, original, low and high are only read by the scalings that use them (0 < low < high).  A magnitude other than 1
+ * belongs to fresh rows: moved ones have it already.
+ *
+ * n_tokens        rows; 0 is allowed
+ * pos             [dev] int32[n_tokens], any value        pos_from [dev] int32[n_tokens] or NULL (0: fresh rows)
+ * q, q_out        [dev] n_tokens rows of n_q_heads * head_dim elements, q_stride and q_out_stride elements apart, each at
+ *                 least a row long and a multiple of 16 bytes: a slice of a fused projection's buffer will do
+ * k, k_out        the same with n_kv_heads.  q or k may be NULL (with its output), not both
+ * In place (the same pointer and stride) is allowed; an output may not overlap an input or output in any other way.
+ */
+typedef enum { KVS_ROTARY_HALF = 0, KVS_ROTARY_INTERLEAVED = 1 } kvs_rotary_layout;
+typedef enum {
+    KVS_ROTARY_PLAIN = 0, KVS_ROTARY_LINEAR = 1, KVS_ROTARY_NTK = 2, KVS_ROTARY_RAMP = 3, KVS_ROTARY_WAVELENGTH = 4
+} kvs_rotary_scaling;
+
+typedef struct {
+    int32_t rotary_dim; /* channels of a head that are turned: even, 2 .. head_dim */
+    int32_t layout;     /* kvs_rotary_layout */
+    int32_t scaling;    /* kvs_rotary_scaling */
+    int32_t original;   /* context length that the unscaled frequencies belong to */
+    double base;        /* > 1 */
+    double factor;      /* > 0 */
+    double low, high;   /* turns */
+    double magnitude;
+} kvs_rotary_spec;
+
+KVS_API kvs_status kvs_rotary(const kvs_shape *shape, const kvs_rotary_spec *spec, int64_t n_tokens,
+                              const int32_t *pos, const int32_t *pos_from,
+                              const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                              void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *stream);
+
+/*
+ * A KV cache held in 8 bits, with a scale for each block of tokens and KV head.  K and V are kept apart: element c of
+ * row i and head g stands for  code[i, g, c] * scale[i / block, g].  Blocks are counted over the cache's rows, so
+ * requests that begin with a block of their own share no scale with another request.  A scale of 0 marks a block that
+ * holds nothing but zeros (whatever its codes): set the scales of a block to 0 before its first use and before another
+ * request takes it over.  A scale that is NaN marks a block that a NaN or infinity was stored into: rows that see one of
+ * its keys become NaN, no others.
+ *
+ * KVS_E4M3 codes are OCP 8-bit floats with 3 mantissa bits (largest 448), KVS_INT8 codes whole numbers from -127 to 127.
+ * A store writes no other codes; e4m3's two NaN codes, where memory that was never stored to holds them, do not reach
+ * rows that do not see their key.
+ *
+ * Everything else stays in the shape's dtype (Q, outputs, rows to store, fresh rows), bf16 or fp32.  head_dim 64 or 128,
+ * up to 64 KV heads.
+ */
+typedef enum { KVS_E4M3 = 0, KVS_INT8 = 1 } kvs_code;
+
+typedef struct {
+    void *k, *v;             /* [dev] [n_rows, n_kv_heads, head_dim] codes, one byte each, 16-byte aligned */
+    float *k_scale, *v_scale; /* [dev] fp32 [(n_rows + block - 1) / block, n_kv_heads] */
+    int64_t n_rows;
+    int32_t block;           /* 16, 32, 64 or 128 tokens */
+    int32_t code;            /* kvs_code */
+} kvs_cache8;
+
+/*
+ * kvs_store_kv8 -- the KV Writer (App. A) for a cache in 8 bits: a prompt's rows, a decode step's new ones, or recomputed
+ * rows in place of reused ones.
+ *
+ * sel_pos == NULL  row row0 + s takes k_new[s], v_new[s]           for s in [0, n_sel)
+ * sel_pos != NULL  row sel_pos[s] takes them (row0 is not read).  Entries of one block have to stand together in the list
+ *                  (an ascending list does that, one that keeps every request's rows together in any order of the
+ *                  requests too); inside a block any order goes, and of equal entries the last one counts.  Entries
+ *                  outside [0, n_rows) are skipped; they count as a block of their own.
+ *
+ * For each block that takes a row, each KV head, K and V apart, with top = 448 (KVS_E4M3) or 127 (KVS_INT8), in fp32:
+ *     need  = max |x| over the rows that the block takes / top, at least 2^-126 (0 if they are all zero)
+ *     scale = max(need, old scale), or need alone if all of the block's rows in the cache are taken
+ *     code  = nearest code (ties to even) to x * (1 / scale)      for the rows taken
+ *     code  = nearest code to code * (old scale / scale)          for the other rows, where the scale has changed
+ * Kept rows are therefore rounded again only when a larger value comes into their block.  If one of the rows taken holds
+ * a NaN or infinity, or a row is kept and the old scale is NaN, the scale becomes NaN.
+ *
+ * k_new, v_new  [dev] [n_sel, n_kv_heads, head_dim] in the shape's dtype
+ * reused, dev_v [dev] uint8[n_rows], fp32[n_kv_heads, n_rows], each may be NULL: cleared for the rows taken, as in
+ *               kvs_scatter_kv
+ * Nothing is accumulated out of order: the result does not depend on timing.  Calls on one cache that could touch the
+ * same block have to be ordered (one stream, or events).
+ */
+KVS_API kvs_status kvs_store_kv8(const kvs_shape *shape, const kvs_cache8 *cache, const void *k_new, const void *v_new,
+                                 const int32_t *sel_pos, int64_t row0, int64_t n_sel,
+                                 uint8_t *reused, float *dev_v, void *stream);
+
+/*
+ * kvs_deviation_kv8 -- kvs_deviation against a cache in 8 bits: what the cache rows row0 .. row0 + n_tokens - 1 stand for
+ * against freshly computed rows.
+ *
+ *   dev_v[g,i] = sum_c | v_fresh[i,g,c] - v_code[row0+i,g,c] * v_scale[(row0+i) / block, g] |,   dev_k likewise
+ *
+ * score, alpha, reused and mode as in kvs_deviation, all of n_tokens entries: scores go on to kvs_select_topk.  k_fresh
+ * may be NULL in mode KVS_SCORE_V with dev_k == NULL.  fp32 in a fixed order (bit-reproducible).
+ */
+KVS_API kvs_status kvs_deviation_kv8(const kvs_shape *shape, const kvs_cache8 *cache, int64_t row0, int64_t n_tokens,
+                                     const void *k_fresh, const void *v_fresh,
+                                     const uint8_t *reused, const float *alpha, int32_t mode,
+                                     float *dev_k, float *dev_v, float *score, void *stream);
+
+/*
+ * kvs_attention_kv8 -- kvs_partial_attention over a cache in 8 bits; a decode step is the call with one selected token a
+ * request, at position ctx_len - 1.
+ *
+ * Request b owns cache rows [ctx_off[b], ctx_off[b] + ctx_len[b]) and the selected tokens [cu_sel[b], cu_sel[b+1]); token
+ * s at request-local position p = sel_pos[s] sees its request's rows 0 .. p.  A negative position sees nothing (a place
+ * of a padded batch that holds no token): its out rows are 0 and its lse -inf; a position past the context sees all of
+ * it.  Positions may come in any order (ascending is fastest); contexts may overlap, begin anywhere in a block, and lie
+ * inside [0, n_rows).
+ *
+ * q_sel, out [dev] [n_sel, n_q_heads, head_dim]      lse_out [dev] fp32[n_sel, n_q_heads] or NULL (natural log)
+ * scale      any finite number
+ * workspace  [dev] optional (NULL / 0 is valid), 256-byte aligned, kvs_workspace_size("attention_kv8", shape, batch, cache
+ *            rows, n_sel) bytes: launches that would leave units idle cut their key ranges into pieces and merge them.
+ *            Less of it means fewer pieces; results are the same up to fp32 summation order.  One call's until that call
+ *            has ended on its stream.
+ * Codes enter the matrix cores as the bf16 numbers that they are, exactly; K's scales multiply the scores in fp32.
+ * bf16: softmax weights times V's scales enter the second product rounded to bf16.  fp32: Q and these products enter as
+ * three bf16 numbers each, which together hold all their bits, and everything else is fp32.
+ */
+KVS_API kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8 *cache, int32_t batch,
+                                     const int64_t *ctx_off, const int64_t *ctx_len, const int64_t *cu_sel,
+                                     const void *q_sel, const int32_t *sel_pos, float scale,
+                                     void *out, float *lse_out,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Workspace a call needs, in bytes, for the given problem.  `call` is "select_topk",
- * "partial_attention", "decode_check", "attn_colsum", "first_order_impact" or "match_tokens" (anything else
+ * "partial_attention", "decode_check", "attn_colsum", "first_order_impact", "match_tokens" or "attention_kv8" (anything else
  * returns 0).  n_rows_total is the total number of score / cache rows the call will see (match_tokens: the
- * target's tokens), n_sel_total the total number of selected tokens (partial_attention) or the candidate's
+ * target's tokens), n_sel_total the total number of selected tokens (partial_attention, attention_kv8) or the candidate's
  * tokens (match_tokens, which ignores shape: it may be NULL there).  The answer is an upper bound valid for any split of the
  * totals over `batch` requests, and does not shrink as the totals grow.
  */

@@ -21,9 +21,13 @@ LIB_PATH = os.path.join(_PKG, "libkvshare_hip.so")
 F32, BF16 = 0, 1
 SCORE_V, SCORE_KV = 0, 1
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP = 0, 1, 2, 3, 4
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "ramp": 3, "wavelength": 4}
+E4M3, INT8 = 0, 1
 
 EXPORTS = ("kvs_deviation", "kvs_deviation_topk", "kvs_select_topk", "kvs_select_topk_static", "kvs_scatter_kv", "kvs_partial_attention",
-           "kvs_decode_check", "kvs_attn_colsum", "kvs_first_order_impact", "kvs_match_tokens", "kvs_project_qkv", "kvs_workspace_size", "kvs_strerror", "kvs_last_error", "kvs_version")
+           "kvs_decode_check", "kvs_attn_colsum", "kvs_first_order_impact", "kvs_match_tokens", "kvs_project_qkv",
+           "kvs_rotary", "kvs_store_kv8", "kvs_deviation_kv8", "kvs_attention_kv8", "kvs_workspace_size", "kvs_strerror", "kvs_last_error", "kvs_version")
 
 
 class KvsError(RuntimeError):
@@ -35,6 +39,17 @@ class KvsError(RuntimeError):
 class Shape(ctypes.Structure):
     _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class RotarySpec(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32), ("original", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("magnitude", ctypes.c_double)]
+
+
+class _Cache8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_rows", ctypes.c_int64), ("block", ctypes.c_int32), ("code", ctypes.c_int32)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -64,9 +79,15 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.kvs_first_order_impact.argtypes = [sp, i64, vp, vp, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp]
     lib.kvs_match_tokens.argtypes = [vp, i64, vp, i64, i32, ctypes.c_uint32, ctypes.c_uint32, vp, vp, vp, vp, vp, sz, vp]
     lib.kvs_project_qkv.argtypes = [sp, i32, vp, i64, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp]
+    rp, cp = ctypes.POINTER(RotarySpec), ctypes.POINTER(_Cache8)
+    lib.kvs_rotary.argtypes = [sp, rp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.kvs_store_kv8.argtypes = [sp, cp, vp, vp, vp, i64, i64, vp, vp, vp]
+    lib.kvs_deviation_kv8.argtypes = [sp, cp, i64, i64, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.kvs_attention_kv8.argtypes = [sp, cp, i32, vp, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]
     lib.kvs_workspace_size.argtypes = [ctypes.c_char_p, sp, i32, i64, i64]
     for n in ("kvs_deviation", "kvs_deviation_topk", "kvs_select_topk", "kvs_select_topk_static", "kvs_scatter_kv", "kvs_partial_attention",
-              "kvs_decode_check", "kvs_attn_colsum", "kvs_first_order_impact", "kvs_match_tokens", "kvs_project_qkv"):
+              "kvs_decode_check", "kvs_attn_colsum", "kvs_first_order_impact", "kvs_match_tokens", "kvs_project_qkv",
+              "kvs_rotary", "kvs_store_kv8", "kvs_deviation_kv8", "kvs_attention_kv8"):
         getattr(lib, n).restype = ctypes.c_int
     lib.kvs_workspace_size.restype = sz
     lib.kvs_strerror.argtypes = [ctypes.c_int]
@@ -261,6 +282,131 @@ def kvs_project_qkv(shape: Shape, x, x_rows, sel_pos, n_sel: int, w_qkv, rope, q
                                 _ptr(sel_pos, torch.int32), n_sel, _ptr(w_qkv), _ptr(rope, torch.float32),
                                 rope.shape[0] if rope is not None else 0, _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream))
     _check(rc, "kvs_project_qkv")
+
+
+def rotary_spec(rotary_dim: int, layout: str = "half", scaling: str = "plain", base: float = 10000.0, factor: float = 1.0,
+                original: int = 0, low: float = 1.0, high: float = 4.0, magnitude: float = 1.0) -> RotarySpec:
+    return RotarySpec(rotary_dim, ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], original, base, factor, low, high, magnitude)
+
+
+def _rows(t: Optional[torch.Tensor], shape: Shape, heads: int, n: int):
+    """Address and row stride of [n, heads, head_dim] rows, each row in one piece, rows any distance apart."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise TypeError("device tensor expected")
+    if t.shape != (n, heads, shape.head_dim) or _dtype_code(t) != shape.dtype:
+        raise ValueError(f"expected {(n, heads, shape.head_dim)} in the shape's dtype, got {tuple(t.shape)} {t.dtype}")
+    if n and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != shape.head_dim)):
+        raise TypeError("the heads of a row have to be contiguous")
+    return t.data_ptr(), t.stride(0) if n > 1 else heads * shape.head_dim
+
+
+def _one_device(*tensors) -> None:
+    """The kernels run on the current device: what lies on another one is refused."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != dev:
+            raise ValueError(f"tensor on device {t.get_device()}, the current device is {dev}")
+
+
+def _entries(t: Optional[torch.Tensor], n: int, what: str) -> None:
+    if t is not None and t.numel() < n:
+        raise ValueError(f"{what} has {t.numel()} entries, {n} are needed")
+
+
+def kvs_rotary(shape: Shape, spec: RotarySpec, pos, pos_from, q, k, q_out, k_out, stream=None) -> None:
+    n = pos.numel()
+    _one_device(pos, pos_from, q, k, q_out, k_out)
+    _entries(pos_from, n, "pos_from")
+    (qp, qs), (qop, qos) = (_rows(t, shape, shape.n_q_heads, n) for t in (q, q_out))
+    (kp, ks), (kop, kos) = (_rows(t, shape, shape.n_kv_heads, n) for t in (k, k_out))
+    rc = load().kvs_rotary(ctypes.byref(shape), ctypes.byref(spec), n, _ptr(pos, torch.int32), _ptr(pos_from, torch.int32),
+                           qp, qs, kp, ks, qop, qos, kop, kos, _stream(stream))
+    _check(rc, "kvs_rotary")
+
+
+class Cache8:
+    """A KV cache held in 8 bits: k, v [rows, KV heads, head_dim] (torch.float8_e4m3fn or torch.int8), k_scale and v_scale
+    fp32 [blocks, KV heads], `block` tokens to a scale."""
+
+    def __init__(self, k, v, k_scale, v_scale, block: int):
+        codes = {torch.float8_e4m3fn: E4M3, torch.int8: INT8}
+        if k.dtype not in codes or v.dtype is not k.dtype:
+            raise TypeError(f"codes are torch.float8_e4m3fn or torch.int8, not {k.dtype}, {v.dtype}")
+        if k.dim() != 3 or v.shape != k.shape:
+            raise ValueError("k and v are [rows, KV heads, head_dim], of one shape")
+        if block <= 0:
+            raise ValueError("a block holds 16, 32, 64 or 128 tokens")
+        blocks = (-(-k.shape[0] // block), k.shape[1])
+        if tuple(k_scale.shape) != blocks or tuple(v_scale.shape) != blocks:
+            raise ValueError(f"scales are {list(blocks)}, not {list(k_scale.shape)}, {list(v_scale.shape)}")
+        self.k, self.v, self.k_scale, self.v_scale, self.block = k, v, k_scale, v_scale, block
+        self.n_rows, self.n_kv_heads, self.head_dim = k.shape
+        self.raw = _Cache8(_ptr(k), _ptr(v), _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), k.shape[0], block, codes[k.dtype])
+
+    @classmethod
+    def empty(cls, shape: Shape, n_rows: int, block: int, code: int = E4M3, device="cuda") -> "Cache8":
+        """A cache of n_rows rows that holds nothing."""
+        dt = torch.float8_e4m3fn if code == E4M3 else torch.int8
+        k, v = (torch.zeros((n_rows, shape.n_kv_heads, shape.head_dim), dtype=torch.uint8, device=device).view(dt) for _ in range(2))
+        ks, vs = (torch.zeros((-(-n_rows // block), shape.n_kv_heads), device=device) for _ in range(2))
+        return cls(k, v, ks, vs, block)
+
+
+def _cache8(cache: Cache8, shape: Shape):
+    if (cache.n_kv_heads, cache.head_dim) != (shape.n_kv_heads, shape.head_dim):
+        raise ValueError(f"the cache has {cache.n_kv_heads} KV heads of {cache.head_dim}, the shape {shape.n_kv_heads} of {shape.head_dim}")
+    return ctypes.byref(cache.raw)
+
+
+def kvs_store_kv8(shape: Shape, cache: Cache8, k_new, v_new, sel_pos, row0: int = 0, reused=None, dev_v=None, stream=None) -> None:
+    n = k_new.shape[0]
+    _one_device(cache.k, k_new, v_new, sel_pos, reused, dev_v)
+    for t in (k_new, v_new):
+        _rows(t, shape, shape.n_kv_heads, n)
+    _entries(sel_pos, n, "sel_pos")
+    _entries(reused, cache.n_rows, "reused")
+    _entries(dev_v, cache.n_rows * shape.n_kv_heads, "dev_v")
+    rc = load().kvs_store_kv8(ctypes.byref(shape), _cache8(cache, shape), _ptr(k_new), _ptr(v_new), _ptr(sel_pos, torch.int32), row0, n,
+                              _ptr(reused, torch.uint8), _ptr(dev_v, torch.float32), _stream(stream))
+    _check(rc, "kvs_store_kv8")
+
+
+def kvs_deviation_kv8(shape: Shape, cache: Cache8, row0: int, n_tokens: int, k_fresh, v_fresh, reused, alpha, mode: int,
+                      dev_k, dev_v, score, stream=None) -> None:
+    _one_device(cache.k, k_fresh, v_fresh, reused, alpha, dev_k, dev_v, score)
+    cells = n_tokens * shape.n_kv_heads
+    for t, n, what in ((k_fresh, cells * shape.head_dim, "k_fresh"), (v_fresh, cells * shape.head_dim, "v_fresh"), (reused, n_tokens, "reused"),
+                       (alpha, cells, "alpha"), (dev_k, cells, "dev_k"), (dev_v, cells, "dev_v"), (score, n_tokens, "score")):
+        _entries(t, n, what)
+    for t in (k_fresh, v_fresh):
+        if t is not None and _dtype_code(t) != shape.dtype:
+            raise TypeError(f"fresh rows are in the shape's dtype, not {t.dtype}")
+    rc = load().kvs_deviation_kv8(ctypes.byref(shape), _cache8(cache, shape), row0, n_tokens, _ptr(k_fresh), _ptr(v_fresh),
+                                  _ptr(reused, torch.uint8), _ptr(alpha, torch.float32), mode, _ptr(dev_k, torch.float32),
+                                  _ptr(dev_v, torch.float32), _ptr(score, torch.float32), _stream(stream))
+    _check(rc, "kvs_deviation_kv8")
+
+
+def kvs_attention_kv8(shape: Shape, cache: Cache8, ctx_off: Sequence[int], ctx_len: Sequence[int], cu_sel: Sequence[int],
+                      q_sel, sel_pos, scale: float, out, lse_out=None, workspace=None, stream=None) -> None:
+    co, cl, cs = _i64(ctx_off), _i64(ctx_len), _i64(cu_sel)
+    if co.n != cl.n or cs.n != co.n + 1:
+        raise ValueError("ctx_off/ctx_len need one entry per request and cu_sel one more")
+    n = int(cs.data[-1])
+    _one_device(cache.k, q_sel, sel_pos, out, lse_out, workspace)
+    for t, cells, what in ((q_sel, n * shape.n_q_heads * shape.head_dim, "q_sel"), (out, n * shape.n_q_heads * shape.head_dim, "out"),
+                           (sel_pos, n, "sel_pos"), (lse_out, n * shape.n_q_heads, "lse_out")):
+        _entries(t, cells, what)
+    for t in (q_sel, out):
+        if t is not None and _dtype_code(t) != shape.dtype:
+            raise TypeError(f"q_sel and out are in the shape's dtype, not {t.dtype}")
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    rc = load().kvs_attention_kv8(ctypes.byref(shape), _cache8(cache, shape), co.n, co.ptr, cl.ptr, cs.ptr, _ptr(q_sel),
+                                  _ptr(sel_pos, torch.int32), scale, _ptr(out), _ptr(lse_out, torch.float32), _ptr(workspace), ws_bytes,
+                                  _stream(stream))
+    _check(rc, "kvs_attention_kv8")
 
 
 def shape_of(workload) -> Shape:

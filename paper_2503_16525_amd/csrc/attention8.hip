@@ -1,0 +1,619 @@
+// kvs_attention_kv8: attention of selected rows, or of a decode step's single ones, over a cache held in 8 bits.
+//
+// Mathematics.  With codes k, v and their scales s_k, s_v for a block of tokens and a head, a row's output is
+//     sum_i p_i s_v(i) v_i / sum_i p_i,   p_i = exp(scale s_k(i) (q . k_i) - max)
+// Codes are bf16 numbers exactly, so they go to the matrix cores as they are: K's scale multiplies the score behind the
+// first product, V's the weight before the second.  One pass over the keys with a running maximum and sum.
+//
+// Tiles.  A wave takes 32 rows (the query heads of one KV head flattened with the selected tokens, as in the bf16
+// kernels) against tiles of 32 keys, S^T = K Q^T and O^T += V^T P^T, so that P stays in registers as the operand of the
+// second product.  Tiles begin at multiples of 16 cache rows, whatever row a context begins at: each half of a tile then
+// lies in one block, and its two scales are the same for all lanes.  What lies before a context, behind a row's position or
+// behind the cache is masked.
+//
+// What bounds it with few rows, a decode step's, is the cache's bytes: 2 d a key and KV head.  So a workgroup's four
+// waves take the same 32 rows and every fourth tile, each with LDS slots of its own that its loads go to directly
+// (global to LDS, 16 bytes a lane, no registers), two tiles deep and without a barrier; at the end the waves meet in LDS.
+// Launches of too few workgroups cut the key ranges into pieces, which a second kernel merges.
+//
+// A lane's V operand is 8 keys of one channel, but a row of codes lies along the channels: a lane reads D/32 neighbouring
+// channels of each of 8 keys and permutes bytes, and channel D/32 * m + db stands at matrix row m of product db, which
+// costs nothing (the output's order is undone where it is stored).
+#include "cache8.h"
+#include "attention.h"
+
+#include <math.h>
+
+namespace kvs {
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
+
+constexpr int kWaves = 4, kThreads = kWaves * kWave;
+constexpr int kRows = 32;              // rows of a unit
+constexpr int kKeys = 32;              // keys of a tile
+constexpr int kAlign = 16;             // cache rows that tiles are aligned to: no block is shorter
+constexpr int kSplitBelow = 1024;      // workgroups below which key ranges are cut
+constexpr int kTargetWgs = 1024;
+constexpr int kMinPieceTiles = 8;      // tiles of a piece: two for each wave
+constexpr int kMaxPieces = 512;
+
+// The launch's requests.  Workgroup = (unit, KV head); a unit is a block of 32 rows of one request and one piece of its keys.
+struct Table {
+    int64_t ctx_off[kAttnMaxReq];
+    int64_t sel_lo[kAttnMaxReq];           // first selected token
+    int64_t slot_lo[kAttnMaxReq];          // first slot in the workspace
+    int32_t ctx_len[kAttnMaxReq], n_sel[kAttnMaxReq], pieces[kAttnMaxReq];
+    int32_t unit_begin[kAttnMaxReq + 1];
+    int32_t sel_begin[kAttnMaxReq + 1];    // selected tokens before the request, in this launch
+    int32_t n_req, piece_tiles;
+};
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4_t v) { return __builtin_bit_cast(bf16x8, v); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    f32x2 f = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+}
+
+// a pair of codes (half `hi` of four) as a pair of bf16, exactly
+template <int CODE, bool HI>
+__device__ __forceinline__ uint32_t pair_of(uint32_t w)
+{
+    if constexpr (CODE == KVS_E4M3) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+    } else {
+        const float a = (float)(int8_t)((w >> (HI ? 16 : 0)) & 0xffu), b = (float)(int8_t)((w >> (HI ? 24 : 8)) & 0xffu);
+        return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);   // whole numbers up to 128: 8 bits are enough
+    }
+}
+
+// Three bf16 that add up to an fp32 number (24 bits in three times 8), for eight numbers.
+__device__ __forceinline__ void split3(const float (&x)[8], u32x4_t (&part)[3])
+{
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = pack2(y[2 * i], y[2 * i + 1]);
+            y[2 * i] -= bf16_lo(w[i]);
+            y[2 * i + 1] -= bf16_hi(w[i]);
+        }
+        part[p] = u32x4_t{w[0], w[1], w[2], w[3]};
+    }
+}
+
+typedef const __attribute__((address_space(4))) float *scalar_f32;    // read by all lanes at one address: scalar loads
+
+template <int DTYPE, int CODE, int D>
+__global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
+    const Table td, int n_q_heads, int n_kv_heads, int64_t n_rows, int block_log2,
+    const uint8_t *__restrict__ k_codes, const uint8_t *__restrict__ v_codes, const float *__restrict__ k_scale, const float *__restrict__ v_scale,
+    const void *__restrict__ q_sel, const int32_t *__restrict__ sel_pos, float scale_log2,
+    void *__restrict__ out, float *__restrict__ lse_out, float *__restrict__ part_o, float4 *__restrict__ part_ml)
+{
+    constexpr int NP = DTYPE == KVS_F32 ? 3 : 1;            // bf16 numbers that Q and the weights enter as
+    constexpr int NDB = D / 32;                             // products of the second kind, channels a lane reads at once
+    constexpr int CPR = D / 16;                             // 16-byte chunks of a row
+    constexpr int RPL = kWave / CPR;                        // rows a load moves
+    constexpr int NL = kKeys / RPL;                         // loads of a K or V tile
+    constexpr int TILE_B = kKeys * D;
+    constexpr int WAVE_B = 4 * TILE_B;                      // two slots of (K, V); later the wave's 32 x D fp32 sums
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float4 ml_s[kWaves][kRows];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hf = lane >> 5, ln = lane & 31;
+
+    const int g = blockIdx.x % n_kv_heads;
+    const int unit = (int)(blockIdx.x / n_kv_heads);
+    const int b = request_of(td.unit_begin, td.n_req, unit);
+    const int in_req = unit - td.unit_begin[b];
+    const int pieces = td.pieces[b], piece = in_req % pieces, row_block = in_req / pieces;
+    const int grp = n_q_heads / n_kv_heads;
+    const int ctx_len = td.ctx_len[b];
+    const int rows = td.n_sel[b] * grp;                     // the host keeps this below 2^31
+    const int64_t sel_lo = td.sel_lo[b];
+
+    // ---- this lane's row (both half-waves hold the same 32) ------------------------------------------------
+    const int rq = min(row_block * kRows + ln, rows - 1);
+    const int t_sel = rq / grp, hh = rq - t_sel * grp;
+    int pos = sel_pos[sel_lo + t_sel];
+    pos = pos < 0 ? -1 : min(pos, ctx_len - 1);
+    int pmin = pos, pmax = pos;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        pmin = min(pmin, __shfl_xor(pmin, o));
+        pmax = max(pmax, __shfl_xor(pmax, o));
+    }
+    pmin = __builtin_amdgcn_readfirstlane(pmin);
+    pmax = __builtin_amdgcn_readfirstlane(pmax);
+
+    // keys are counted from the 16-row boundary at or before the context: x = key + shift
+    const int shift = (int)(td.ctx_off[b] & (kAlign - 1));
+    const int64_t row0 = td.ctx_off[b] - shift;
+    const int xpos = pos < 0 ? -1 : pos + shift;            // last x that the row sees; the first is `shift`
+    const int64_t n_tiles = pmax < 0 ? 0 : ((int64_t)pmax + shift) / kKeys + 1;
+    const int64_t t_lo = (int64_t)piece * td.piece_tiles;
+    const int64_t t_hi = min(n_tiles, t_lo + td.piece_tiles);
+    const int mine = (int)max((int64_t)0, (t_hi - t_lo - wave + kWaves - 1) / kWaves);      // tiles t_lo + wave + 4 i
+
+    // ---- Q as the B operand: k-step 2i + s takes channels 32i + 16hf + 8s .. +7, as the K rows are read below ---
+    bf16x8 qreg[NP][D / 16];
+    {
+        const int64_t at = ((sel_lo + t_sel) * n_q_heads + g * grp + hh) * (int64_t)D + 16 * hf;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            const int c = 32 * (ks >> 1) + 8 * (ks & 1);
+            if constexpr (DTYPE == KVS_BF16) {
+                qreg[0][ks] = as_bf16x8(*reinterpret_cast<const u32x4_t *>((const uint16_t *)q_sel + at + c));
+            } else {
+                const float4 lo = *reinterpret_cast<const float4 *>((const float *)q_sel + at + c), hi = *reinterpret_cast<const float4 *>((const float *)q_sel + at + c + 4);
+                const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                u32x4_t part[3];
+                split3(x, part);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) qreg[p][ks] = as_bf16x8(part[p]);
+            }
+        }
+    }
+
+    // ---- staging ------------------------------------------------------------------------------------------------
+    // A load moves RPL rows of the tile, 16 bytes a lane, to consecutive LDS.  Chunk c of row r lies at position c ^ swz(r):
+    // eight (four) neighbouring rows then use all banks where a chunk is read down the rows.
+    char *const my_lds = lds + wave * WAVE_B;
+    const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)my_lds);
+    const uint32_t row_bytes = (uint32_t)n_kv_heads * D;
+    auto swz = [](int r) { return D == 128 ? (r & 7) : ((r >> 1) & 3); };
+    const int st_row = lane / CPR, st_chunk = (lane % CPR) ^ swz(st_row);
+    const uint32_t st_off = (uint32_t)st_row * row_bytes + (uint32_t)st_chunk * 16u;
+    // Written by hand: issued through the compiler's builtin, every later LDS read would wait for all loads in flight.  M0 holds
+    // the LDS address of lane 0; the nop is the wait state that a write to M0 needs before such a load.
+    auto load_1k = [&](uint32_t dst, uint32_t off, const uint8_t *base) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(base) : "memory");
+    };
+    auto stage = [&](int64_t t, int slot) {
+        const int64_t first = row0 + t * kKeys;
+        const int64_t at = (first * n_kv_heads + g) * D;
+        const uint32_t dst = lds_base + (uint32_t)slot * (2 * TILE_B);
+        if (first + kKeys <= n_rows) {
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                load_1k(dst + j * 1024, st_off + (uint32_t)(j * RPL) * row_bytes, k_codes + at);
+                load_1k(dst + TILE_B + j * 1024, st_off + (uint32_t)(j * RPL) * row_bytes, v_codes + at);
+            }
+        } else {                                            // the cache ends inside: its last row again and again
+            const int last = (int)(n_rows - 1 - first);
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                const uint32_t off = (uint32_t)min(st_row + j * RPL, last) * row_bytes + (uint32_t)st_chunk * 16u;
+                load_1k(dst + j * 1024, off, k_codes + at);
+                load_1k(dst + TILE_B + j * 1024, off, v_codes + at);
+            }
+        }
+    };
+    const scalar_f32 ks_p = (scalar_f32)(uintptr_t)k_scale, vs_p = (scalar_f32)(uintptr_t)v_scale;
+    const int64_t last_block = (n_rows - 1) >> block_log2;
+    struct Scales { float k[2], v[2]; };
+    auto scales_of = [&](int64_t t) {
+        Scales s;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            const int64_t blk = min((row0 + t * kKeys + kAlign * a) >> block_log2, last_block);
+            s.k[a] = ks_p[blk * n_kv_heads + g];
+            s.v[a] = vs_p[blk * n_kv_heads + g];
+        }
+        return s;
+    };
+
+    // ---- running state ------------------------------------------------------------------------------------------
+    floatx16 o_acc[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o_acc[db][r] = 0.f;
+    float m_run = kLowest;     // running maximum of the scores times log2 e, the same in both half-waves
+    float l_run = 0.f;         // this half-wave's share of the sum of weights
+    float l_rnd = 0.f;         // the same of the weights as the second product sees them (bf16)
+    // K row of matrix row ln: bits 2 and 3 swapped, so that accumulator entry r is key 16 (r >> 3) + 8 hf + (r & 7)
+    const int krow = (ln & ~12) | ((ln & 4) << 1) | ((ln & 8) >> 1);
+
+    if (mine > 0) stage(t_lo + wave, 0);
+    if (mine > 1) stage(t_lo + wave + kWaves, 1);
+    Scales next = {};
+    if (mine > 0) next = scales_of(t_lo + wave);
+    for (int i = 0; i < mine; ++i) {
+        const int64_t t = t_lo + wave + (int64_t)kWaves * i;
+        const Scales sc = next;
+        if (i + 1 < mine) next = scales_of(t + kWaves);
+        // this tile has landed; the next one's loads may still be on their way
+        if (i + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * NL) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        char *const kt = my_lds + (i & 1) * (2 * TILE_B);
+        char *const vt = kt + TILE_B;
+        const int x0 = (int)(t * kKeys);                     // (contexts are shorter than 2^31)
+        const bool masked = x0 < shift || x0 + kKeys - 1 > pmin + shift || pmin < 0;
+
+        // Memory that was never stored to may hold NaN codes: in rows that are masked, and in blocks of scale 0.
+        if (CODE == KVS_E4M3 && (masked || sc.k[0] == 0.f || sc.k[1] == 0.f || sc.v[0] == 0.f || sc.v[1] == 0.f)) {
+#pragma unroll
+            for (int e = 0; e < 2 * TILE_B / 1024; ++e) {
+                u32x4_t *w = reinterpret_cast<u32x4_t *>(kt) + e * kWave + lane;
+                u32x4_t c = *w;
+                c.x = numbers_only(c.x); c.y = numbers_only(c.y); c.z = numbers_only(c.z); c.w = numbers_only(c.w);
+                *w = c;
+            }
+        }
+        floatx16 s = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(kt + krow * D + ((2 * c + hf) ^ swz(krow)) * 16);
+            const u32x4_t lo = {pair_of<CODE, false>(w.x), pair_of<CODE, true>(w.x), pair_of<CODE, false>(w.y), pair_of<CODE, true>(w.y)};
+            const u32x4_t hi = {pair_of<CODE, false>(w.z), pair_of<CODE, true>(w.z), pair_of<CODE, false>(w.w), pair_of<CODE, true>(w.w)};
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(lo), qreg[p][2 * c], s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(hi), qreg[p][2 * c + 1], s, 0, 0, 0);
+            }
+        }
+        bool seen[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int x = x0 + 16 * (r >> 3) + 8 * hf + (r & 7);
+            seen[r] = !masked || (x >= shift && x <= xpos);
+            const float y = s[r] * (sc.k[r >> 3] * scale_log2);
+            s[r] = seen[r] ? y : -INFINITY;                 // behind the scale, which may be a NaN
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m_run, mx);
+        const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        u32x4_t pop[2][NP];
+        float psum = 0.f, rsum = 0.f;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            float y[8], group = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float p = __builtin_amdgcn_exp2f(s[8 * a + j] - m_new);
+                group += p;
+                y[j] = seen[8 * a + j] ? p * sc.v[a] : 0.f;
+            }
+            psum += group;
+            if constexpr (DTYPE == KVS_BF16) {
+                // The normaliser is made of the rounded weights: numerator and denominator then carry the same rounding, and a
+                // row that one key dominates returns that key's V to within the output's own rounding.
+                typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                float rounded = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = pack2(y[2 * j], y[2 * j + 1]);
+                    pop[a][0][j] = w;
+                    rounded = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3f803f80u), rounded, false);
+                }
+                // (scales below 2^-80 would bring weights below what bf16 holds)
+                rsum += sc.v[a] > 8.271806e-25f ? rounded * __builtin_amdgcn_rcpf(sc.v[a]) : group;
+            } else {
+                split3(y, pop[a]);
+            }
+        }
+        if (__builtin_amdgcn_ballot_w64(corr != 1.0f) != 0) {
+            l_run *= corr;
+            l_rnd *= corr;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o_acc[db][r] *= corr;
+        }
+        l_run += psum;
+        l_rnd += rsum;
+
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            uint32_t lo[8], hi[8];                          // channels 0, 1 and 2, 3 of the lane's four, key by key
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int key = 16 * a + 8 * hf + j;
+                const int chunk = NDB == 4 ? ln >> 2 : ln >> 3, in_chunk = NDB == 4 ? (ln & 3) * 4 : (ln & 7) * 2;
+                const char *p = vt + key * D + (chunk ^ swz(key)) * 16 + in_chunk;
+                const uint32_t w = NDB == 4 ? *reinterpret_cast<const uint32_t *>(p) : (uint32_t) * reinterpret_cast<const uint16_t *>(p);
+                lo[j] = pair_of<CODE, false>(w);
+                hi[j] = NDB == 4 ? pair_of<CODE, true>(w) : 0u;
+            }
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) {
+                const uint32_t *from = db < 2 ? lo : hi;
+                const uint32_t sel = (db & 1) ? 0x07060302u : 0x05040100u;
+                const u32x4_t va = {__builtin_amdgcn_perm(from[1], from[0], sel), __builtin_amdgcn_perm(from[3], from[2], sel),
+                                    __builtin_amdgcn_perm(from[5], from[4], sel), __builtin_amdgcn_perm(from[7], from[6], sel)};
+#pragma unroll
+                for (int p = 0; p < NP; ++p) o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va), as_bf16x8(pop[a][p]), o_acc[db], 0, 0, 0);
+            }
+        }
+        if (i + 2 < mine) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // what lay in the slot has been read
+            stage(t + 2 * kWaves, i & 1);
+        }
+    }
+
+    // ---- the waves meet --------------------------------------------------------------------------------------------
+    {
+        const float l = l_run + __shfl_xor(l_run, 32), lr = l_rnd + __shfl_xor(l_rnd, 32);
+        if (hf == 0) ml_s[wave][ln] = make_float4(m_run, l, DTYPE == KVS_BF16 ? lr : l, 0.f);
+    }
+    __syncthreads();
+    {
+        float top = ml_s[0][ln].x;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml_s[w][ln].x);
+        const float f = __builtin_amdgcn_exp2f(m_run - top);
+        float *mine_o = reinterpret_cast<float *>(my_lds) + ln * D;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int m = 8 * (r >> 2) + 4 * hf + (r & 3);   // channels NDB m .. : at place m ^ row, so that rows use different banks
+            float *p = mine_o + (m ^ ln) * NDB;
+            if constexpr (NDB == 4) *reinterpret_cast<float4 *>(p) = make_float4(o_acc[0][r] * f, o_acc[1][r] * f, o_acc[2][r] * f, o_acc[3][r] * f);
+            else *reinterpret_cast<float2 *>(p) = make_float2(o_acc[0][r] * f, o_acc[1][r] * f);
+        }
+    }
+    __syncthreads();
+    constexpr int CPT = D / 8;                               // channels a thread stores
+    const int row = tid >> 3, part = tid & 7;
+    const int row_q = row_block * kRows + row;
+    if (row_q >= rows) return;
+    float top = kLowest, l = 0.f, lr = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml_s[w][row].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const float4 x = ml_s[w][row];
+        const float f = __builtin_amdgcn_exp2f(x.x - top);
+        l += x.y * f;
+        lr += x.z * f;
+    }
+    float o[CPT];
+#pragma unroll
+    for (int c = 0; c < CPT; ++c) o[c] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const float *from = reinterpret_cast<const float *>(lds + w * WAVE_B) + row * D;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float *p = from + ((4 * part + k) ^ row) * NDB;
+#pragma unroll
+            for (int c = 0; c < NDB; ++c) o[k * NDB + c] += p[c];
+        }
+    }
+    const int t2 = row_q / grp, h2 = row_q - t2 * grp;
+    const int64_t at = (sel_lo + t2) * n_q_heads + g * grp + h2;
+    if (pieces > 1) {
+        const int64_t slot = td.slot_lo[b] + ((int64_t)t2 * n_q_heads + g * grp + h2) * pieces + piece;
+        if (part == 0) part_ml[slot] = make_float4(top, l, lr, 0.f);
+        if (l != 0.f) {                                      // (the merge passes over a piece without keys)
+            float4 *dst = reinterpret_cast<float4 *>(part_o + slot * D + part * CPT);
+#pragma unroll
+            for (int c = 0; c < CPT / 4; ++c) dst[c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+        }
+        return;
+    }
+    const float inv = l != 0.f ? 1.f / lr : 0.f;
+#pragma unroll
+    for (int c = 0; c < CPT; ++c) o[c] = l != 0.f ? o[c] * inv : 0.f;
+    if constexpr (DTYPE == KVS_BF16) {
+        uint4 *dst = reinterpret_cast<uint4 *>((uint16_t *)out + at * D + part * CPT);
+#pragma unroll
+        for (int c = 0; c < CPT / 8; ++c)
+            dst[c] = make_uint4(pack2(o[8 * c], o[8 * c + 1]), pack2(o[8 * c + 2], o[8 * c + 3]), pack2(o[8 * c + 4], o[8 * c + 5]), pack2(o[8 * c + 6], o[8 * c + 7]));
+    } else {
+        float4 *dst = reinterpret_cast<float4 *>((float *)out + at * D + part * CPT);
+#pragma unroll
+        for (int c = 0; c < CPT / 4; ++c) dst[c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+    }
+    if (lse_out && part == 0) lse_out[at] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+}
+
+// out = sum_p w_p O_p / sum_p w_p l_p with w_p = 2^(m_p - max m).  A wave takes one row, a lane D / 64 channels.
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kThreads) void merge8_kernel(const Table td, int n_q_heads, int64_t n_items, const float *__restrict__ part_o,
+                                                          const float4 *__restrict__ part_ml, void *__restrict__ out, float *__restrict__ lse_out)
+{
+    constexpr int C = D / 64;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= n_items) return;
+    const int s = (int)(item / n_q_heads);
+    const int b = request_of(td.sel_begin, td.n_req, s);
+    const int pieces = td.pieces[b];
+    if (pieces <= 1) return;                                 // stored as it is by its only workgroup
+    const int64_t local = item - (int64_t)td.sel_begin[b] * n_q_heads;
+    const int64_t slot = td.slot_lo[b] + local * pieces;
+    float top = kLowest;
+    for (int p = lane; p < pieces; p += 64) top = fmaxf(top, part_ml[slot + p].x);
+    top = wave_max(top);
+    float l = 0.f, lr = 0.f;
+    for (int p = lane; p < pieces; p += 64) {
+        const float4 x = part_ml[slot + p];
+        const float f = __builtin_amdgcn_exp2f(x.x - top);
+        l += x.y * f;
+        lr += x.z * f;
+    }
+    l = wave_sum(l);
+    lr = wave_sum(lr);
+    float o[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < pieces; ++p) {
+        const float4 x = part_ml[slot + p];
+        if (x.y == 0.f) continue;
+        const float f = __builtin_amdgcn_exp2f(x.x - top);
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] += f * part_o[(slot + p) * D + lane * C + c];
+    }
+    const int64_t at = td.sel_lo[b] * n_q_heads + local;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = l != 0.f ? o[c] / lr : 0.f;
+    if constexpr (DTYPE == KVS_BF16) {
+        if constexpr (C == 2) *reinterpret_cast<uint32_t *>((uint16_t *)out + at * D + lane * C) = pack2(o[0], o[1]);
+        else ((uint16_t *)out)[at * D + lane] = (uint16_t)f32_to_bf16_bits(o[0]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c) ((float *)out)[at * D + lane * C + c] = o[c];
+    }
+    if (lse_out && lane == 0) lse_out[at] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+}
+
+inline size_t slot_bytes(int d) { return (size_t)d * sizeof(float) + sizeof(float4); }
+
+// How a launch's key ranges are cut: pieces of `piece_tiles` tiles (0: not at all).
+struct Plan { int64_t piece_tiles, slots; };
+
+inline int64_t tiles_of(int64_t ctx_len) { return (ctx_len + kAlign - 1 + kKeys - 1) / kKeys; }    // wherever in a block it begins
+inline int64_t blocks_of(int64_t n_sel, int grp) { return (n_sel * grp + kRows - 1) / kRows; }
+
+Plan plan_pieces(const kvs_shape *shape, int32_t n_req, const int64_t *ctx_len, const int64_t *cu_sel, size_t workspace_bytes)
+{
+    const int grp = shape->n_q_heads / shape->n_kv_heads, hk = shape->n_kv_heads;
+    int64_t units = 0, tiles = 0;
+    for (int32_t b = 0; b < n_req; ++b) {
+        const int64_t n = blocks_of(cu_sel[b + 1] - cu_sel[b], grp);
+        units += n * hk;
+        tiles += n * hk * tiles_of(ctx_len[b]);
+    }
+    if (units >= kSplitBelow) return {0, 0};
+    int64_t piece = (tiles + kTargetWgs - 1) / kTargetWgs;
+    if (piece < kMinPieceTiles) piece = kMinPieceTiles;
+    for (;; piece *= 2) {
+        piece = (piece + kWaves - 1) / kWaves * kWaves;
+        int64_t slots = 0, most = 1;
+        for (int32_t b = 0; b < n_req; ++b) {
+            const int64_t n = cu_sel[b + 1] - cu_sel[b];
+            const int64_t p = n ? (tiles_of(ctx_len[b]) + piece - 1) / piece : 1;
+            if (p > 1) slots += n * shape->n_q_heads * p;
+            if (p > most) most = p;
+        }
+        if (most <= 1) return {0, 0};
+        if (most <= kMaxPieces && (size_t)slots * slot_bytes(shape->head_dim) <= workspace_bytes) return {piece, slots};
+    }
+}
+
+template <int DTYPE, int CODE, int D>
+kvs_status launch(const kvs_shape *shape, const kvs_cache8 *c, const Table &td, int64_t wgs, const void *q_sel, const int32_t *sel_pos, float scale,
+                  void *out, float *lse_out, float *part_o, float4 *part_ml, hipStream_t hs)
+{
+    static DeviceOnce once;
+    constexpr int lds = kWaves * 4 * kKeys * D;
+    const kvs_status st = once_per_device(once, [&]() -> kvs_status {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention8_kernel<DTYPE, CODE, D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_attention_kv8: %s", hipGetErrorString(e));
+    });
+    if (st != KVS_OK) return st;
+    hipLaunchKernelGGL((attention8_kernel<DTYPE, CODE, D>), dim3((unsigned)wgs), dim3(kThreads), lds, hs, td, shape->n_q_heads, shape->n_kv_heads, c->n_rows,
+                       __builtin_ctz((unsigned)c->block), (const uint8_t *)c->k, (const uint8_t *)c->v, c->k_scale, c->v_scale, q_sel, sel_pos,
+                       scale * 1.4426950408889634f, out, lse_out, part_o, part_ml);
+    return check_launch("kvs_attention_kv8");
+}
+
+} // namespace
+
+size_t attention8_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t n_rows_total, int64_t n_sel_total)
+{
+    // a launch that is cut has fewer than kSplitBelow units, and its pieces are at most kTargetWgs and one more a unit; 32 rows each
+    if (check_shape(shape) != KVS_OK || n_sel_total <= 0) return 256;
+    int64_t pieces = tiles_of(n_rows_total) / kMinPieceTiles + 1;
+    if (pieces > kMaxPieces) pieces = kMaxPieces;
+    const int64_t most = (int64_t)kRows * (kSplitBelow + kTargetWgs);
+    int64_t slots = most;
+    if (n_sel_total < most && n_sel_total * shape->n_q_heads < most) slots = n_sel_total * shape->n_q_heads * pieces < most ? n_sel_total * shape->n_q_heads * pieces : most;
+    return ((size_t)slots * slot_bytes(shape->head_dim) + 255) / 256 * 256;
+}
+
+} // namespace kvs
+
+extern "C" kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8 *cache, int32_t batch,
+                                        const int64_t *ctx_off, const int64_t *ctx_len, const int64_t *cu_sel,
+                                        const void *q_sel, const int32_t *sel_pos, float scale,
+                                        void *out, float *lse_out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace kvs;
+    const char *me = "kvs_attention_kv8";
+    kvs_status st = check_shape(shape);
+    if (st != KVS_OK || (st = check_cache8(me, shape, cache)) != KVS_OK) return st;
+    if (batch < 0) return fail(KVS_EINVAL, "%s: batch < 0", me);
+    if (!isfinite(scale)) return fail(KVS_EINVAL, "%s: the scale is not finite", me);
+    if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return fail(KVS_EINVAL, "%s: workspace must be 256-byte aligned", me);
+    if (!workspace) workspace_bytes = 0;
+    if (batch == 0) return KVS_OK;
+    if (!ctx_off || !ctx_len || !cu_sel) return fail(KVS_EINVAL, "%s: ctx_off/ctx_len/cu_sel is NULL", me);
+    if (cu_sel[0] != 0) return fail(KVS_EINVAL, "%s: cu_sel[0] must be 0", me);
+    const int grp = shape->n_q_heads / shape->n_kv_heads;
+    for (int32_t b = 0; b < batch; ++b) {
+        if (ctx_off[b] < 0 || ctx_len[b] < 0 || ctx_off[b] > cache->n_rows - ctx_len[b])
+            return fail(KVS_EINVAL, "%s: request %d's rows %lld .. +%lld lie outside a cache of %lld", me, b, (long long)ctx_off[b], (long long)ctx_len[b], (long long)cache->n_rows);
+        if (ctx_len[b] > 0x7fffff00LL) return fail(KVS_EINVAL, "%s: context of request %d too long", me, b);
+        if (cu_sel[b + 1] < cu_sel[b]) return fail(KVS_EINVAL, "%s: cu_sel decreases at request %d", me, b);
+        if ((cu_sel[b + 1] - cu_sel[b]) > 0x7fffff00LL / shape->n_q_heads) return fail(KVS_EINVAL, "%s: request %d selects too many tokens", me, b);
+    }
+    if (cu_sel[batch] == 0) return KVS_OK;
+    if (!q_sel || !sel_pos || !out) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
+    if (!aligned16(q_sel) || !aligned16(out)) return fail(KVS_EINVAL, "%s: Q/out pointers must be 16-byte aligned", me);
+    hipStream_t hs = (hipStream_t)stream;
+    for (int32_t b0 = 0; b0 < batch; b0 += kAttnMaxReq) {
+        const int nr = (batch - b0) < kAttnMaxReq ? (batch - b0) : kAttnMaxReq;
+        const int64_t n_sel = cu_sel[b0 + nr] - cu_sel[b0];
+        if (n_sel == 0) continue;
+        if (n_sel > 0x7fffff00LL / shape->n_q_heads) return fail(KVS_EINVAL, "%s: %lld selected tokens in one launch", me, (long long)n_sel);
+        const Plan plan = plan_pieces(shape, nr, ctx_len + b0, cu_sel + b0, workspace_bytes);
+        Table td = {};
+        td.n_req = nr;
+        td.piece_tiles = plan.piece_tiles ? (int32_t)plan.piece_tiles : 0x7fffffff;
+        int64_t units = 0, slot = 0;
+        for (int i = 0; i < kAttnMaxReq; ++i) {
+            td.unit_begin[i] = (int32_t)units;
+            td.sel_begin[i] = i < nr ? (int32_t)(cu_sel[b0 + i] - cu_sel[b0]) : (int32_t)n_sel;
+            if (i >= nr) continue;
+            const int64_t n = cu_sel[b0 + i + 1] - cu_sel[b0 + i];
+            const int64_t p = n && plan.piece_tiles ? (tiles_of(ctx_len[b0 + i]) + plan.piece_tiles - 1) / plan.piece_tiles : 1;
+            td.ctx_off[i] = ctx_off[b0 + i];
+            td.sel_lo[i] = cu_sel[b0 + i];
+            td.slot_lo[i] = slot;
+            td.ctx_len[i] = (int32_t)ctx_len[b0 + i];
+            td.n_sel[i] = (int32_t)n;
+            td.pieces[i] = (int32_t)(p > 1 ? p : 1);
+            if (p > 1) slot += n * shape->n_q_heads * p;
+            units += blocks_of(n, grp) * td.pieces[i];
+            if (units * shape->n_kv_heads > 0x7fffffff / kThreads) return fail(KVS_EINVAL, "%s: too many rows in one launch", me);
+        }
+        td.unit_begin[kAttnMaxReq] = (int32_t)units;
+        td.sel_begin[kAttnMaxReq] = (int32_t)n_sel;
+        float4 *ml = reinterpret_cast<float4 *>(workspace);
+        float *po = reinterpret_cast<float *>(ml + plan.slots);
+        const int64_t wgs = units * shape->n_kv_heads, items = n_sel * shape->n_q_heads;
+        const bool e4m3 = cache->code == KVS_E4M3, wide = shape->head_dim == 128, bf16 = shape->dtype == KVS_BF16;
+#define KVS_A8(DT, C, DD) launch<DT, C, DD>(shape, cache, td, wgs, q_sel, sel_pos, scale, out, lse_out, po, ml, hs)
+        if (bf16) st = e4m3 ? (wide ? KVS_A8(KVS_BF16, KVS_E4M3, 128) : KVS_A8(KVS_BF16, KVS_E4M3, 64)) : (wide ? KVS_A8(KVS_BF16, KVS_INT8, 128) : KVS_A8(KVS_BF16, KVS_INT8, 64));
+        else st = e4m3 ? (wide ? KVS_A8(KVS_F32, KVS_E4M3, 128) : KVS_A8(KVS_F32, KVS_E4M3, 64)) : (wide ? KVS_A8(KVS_F32, KVS_INT8, 128) : KVS_A8(KVS_F32, KVS_INT8, 64));
+#undef KVS_A8
+        if (st != KVS_OK) return st;
+        if (!plan.piece_tiles) continue;
+        const dim3 grid((unsigned)((items + kWaves - 1) / kWaves)), threads(kThreads);
+#define KVS_M8(DT, DD) hipLaunchKernelGGL((merge8_kernel<DT, DD>), grid, threads, 0, hs, td, shape->n_q_heads, items, po, ml, out, lse_out)
+        if (bf16) { if (wide) KVS_M8(KVS_BF16, 128); else KVS_M8(KVS_BF16, 64); }
+        else { if (wide) KVS_M8(KVS_F32, 128); else KVS_M8(KVS_F32, 64); }
+#undef KVS_M8
+        if ((st = check_launch("kvs_attention_kv8")) != KVS_OK) return st;
+    }
+    return KVS_OK;
+}
