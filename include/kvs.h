@@ -463,7 +463,7 @@ typedef struct {
  *                  outside [0, n_rows) are skipped; they count as a block of their own.
  *
  * For each block that takes a row, each KV head, K and V apart, with top = 448 (KVS_E4M3) or 127 (KVS_INT8), in fp32:
- *     need  = max |x| over the rows that the block takes / top, at least 2^-126 (0 if they are all zero)
+ *     need  = max |x| over the rows that the block takes * (1 / top), at least 2^-126 (0 if they are all zero)
  *     scale = max(need, old scale), or need alone if all of the block's rows in the cache are taken
  *     code  = nearest code (ties to even) to x * (1 / scale)      for the rows taken
  *     code  = nearest code to code * (old scale / scale)          for the other rows, where the scale has changed

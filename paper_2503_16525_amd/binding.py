@@ -289,41 +289,60 @@ def rotary_spec(rotary_dim: int, layout: str = "half", scaling: str = "plain", b
     return RotarySpec(rotary_dim, ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], original, base, factor, low, high, magnitude)
 
 
-def _rows(t: Optional[torch.Tensor], shape: Shape, heads: int, n: int):
-    """Address and row stride of [n, heads, head_dim] rows, each row in one piece, rows any distance apart."""
+# The calls below refuse, on the host, what lies on another device than the current one (their kernels run there), has
+# another type, or fewer entries than the call will touch.
+
+def _device() -> int:
+    return _current_device() if _current_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+
+
+def _refuse(t: torch.Tensor, dev: int, dtype: torch.dtype, n: int, what: str) -> None:
+    if not t.is_cuda:
+        raise TypeError(f"{what}: device tensor expected")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on device {t.get_device()}, the current device is {dev}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise TypeError(f"{what}: contiguous tensor expected")
+    raise ValueError(f"{what} has {t.numel()} entries, {n} are needed")
+
+
+def _at(t: Optional[torch.Tensor], dev: int, dtype: torch.dtype, n: int, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+        _refuse(t, dev, dtype, n, what)
+    return t.data_ptr()
+
+
+def _rows_at(t: Optional[torch.Tensor], dev: int, dtype: torch.dtype, n: int, heads: int, d: int, what: str):
+    """Address and row stride of [n, heads, d] rows, each row in one piece, rows any distance apart."""
     if t is None:
         return None, 0
-    if not t.is_cuda:
-        raise TypeError("device tensor expected")
-    if t.shape != (n, heads, shape.head_dim) or _dtype_code(t) != shape.dtype:
-        raise ValueError(f"expected {(n, heads, shape.head_dim)} in the shape's dtype, got {tuple(t.shape)} {t.dtype}")
-    if n and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != shape.head_dim)):
-        raise TypeError("the heads of a row have to be contiguous")
-    return t.data_ptr(), t.stride(0) if n > 1 else heads * shape.head_dim
+    if t.shape != (n, heads, d):
+        raise ValueError(f"{what}: expected {(n, heads, d)}, got {tuple(t.shape)}")
+    if t.dtype is not dtype or t.get_device() != dev:
+        _refuse(t, dev, dtype, 0, what)
+    row, head, one = t.stride()
+    if n and (one != 1 or (heads > 1 and head != d)):
+        raise TypeError(f"{what}: the heads of a row have to be contiguous")
+    return t.data_ptr(), row if n > 1 else heads * d
 
 
-def _one_device(*tensors) -> None:
-    """The kernels run on the current device: what lies on another one is refused."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != dev:
-            raise ValueError(f"tensor on device {t.get_device()}, the current device is {dev}")
-
-
-def _entries(t: Optional[torch.Tensor], n: int, what: str) -> None:
-    if t is not None and t.numel() < n:
-        raise ValueError(f"{what} has {t.numel()} entries, {n} are needed")
+_TYPES = {F32: torch.float32, BF16: torch.bfloat16}
 
 
 def kvs_rotary(shape: Shape, spec: RotarySpec, pos, pos_from, q, k, q_out, k_out, stream=None) -> None:
-    n = pos.numel()
-    _one_device(pos, pos_from, q, k, q_out, k_out)
-    _entries(pos_from, n, "pos_from")
-    (qp, qs), (qop, qos) = (_rows(t, shape, shape.n_q_heads, n) for t in (q, q_out))
-    (kp, ks), (kop, kos) = (_rows(t, shape, shape.n_kv_heads, n) for t in (k, k_out))
-    rc = load().kvs_rotary(ctypes.byref(shape), ctypes.byref(spec), n, _ptr(pos, torch.int32), _ptr(pos_from, torch.int32),
-                           qp, qs, kp, ks, qop, qos, kop, kos, _stream(stream))
-    _check(rc, "kvs_rotary")
+    n, dev, dt, d = pos.numel(), _device(), _TYPES[shape.dtype], shape.head_dim
+    qp, qs = _rows_at(q, dev, dt, n, shape.n_q_heads, d, "q")
+    qo, qos = _rows_at(q_out, dev, dt, n, shape.n_q_heads, d, "q_out")
+    kp, ks = _rows_at(k, dev, dt, n, shape.n_kv_heads, d, "k")
+    ko, kos = _rows_at(k_out, dev, dt, n, shape.n_kv_heads, d, "k_out")
+    rc = load().kvs_rotary(shape, spec, n, _at(pos, dev, torch.int32, n, "pos"), _at(pos_from, dev, torch.int32, n, "pos_from"),
+                           qp, qs, kp, ks, qo, qos, ko, kos, _stream(stream))
+    if rc:
+        _check(rc, "kvs_rotary")
 
 
 class Cache8:
@@ -343,6 +362,9 @@ class Cache8:
             raise ValueError(f"scales are {list(blocks)}, not {list(k_scale.shape)}, {list(v_scale.shape)}")
         self.k, self.v, self.k_scale, self.v_scale, self.block = k, v, k_scale, v_scale, block
         self.n_rows, self.n_kv_heads, self.head_dim = k.shape
+        self.device = k.get_device()
+        if any(t.get_device() != self.device for t in (v, k_scale, v_scale)):
+            raise ValueError("the cache's tensors are on one device")
         self.raw = _Cache8(_ptr(k), _ptr(v), _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), k.shape[0], block, codes[k.dtype])
 
     @classmethod
@@ -354,39 +376,35 @@ class Cache8:
         return cls(k, v, ks, vs, block)
 
 
-def _cache8(cache: Cache8, shape: Shape):
-    if (cache.n_kv_heads, cache.head_dim) != (shape.n_kv_heads, shape.head_dim):
+def _cache8(cache: Cache8, shape: Shape, dev: int) -> _Cache8:
+    if cache.n_kv_heads != shape.n_kv_heads or cache.head_dim != shape.head_dim:
         raise ValueError(f"the cache has {cache.n_kv_heads} KV heads of {cache.head_dim}, the shape {shape.n_kv_heads} of {shape.head_dim}")
-    return ctypes.byref(cache.raw)
+    if cache.device != dev:
+        raise ValueError(f"the cache is on device {cache.device}, the current device is {dev}")
+    return cache.raw
 
 
 def kvs_store_kv8(shape: Shape, cache: Cache8, k_new, v_new, sel_pos, row0: int = 0, reused=None, dev_v=None, stream=None) -> None:
-    n = k_new.shape[0]
-    _one_device(cache.k, k_new, v_new, sel_pos, reused, dev_v)
-    for t in (k_new, v_new):
-        _rows(t, shape, shape.n_kv_heads, n)
-    _entries(sel_pos, n, "sel_pos")
-    _entries(reused, cache.n_rows, "reused")
-    _entries(dev_v, cache.n_rows * shape.n_kv_heads, "dev_v")
-    rc = load().kvs_store_kv8(ctypes.byref(shape), _cache8(cache, shape), _ptr(k_new), _ptr(v_new), _ptr(sel_pos, torch.int32), row0, n,
-                              _ptr(reused, torch.uint8), _ptr(dev_v, torch.float32), _stream(stream))
-    _check(rc, "kvs_store_kv8")
+    n, dev, dt = k_new.shape[0], _device(), _TYPES[shape.dtype]
+    cells = n * shape.n_kv_heads * shape.head_dim
+    rc = load().kvs_store_kv8(shape, _cache8(cache, shape, dev), _at(k_new, dev, dt, cells, "k_new"), _at(v_new, dev, dt, cells, "v_new"),
+                              _at(sel_pos, dev, torch.int32, n, "sel_pos"), row0, n, _at(reused, dev, torch.uint8, cache.n_rows, "reused"),
+                              _at(dev_v, dev, torch.float32, cache.n_rows * shape.n_kv_heads, "dev_v"), _stream(stream))
+    if rc:
+        _check(rc, "kvs_store_kv8")
 
 
 def kvs_deviation_kv8(shape: Shape, cache: Cache8, row0: int, n_tokens: int, k_fresh, v_fresh, reused, alpha, mode: int,
                       dev_k, dev_v, score, stream=None) -> None:
-    _one_device(cache.k, k_fresh, v_fresh, reused, alpha, dev_k, dev_v, score)
-    cells = n_tokens * shape.n_kv_heads
-    for t, n, what in ((k_fresh, cells * shape.head_dim, "k_fresh"), (v_fresh, cells * shape.head_dim, "v_fresh"), (reused, n_tokens, "reused"),
-                       (alpha, cells, "alpha"), (dev_k, cells, "dev_k"), (dev_v, cells, "dev_v"), (score, n_tokens, "score")):
-        _entries(t, n, what)
-    for t in (k_fresh, v_fresh):
-        if t is not None and _dtype_code(t) != shape.dtype:
-            raise TypeError(f"fresh rows are in the shape's dtype, not {t.dtype}")
-    rc = load().kvs_deviation_kv8(ctypes.byref(shape), _cache8(cache, shape), row0, n_tokens, _ptr(k_fresh), _ptr(v_fresh),
-                                  _ptr(reused, torch.uint8), _ptr(alpha, torch.float32), mode, _ptr(dev_k, torch.float32),
-                                  _ptr(dev_v, torch.float32), _ptr(score, torch.float32), _stream(stream))
-    _check(rc, "kvs_deviation_kv8")
+    dev, dt, f32 = _device(), _TYPES[shape.dtype], torch.float32
+    heads = n_tokens * shape.n_kv_heads
+    cells = heads * shape.head_dim
+    rc = load().kvs_deviation_kv8(shape, _cache8(cache, shape, dev), row0, n_tokens, _at(k_fresh, dev, dt, cells, "k_fresh"),
+                                  _at(v_fresh, dev, dt, cells, "v_fresh"), _at(reused, dev, torch.uint8, n_tokens, "reused"),
+                                  _at(alpha, dev, f32, heads, "alpha"), mode, _at(dev_k, dev, f32, heads, "dev_k"),
+                                  _at(dev_v, dev, f32, heads, "dev_v"), _at(score, dev, f32, n_tokens, "score"), _stream(stream))
+    if rc:
+        _check(rc, "kvs_deviation_kv8")
 
 
 def kvs_attention_kv8(shape: Shape, cache: Cache8, ctx_off: Sequence[int], ctx_len: Sequence[int], cu_sel: Sequence[int],
@@ -394,19 +412,17 @@ def kvs_attention_kv8(shape: Shape, cache: Cache8, ctx_off: Sequence[int], ctx_l
     co, cl, cs = _i64(ctx_off), _i64(ctx_len), _i64(cu_sel)
     if co.n != cl.n or cs.n != co.n + 1:
         raise ValueError("ctx_off/ctx_len need one entry per request and cu_sel one more")
-    n = int(cs.data[-1])
-    _one_device(cache.k, q_sel, sel_pos, out, lse_out, workspace)
-    for t, cells, what in ((q_sel, n * shape.n_q_heads * shape.head_dim, "q_sel"), (out, n * shape.n_q_heads * shape.head_dim, "out"),
-                           (sel_pos, n, "sel_pos"), (lse_out, n * shape.n_q_heads, "lse_out")):
-        _entries(t, cells, what)
-    for t in (q_sel, out):
-        if t is not None and _dtype_code(t) != shape.dtype:
-            raise TypeError(f"q_sel and out are in the shape's dtype, not {t.dtype}")
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    rc = load().kvs_attention_kv8(ctypes.byref(shape), _cache8(cache, shape), co.n, co.ptr, cl.ptr, cs.ptr, _ptr(q_sel),
-                                  _ptr(sel_pos, torch.int32), scale, _ptr(out), _ptr(lse_out, torch.float32), _ptr(workspace), ws_bytes,
-                                  _stream(stream))
-    _check(rc, "kvs_attention_kv8")
+    n, dev, dt = int(cs.data[-1]), _device(), _TYPES[shape.dtype]
+    heads = n * shape.n_q_heads
+    cells = heads * shape.head_dim
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        ws, ws_bytes = _at(workspace, dev, workspace.dtype, 0, "workspace"), workspace.numel() * workspace.element_size()
+    rc = load().kvs_attention_kv8(shape, _cache8(cache, shape, dev), co.n, co.ptr, cl.ptr, cs.ptr, _at(q_sel, dev, dt, cells, "q_sel"),
+                                  _at(sel_pos, dev, torch.int32, n, "sel_pos"), scale, _at(out, dev, dt, cells, "out"),
+                                  _at(lse_out, dev, torch.float32, heads, "lse_out"), ws, ws_bytes, _stream(stream))
+    if rc:
+        _check(rc, "kvs_attention_kv8")
 
 
 def shape_of(workload) -> Shape:

@@ -424,55 +424,77 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     if (lse_out && part == 0) lse_out[at] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
-// out = sum_p w_p O_p / sum_p w_p l_p with w_p = 2^(m_p - max m).  A wave takes one row, a lane D / 64 channels.
+// out = sum_p w_p O_p / sum_p w_p l_p with w_p = 2^(m_p - max m).  A workgroup takes one row: its threads make the pieces'
+// weights once, into LDS, then groups of D / 4 threads take every kGroups-th piece, four channels a thread, and meet in LDS.
+// (A wave a row, piece after piece, spent its time on one round trip to memory after the other: 256 pieces 80 us.)
 template <int DTYPE, int D>
-__global__ __launch_bounds__(kThreads) void merge8_kernel(const Table td, int n_q_heads, int64_t n_items, const float *__restrict__ part_o,
+__global__ __launch_bounds__(kThreads) void merge8_kernel(const Table td, int n_q_heads, const float *__restrict__ part_o,
                                                           const float4 *__restrict__ part_ml, void *__restrict__ out, float *__restrict__ lse_out)
 {
-    constexpr int C = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (item >= n_items) return;
-    const int s = (int)(item / n_q_heads);
-    const int b = request_of(td.sel_begin, td.n_req, s);
+    constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
+    __shared__ float weight[kMaxPieces];
+    __shared__ float meet[3][kWaves];
+    __shared__ float4 sum_s[kGroups][kLanes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int item = (int)blockIdx.x;
+    const int b = request_of(td.sel_begin, td.n_req, item / n_q_heads);
     const int pieces = td.pieces[b];
     if (pieces <= 1) return;                                 // stored as it is by its only workgroup
     const int64_t local = item - (int64_t)td.sel_begin[b] * n_q_heads;
     const int64_t slot = td.slot_lo[b] + local * pieces;
+    static_assert(kMaxPieces == 2 * kThreads, "two records a thread");
+    float4 x[2];
     float top = kLowest;
-    for (int p = lane; p < pieces; p += 64) top = fmaxf(top, part_ml[slot + p].x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int p = tid + i * kThreads;
+        x[i] = p < pieces ? part_ml[slot + p] : make_float4(kLowest, 0.f, 0.f, 0.f);
+        top = fmaxf(top, x[i].x);
+    }
     top = wave_max(top);
+    if (lane == 0) meet[0][wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, meet[0][w]);
     float l = 0.f, lr = 0.f;
-    for (int p = lane; p < pieces; p += 64) {
-        const float4 x = part_ml[slot + p];
-        const float f = __builtin_amdgcn_exp2f(x.x - top);
-        l += x.y * f;
-        lr += x.z * f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float f = __builtin_amdgcn_exp2f(x[i].x - top);
+        l += x[i].y * f;
+        lr += x[i].z * f;
+        if (tid + i * kThreads < pieces) weight[tid + i * kThreads] = x[i].y != 0.f ? f : -1.f;      // (-1: a piece without keys has left no sums)
     }
     l = wave_sum(l);
     lr = wave_sum(lr);
-    float o[C];
+    if (lane == 0) { meet[1][wave] = l; meet[2][wave] = lr; }
+    __syncthreads();
+    l = (meet[1][0] + meet[1][1]) + (meet[1][2] + meet[1][3]);
+    lr = (meet[2][0] + meet[2][1]) + (meet[2][2] + meet[2][3]);
+    const int c = tid % kLanes, grp = tid / kLanes;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 *from = reinterpret_cast<const float4 *>(part_o + slot * D) + c;
+#pragma unroll 8
+    for (int p = grp; p < pieces; p += kGroups) {
+        const float f = weight[p];
+        const float4 y = f >= 0.f ? from[(int64_t)p * kLanes] : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float g = fmaxf(f, 0.f);
+        o.x += g * y.x; o.y += g * y.y; o.z += g * y.z; o.w += g * y.w;
+    }
+    sum_s[grp][c] = o;
+    __syncthreads();
+    if (grp != 0) return;
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < pieces; ++p) {
-        const float4 x = part_ml[slot + p];
-        if (x.y == 0.f) continue;
-        const float f = __builtin_amdgcn_exp2f(x.x - top);
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[c] += f * part_o[(slot + p) * D + lane * C + c];
+    for (int i = 1; i < kGroups; ++i) {
+        const float4 y = sum_s[i][c];
+        o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
     }
     const int64_t at = td.sel_lo[b] * n_q_heads + local;
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = l != 0.f ? o[c] / lr : 0.f;
-    if constexpr (DTYPE == KVS_BF16) {
-        if constexpr (C == 2) *reinterpret_cast<uint32_t *>((uint16_t *)out + at * D + lane * C) = pack2(o[0], o[1]);
-        else ((uint16_t *)out)[at * D + lane] = (uint16_t)f32_to_bf16_bits(o[0]);
-    } else {
-#pragma unroll
-        for (int c = 0; c < C; ++c) ((float *)out)[at * D + lane * C + c] = o[c];
-    }
-    if (lse_out && lane == 0) lse_out[at] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    const float inv = 1.f / lr;
+    if (l != 0.f) { o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv; }
+    else o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (DTYPE == KVS_BF16) *reinterpret_cast<uint2 *>((uint16_t *)out + at * D + 4 * c) = make_uint2(pack2(o.x, o.y), pack2(o.z, o.w));
+    else *reinterpret_cast<float4 *>((float *)out + at * D + 4 * c) = o;
+    if (lse_out && c == 0) lse_out[at] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
 inline size_t slot_bytes(int d) { return (size_t)d * sizeof(float) + sizeof(float4); }
@@ -608,8 +630,8 @@ extern "C" kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8
 #undef KVS_A8
         if (st != KVS_OK) return st;
         if (!plan.piece_tiles) continue;
-        const dim3 grid((unsigned)((items + kWaves - 1) / kWaves)), threads(kThreads);
-#define KVS_M8(DT, DD) hipLaunchKernelGGL((merge8_kernel<DT, DD>), grid, threads, 0, hs, td, shape->n_q_heads, items, po, ml, out, lse_out)
+        const dim3 grid((unsigned)items), threads(kThreads);
+#define KVS_M8(DT, DD) hipLaunchKernelGGL((merge8_kernel<DT, DD>), grid, threads, 0, hs, td, shape->n_q_heads, po, ml, out, lse_out)
         if (bf16) { if (wide) KVS_M8(KVS_BF16, 128); else KVS_M8(KVS_BF16, 64); }
         else { if (wide) KVS_M8(KVS_F32, 128); else KVS_M8(KVS_F32, 64); }
 #undef KVS_M8

@@ -58,7 +58,7 @@ def store(codes, scale, new, pos, block, code):
                     scale[blk, g] = np.nan
                     codes[taken, g] = 0
                     continue
-                need = max(np.float32(most / TOP[code]), np.float32(2.0 ** -126)) if most > 0 else np.float32(0)
+                need = max(most * (np.float32(1) / TOP[code]), np.float32(2.0 ** -126)) if most > 0 else np.float32(0)
                 now = max(need, old) if kept else need
                 inv = np.float32(1) / now if now > 0 else np.float32(0)
                 codes[taken, g] = nearest(x * inv, code)
