@@ -507,12 +507,15 @@ KVS_API kvs_status kvs_deviation_kv8(const kvs_shape *shape, const kvs_cache8 *c
  * q_sel, out [dev] [n_sel, n_q_heads, head_dim]      lse_out [dev] fp32[n_sel, n_q_heads] or NULL (natural log)
  * scale      any finite number
  * workspace  [dev] optional (NULL / 0 is valid), 256-byte aligned, kvs_workspace_size("attention_kv8", shape, batch, cache
- *            rows, n_sel) bytes: launches that would leave units idle cut their key ranges into pieces and merge them.
- *            Less of it means fewer pieces; results are the same up to fp32 summation order.  One call's until that call
- *            has ended on its stream.
+ *            rows, n_sel) bytes.  Launches that would leave units idle cut their key ranges into pieces and merge them.
+ *            Launches of so many rows that it pays (bf16, head_dim 128, scale > 0, contexts that begin at multiples of
+ *            16 rows) widen their contexts to bf16 in it, 4 bytes an element of K, and go on as kvs_partial_attention; the
+ *            size asked for has room for that from 7373 rows (tokens times query heads) on; what a key adds to an output
+ *            there is lost below 2^-65.  Less workspace means fewer pieces and no widening.  One call's until that call has ended on its stream.
  * Codes enter the matrix cores as the bf16 numbers that they are, exactly; K's scales multiply the scores in fp32.
- * bf16: softmax weights times V's scales enter the second product rounded to bf16.  fp32: Q and these products enter as
- * three bf16 numbers each, which together hold all their bits, and everything else is fp32.
+ * bf16: softmax weights enter the second product times V's scales and rounded to bf16, in widened contexts both factors are
+ * rounded.  fp32: Q and these products enter as three bf16 numbers each, which together hold all their bits, and
+ * everything else is fp32.
  */
 KVS_API kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8 *cache, int32_t batch,
                                      const int64_t *ctx_off, const int64_t *ctx_len, const int64_t *cu_sel,

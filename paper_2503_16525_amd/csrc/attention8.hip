@@ -531,6 +531,153 @@ Plan plan_pieces(const kvs_shape *shape, int32_t n_req, const int64_t *ctx_len, 
     }
 }
 
+// ---- many rows a key: a bf16 copy --------------------------------------------------------------------------------
+// With hundreds of rows a key and KV head the matrix cores bound the call, and right behind them the vector instructions, and
+// above every wave widens all keys that it multiplies with: 96 instructions beside the 16 matrix products of a tile.  Such
+// launches widen the contexts once, into the workspace, and go to the bf16 kernel of 256 rows (attention_mfma2.hip).  K
+// goes there as its codes, which bf16 holds exactly, with factors of the scores for every 16 rows; V as code * scale,
+// rounded to bf16 as a cache in bf16 would hold it.
+constexpr int kCopyThreads = 256;
+
+struct CopyRanges {
+    int64_t row[kAttnMaxReq];              // first row of request b, a multiple of 16
+    int32_t begin[kAttnMaxReq + 1];        // groups of 16 rows before it in the launch
+    int32_t n_req;
+};
+
+template <int CODE>
+__global__ __launch_bounds__(kCopyThreads) void copy8_kernel(const CopyRanges cr, int n_kv_heads, int64_t n_rows, int64_t first_row, int64_t end_row, int block_log2,
+                                                             const uint4 *__restrict__ k_codes, const uint4 *__restrict__ v_codes,
+                                                             const float *__restrict__ k_scale, const float *__restrict__ v_scale, float scale_log2,
+                                                             uint4 *__restrict__ k_out, uint4 *__restrict__ v_out, float *__restrict__ factors)
+{
+    constexpr int kChunks = 128 / 16;
+    const int b = request_of(cr.begin, cr.n_req, (int)blockIdx.x);
+    const int64_t row0 = cr.row[b] + ((int64_t)blockIdx.x - cr.begin[b]) * kAlign;      // the workgroup's 16 rows: one block of scales
+    const int64_t scales = (min(row0, n_rows - 1) >> block_log2) * n_kv_heads;
+    const int rows = (int)min((int64_t)kAlign, min(n_rows, end_row) - row0);            // (none where only the factors of a tile's second half are wanted)
+    for (int g = threadIdx.x; g < n_kv_heads; g += kCopyThreads) {
+        // (positive and finite, whatever the scale: a block that stands for zeros has codes of 0, a broken one NaN in K)
+        const float f = k_scale[scales + g] * scale_log2;
+        factors[((row0 - first_row) / kAlign) * n_kv_heads + g] = f >= 7.888609e-31f && f < INFINITY ? f : 7.888609e-31f;
+    }
+    const int per_row = n_kv_heads * kChunks;
+    for (int e = threadIdx.x; e < rows * per_row; e += kCopyThreads) {
+        const int c = e % per_row;
+        const int64_t from = row0 * per_row + e, to = ((row0 - first_row) * per_row + e) * 2;
+        const float ks = k_scale[scales + c / kChunks], vs = v_scale[scales + c / kChunks];
+        const uint4 k = stream_load16(k_codes + from), v = stream_load16(v_codes + from);
+        const bool broken = !(fabsf(ks) < INFINITY) || !(fabsf(vs) < INFINITY);
+        const uint32_t kw[4] = {k.x, k.y, k.z, k.w}, vw[4] = {v.x, v.y, v.z, v.w};
+        uint32_t ko[8], vo[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t kc = CODE == KVS_E4M3 ? numbers_only(kw[i]) : kw[i], vc = CODE == KVS_E4M3 ? numbers_only(vw[i]) : vw[i];
+            ko[2 * i] = broken ? 0x7fc07fc0u : ks > 0.f ? pair_of<CODE, false>(kc) : 0u;
+            ko[2 * i + 1] = broken ? 0x7fc07fc0u : ks > 0.f ? pair_of<CODE, true>(kc) : 0u;
+            float x[4];
+            widen_codes<CODE>(vc, x);
+            vo[2 * i] = broken ? 0u : pack2(x[0] * vs, x[1] * vs);
+            vo[2 * i + 1] = broken ? 0u : pack2(x[2] * vs, x[3] * vs);
+        }
+        k_out[to] = make_uint4(ko[0], ko[1], ko[2], ko[3]);
+        k_out[to + 1] = make_uint4(ko[4], ko[5], ko[6], ko[7]);
+        v_out[to] = make_uint4(vo[0], vo[1], vo[2], vo[3]);
+        v_out[to + 1] = make_uint4(vo[4], vo[5], vo[6], vo[7]);
+    }
+}
+
+// The bf16 kernel takes a negative position for 0: the rows of tokens that see nothing become 0 here.  A wave a token.
+__global__ __launch_bounds__(kThreads) void empty_rows_kernel(int64_t n_sel, int n_q_heads, const int32_t *__restrict__ sel_pos, uint4 *__restrict__ out,
+                                                              float *__restrict__ lse_out)
+{
+    const int64_t s = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (s >= n_sel || sel_pos[s] >= 0) return;
+    const int lane = threadIdx.x & 63;
+    for (int e = lane; e < n_q_heads * 16; e += 64) out[s * n_q_heads * 16 + e] = make_uint4(0u, 0u, 0u, 0u);
+    for (int h = lane; lse_out && h < n_q_heads; h += 64) lse_out[s * n_q_heads + h] = -INFINITY;
+}
+
+constexpr int64_t kCopyMinRows = 7373;     // selected rows over all query heads: 48 tiles of 256, 0.6 full, as the bf16 kernel asks for
+constexpr int64_t kCopyPad = 8;            // factors behind the last row's: what a step ahead asks for
+inline size_t copy_bytes(const kvs_shape *shape, int64_t rows)
+{
+    const int64_t groups = (rows + kAlign - 1) / kAlign;
+    return (size_t)(groups * kAlign * shape->n_kv_heads * 128 * 4 + (groups + kCopyPad) * shape->n_kv_heads * 4 + 512);
+}
+
+// Whether a copy for the bf16 kernel is worth its bytes.  Measured rates: the kernel above 0.6 PFLOP/s of what rows in the middle of
+// their contexts take, the bf16 kernel 1.0 (pieces and all), the copy 6 bytes an element of K and V at 4.5 TB/s and 10 us.
+bool bf16_copy_pays(const kvs_shape *shape, const kvs_cache8 *cache, int32_t n_req, const int64_t *ctx_off, const int64_t *ctx_len, const int64_t *cu_sel, float scale)
+{
+    if (shape->dtype != KVS_BF16 || shape->head_dim != 128 || !(scale > 0.f)) return false;
+    const int64_t rows = (cu_sel[n_req] - cu_sel[0]) * shape->n_q_heads;
+    if (rows < kCopyMinRows) return false;
+    double flops = 0, bytes = 0;
+    for (int32_t b = 0; b < n_req; ++b) {
+        const int64_t n = cu_sel[b + 1] - cu_sel[b];
+        if (n == 0) continue;
+        // (factors are for 16 rows of the cache: contexts have to begin with one; and the bf16 kernel expects a token's row to exist)
+        if (ctx_off[b] % kAlign || n > ctx_len[b]) return false;
+        flops += 256.0 * shape->n_q_heads * (double)n * (double)ctx_len[b];
+        bytes += 768.0 * shape->n_kv_heads * (double)ctx_len[b];
+    }
+    return flops * (1 / 0.6e15 - 1 / 1.0e15) > bytes / 4.5e12 + 10e-6;
+}
+
+// *taken: whether the launch was made (it is not where the workspace is too small for the copy, or the bf16 kernel would not take it)
+kvs_status launch_from_copy(const kvs_shape *shape, const kvs_cache8 *c, int32_t n_req, const int64_t *ctx_off, const int64_t *ctx_len, const int64_t *cu_sel,
+                            const void *q_sel, const int32_t *sel_pos, float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
+                            hipStream_t hs, bool *taken)
+{
+    CopyRanges cr = {};
+    AttnBatch bd = {};
+    int64_t lo = INT64_MAX, hi = 0, groups = 0;
+    for (int b = 0; b < n_req; ++b) {
+        if (cu_sel[b + 1] == cu_sel[b]) continue;
+        if (ctx_off[b] < lo) lo = ctx_off[b];
+        if (ctx_off[b] + ctx_len[b] > hi) hi = ctx_off[b] + ctx_len[b];
+    }
+    for (int b = 0; b < kAttnMaxReq; ++b) {
+        const bool live = b < n_req && cu_sel[b + 1] > cu_sel[b];
+        cr.begin[b] = (int32_t)groups;
+        cr.row[b] = live ? ctx_off[b] : 0;
+        bd.ctx_off[b] = live ? ctx_off[b] - lo : 0;
+        bd.ctx_len[b] = live ? ctx_len[b] : 0;
+        bd.cu_sel[b] = cu_sel[b < n_req ? b : n_req];
+        if (live) groups += (ctx_len[b] + 2 * kAlign - 1) / (2 * kAlign) * 2;       // whole tiles of 32 keys have factors
+        if (groups > 0x7fffff) return KVS_OK;
+    }
+    cr.begin[kAttnMaxReq] = (int32_t)groups;
+    bd.cu_sel[kAttnMaxReq] = cu_sel[n_req];
+    bd.sel_begin = cu_sel[0];
+    cr.n_req = bd.n_req = n_req;
+    const size_t need = copy_bytes(shape, hi - lo);
+    if (workspace_bytes < need + 256) return KVS_OK;
+    const size_t left = (workspace_bytes - need) / 256 * 256;        // the bf16 kernel's, in front of the copy
+    AttnSplitPlan plan;
+    if (!attention_takes_large(shape, bd, left, &plan)) return KVS_OK;
+    *taken = true;
+    const int64_t rows = (hi - lo + kAlign - 1) / kAlign * kAlign;
+    char *at = (char *)workspace + left;
+    uint4 *k_copy = (uint4 *)at, *v_copy = (uint4 *)(at + rows * shape->n_kv_heads * 256);
+    float *factors = (float *)(at + rows * shape->n_kv_heads * 512);
+    const float scale_log2 = scale * 1.4426950408889634f;
+    const dim3 grid((unsigned)groups), threads(kCopyThreads);
+#define KVS_COPY(C) hipLaunchKernelGGL((copy8_kernel<C>), grid, threads, 0, hs, cr, shape->n_kv_heads, c->n_rows, lo, lo + rows, __builtin_ctz((unsigned)c->block), \
+                                       (const uint4 *)c->k, (const uint4 *)c->v, c->k_scale, c->v_scale, scale_log2, k_copy, v_copy, factors)
+    if (c->code == KVS_E4M3) KVS_COPY(KVS_E4M3); else KVS_COPY(KVS_INT8);
+#undef KVS_COPY
+    kvs_status st = check_launch("kvs_attention_kv8(copy)");
+    if (st != KVS_OK) return st;
+    st = launch_attention_mfma2(shape, bd, q_sel, sel_pos, k_copy, v_copy, scale, out, lse_out, left ? workspace : nullptr, left, plan, hs, factors);
+    if (st != KVS_OK) return st;
+    const int64_t n_sel = cu_sel[n_req] - cu_sel[0];
+    hipLaunchKernelGGL(empty_rows_kernel, dim3((unsigned)((n_sel + kWaves - 1) / kWaves)), dim3(kThreads), 0, hs, n_sel, shape->n_q_heads, sel_pos + cu_sel[0],
+                       (uint4 *)out + cu_sel[0] * shape->n_q_heads * 16, lse_out ? lse_out + cu_sel[0] * shape->n_q_heads : nullptr);
+    return check_launch("kvs_attention_kv8(rows)");
+}
+
 template <int DTYPE, int CODE, int D>
 kvs_status launch(const kvs_shape *shape, const kvs_cache8 *c, const Table &td, int64_t wgs, const void *q_sel, const int32_t *sel_pos, float scale,
                   void *out, float *lse_out, float *part_o, float4 *part_ml, hipStream_t hs)
@@ -559,7 +706,12 @@ size_t attention8_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t
     const int64_t most = (int64_t)kRows * (kSplitBelow + kTargetWgs);
     int64_t slots = most;
     if (n_sel_total < most && n_sel_total * shape->n_q_heads < most) slots = n_sel_total * shape->n_q_heads * pieces < most ? n_sel_total * shape->n_q_heads * pieces : most;
-    return ((size_t)slots * slot_bytes(shape->head_dim) + 255) / 256 * 256;
+    size_t bytes = ((size_t)slots * slot_bytes(shape->head_dim) + 255) / 256 * 256;
+    if (shape->dtype == KVS_BF16 && shape->head_dim == 128 && n_sel_total >= kCopyMinRows / shape->n_q_heads) {
+        const size_t copy = (copy_bytes(shape, n_rows_total) + attention_workspace_bytes(shape, batch, n_rows_total, n_sel_total) + 511) / 256 * 256;
+        if (copy > bytes) bytes = copy;
+    }
+    return bytes;
 }
 
 } // namespace kvs
@@ -597,6 +749,12 @@ extern "C" kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8
         const int64_t n_sel = cu_sel[b0 + nr] - cu_sel[b0];
         if (n_sel == 0) continue;
         if (n_sel > 0x7fffff00LL / shape->n_q_heads) return fail(KVS_EINVAL, "%s: %lld selected tokens in one launch", me, (long long)n_sel);
+        if (bf16_copy_pays(shape, cache, nr, ctx_off + b0, ctx_len + b0, cu_sel + b0, scale)) {
+            bool taken = false;
+            st = launch_from_copy(shape, cache, nr, ctx_off + b0, ctx_len + b0, cu_sel + b0, q_sel, sel_pos, scale, out, lse_out, workspace, workspace_bytes, hs, &taken);
+            if (st != KVS_OK) return st;
+            if (taken) continue;
+        }
         const Plan plan = plan_pieces(shape, nr, ctx_len + b0, cu_sel + b0, workspace_bytes);
         Table td = {};
         td.n_req = nr;

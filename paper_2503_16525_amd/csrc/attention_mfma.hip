@@ -531,13 +531,8 @@ bool attention_mfma_supports(const kvs_shape *shape)
     return shape->dtype == KVS_BF16 && shape->head_dim == D;
 }
 
-kvs_status launch_attention_mfma(const kvs_shape *shape, const AttnBatch &bd, int64_t n_sel,
-                                 const void *q_sel, const int32_t *sel_pos, const void *k_cache,
-                                 const void *v_cache, float scale, void *out, float *lse_out,
-                                 void *workspace, size_t workspace_bytes, hipStream_t st)
+bool attention_takes_large(const kvs_shape *shape, const AttnBatch &bd, size_t workspace_bytes, AttnSplitPlan *plan)
 {
-    if (!attention_mfma_supports(shape)) return fail(KVS_EUNSUPPORTED, "kvs_partial_attention: matrix-core path needs bf16, head_dim 128");
-    if (!(scale > 0.f) || !isfinite(scale)) return fail(KVS_EUNSUPPORTED, "kvs_partial_attention: matrix-core path needs a positive finite scale");
     // enough 256-row tiles to give every CU work: the 64-rows-per-wave kernel; otherwise the
     // finer-grained one, which fills the chip better.  A build with -DKVS_ATTN_FORCE=1 (small) or 2
     // (large) pins the choice: the test suite builds such a library beside the shipped one to reach
@@ -558,7 +553,7 @@ kvs_status launch_attention_mfma(const kvs_shape *shape, const AttnBatch &bd, in
     // with fewer 256-row tiles than compute units the large kernel still wins if the caller's
     // workspace lets it cut the key ranges and its tiles are not mostly padding
     AttnSplitPlan plan2 = {1, 0, false};
-    if (fits32) plan2 = attention_mfma2_plan(shape, bd, workspace ? workspace_bytes : 0);
+    if (fits32) plan2 = attention_mfma2_plan(shape, bd, workspace_bytes);
     const int splits2 = plan2.n_splits;
     const bool dense_tiles = rows * 10 >= big_tiles * 256 * 6;
     const bool fills = big_tiles * shape->n_kv_heads >= kAttnBigTileMinGrid;
@@ -569,10 +564,21 @@ kvs_status launch_attention_mfma(const kvs_shape *shape, const AttnBatch &bd, in
     const bool whole = bd.n_req > 1 || big_tiles * shape->n_kv_heads >= kAttnWholeFrom || !dense_tiles || splits2 < 2;
     // (below ~50 such tiles the per-workgroup start-up of the large kernel costs more than it gains)
     const bool big = fits32 && (forced ? forced == 2 : fills || (splits2 >= 2 && dense_tiles && big_tiles * shape->n_kv_heads >= 48));
-    if (big) {
-        if (fills && whole && !forced) plan2 = {1, 0, plan2.recentre};
-        return launch_attention_mfma2(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan2, st);
-    }
+    if (big && fills && whole && !forced) plan2 = {1, 0, plan2.recentre};
+    *plan = plan2;
+    return big;
+}
+
+kvs_status launch_attention_mfma(const kvs_shape *shape, const AttnBatch &bd, int64_t n_sel,
+                                 const void *q_sel, const int32_t *sel_pos, const void *k_cache,
+                                 const void *v_cache, float scale, void *out, float *lse_out,
+                                 void *workspace, size_t workspace_bytes, hipStream_t st)
+{
+    if (!attention_mfma_supports(shape)) return fail(KVS_EUNSUPPORTED, "kvs_partial_attention: matrix-core path needs bf16, head_dim 128");
+    if (!(scale > 0.f) || !isfinite(scale)) return fail(KVS_EUNSUPPORTED, "kvs_partial_attention: matrix-core path needs a positive finite scale");
+    AttnSplitPlan plan;
+    if (attention_takes_large(shape, bd, workspace ? workspace_bytes : 0, &plan))
+        return launch_attention_mfma2(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, st);
     return launch_mfma_variant<KVS_ATTN_NWAVES>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out,
                                                 workspace, workspace_bytes, st);
 }

@@ -241,14 +241,16 @@ __device__ __forceinline__ void plan_shares(const AttnTiles &td, int grp, int to
 // together read the same stretch of K and V, which then stays in L2.
 // RECENTRE: the softmax reference is not fixed for the sweep; see recentre below, and AttnSplitPlan for when.
 // QUEUE: the workgroup draws its tiles; see attn_queue_kernel.
-template <bool WANT_LSE, bool SPLIT, bool RECENTRE, bool QUEUE>
+// SCALED: K holds codes, whose scores are multiplied by a factor for each 16 keys and KV head (key_scale, all positive and finite; the
+// contexts begin at multiples of 16 rows); scale_log2 is not read.  Two scalar loads a step, a step ahead.
+template <bool WANT_LSE, bool SPLIT, bool RECENTRE, bool QUEUE, bool SCALED>
 __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     const AttnTiles td, int n_q_heads, int n_kv_heads, int total_tiles,
     const uint16_t *__restrict__ q_sel, const int32_t *__restrict__ sel_pos,
     const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache,
     float scale_log2, uint16_t *__restrict__ out, float *__restrict__ lse_out,
     int n_splits, const int4 *__restrict__ split_plan, const uint16_t *__restrict__ piece_list,
-    float *__restrict__ part_o, float4 *__restrict__ part_ml, int share_units, int32_t *__restrict__ queue)
+    float *__restrict__ part_o, float4 *__restrict__ part_ml, int share_units, int32_t *__restrict__ queue, const float *__restrict__ key_scale)
 {
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];   // K ring, then V^T ring
     __shared__ int wg_max_pos[NWAVES];
@@ -510,12 +512,33 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
                 }
         }
     };
+    // What a score of tile jt is multiplied with: one number, or one for each half of the tile's keys.
+    struct Factors { float half[SCALED ? 2 : 1]; };
+    typedef const __attribute__((address_space(4))) float *scalar_f32;
+    const scalar_f32 factor_at = (scalar_f32)(uintptr_t)(SCALED ? key_scale + (ctx_off >> 4) * n_kv_heads + g : nullptr);
+    auto factors = [&](int jt) -> Factors {
+        Factors f;
+        if constexpr (SCALED) {
+            f.half[0] = factor_at[2 * jt * n_kv_heads];
+            f.half[1] = factor_at[(2 * jt + 1) * n_kv_heads];
+        } else {
+            f.half[0] = scale_log2;
+        }
+        return f;
+    };
     // max over the tile's keys of scale*log2(e)*logit, per query (combines the two half-waves)
-    auto row_max = [&](const floatx16 &s) -> float {
+    auto row_max = [&](const floatx16 &s, const Factors &f) -> float {
+        if constexpr (SCALED) {
+            float mx = s[0] * f.half[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r] * f.half[r >> 3]);
+            return fmaxf(mx, __shfl_xor(mx, 32));
+        } else {
         float mx = s[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
         return fmaxf(mx, __shfl_xor(mx, 32)) * scale_log2;
+        }
     };
 
     floatx16 o_acc[D / 32][NB];
@@ -526,11 +549,12 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     // contribution to the running sums.  P = exp2(scale*log2e*S - m_ref); the reference is fixed for
     // the whole pass, so the output accumulators are touched by MFMAs only and can stay in the
     // accumulation registers; see the comment at the pass loop for why that is safe.
-    auto softmax4 = [&](const floatx16 &s, int nb, int r0, u32x4_t (&pop)[2]) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 0], scale_log2, -m_ref[nb]));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 1], scale_log2, -m_ref[nb]));
-        const float e2 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 2], scale_log2, -m_ref[nb]));
-        const float e3 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 3], scale_log2, -m_ref[nb]));
+    auto softmax4 = [&](const floatx16 &s, const Factors &f, int nb, int r0, u32x4_t (&pop)[2]) {
+        const float by = f.half[SCALED ? r0 >> 3 : 0];
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 0], by, -m_ref[nb]));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 1], by, -m_ref[nb]));
+        const float e2 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 2], by, -m_ref[nb]));
+        const float e3 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 3], by, -m_ref[nb]));
         const uint32_t w0 = pack2(e0, e1), w1 = pack2(e2, e3);
         pop[r0 >> 3][(r0 & 7) >> 1] = w0;
         pop[r0 >> 3][((r0 & 7) >> 1) + 1] = w1;
@@ -539,10 +563,11 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     };
     auto softmax = [&](int jt, floatx16 (&s)[NB], u32x4_t (&pop)[NB][2]) {
         mask_tile(jt, s);
+        const Factors f = factors(jt);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int r0 = 0; r0 < 16; r0 += 4) softmax4(s[nb], nb, r0, pop[nb]);
+            for (int r0 = 0; r0 < 16; r0 += 4) softmax4(s[nb], f, nb, r0, pop[nb]);
     };
     auto pv_product = [&](int jt, const u32x4_t (&pop)[NB][2]) {
         const uint32_t vs = v_slot(jt);
@@ -580,13 +605,14 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
         }
     };
     auto recentre = [&](int jt, floatx16 (&s)[NB], u32x4_t (&pop)[NB][2]) __attribute__((always_inline)) {
+        const Factors f = factors(jt);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             floatx16 &m = s[nb];          // (the scores are not read again)
 #pragma unroll
             for (int r = 0; r < 16; ++r) m[r] = jt * BN + 16 * (r >> 3) + 8 * hf + (r & 7) > pos[nb] ? -INFINITY : m[r];
             const float other = __shfl_xor(l_run[nb], 32);
-            const float up = !(l_run[nb] >= kSumLimit || other >= kSumLimit) ? 0.f : fmaxf(ceilf(row_max(m) + kRefShift - m_ref[nb]), 100.f);
+            const float up = !(l_run[nb] >= kSumLimit || other >= kSumLimit) ? 0.f : fmaxf(ceilf(row_max(m, f) + kRefShift - m_ref[nb]), 100.f);
             const float down = __builtin_amdgcn_exp2f(-up);
             m_ref[nb] += up;
             l_run[nb] = l_before[nb] * down;
@@ -598,7 +624,7 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o_acc[db][nb][r] *= down;
 #pragma unroll
-            for (int r0 = 0; r0 < 16; r0 += 4) softmax4(m, nb, r0, pop[nb]);
+            for (int r0 = 0; r0 < 16; r0 += 4) softmax4(m, f, nb, r0, pop[nb]);
         }
     };
 
@@ -612,12 +638,15 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     int key_lim[NB];   // a key of the tile is visible to the lane's query nb iff its (half-wave-relative) index <= this
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) key_lim[nb] = pos[nb] - 8 * hf;
+    Factors f_next = {};   // SCALED: of the next step's tile
     auto fast_step = [&](auto masked, auto live, int jt, floatx16 (&s_in)[NB], floatx16 (&s_out)[NB],
                          const u32x4_t (&p_in)[NB][2], u32x4_t (&p_out)[NB][2],
                          u32x4_t &ka, u32x4_t &va) __attribute__((always_inline)) {
         constexpr int MASKED = decltype(masked)::value, FIRST = decltype(live)::value;   // block nb: bit nb; blocks FIRST .. NB-1 are worked on
         constexpr int PER = FIRST == 0 ? 4 : 2;                                          // scores per slice
         keep_sums();
+        const Factors f = SCALED ? f_next : factors(jt);
+        if (SCALED) f_next = factors(jt + 1);
         const uint32_t ks = k_slot(jt + 1), vs = v_slot(jt - 1), ks_next = k_slot(jt + 2), vs_next = v_slot(jt);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -637,7 +666,7 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
             if (FIRST == 0) s_out[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ka), qreg[0][i], i == 0 ? zero : s_out[0], 0, 0, 0);
             float x[PER], e[PER];
 #pragma unroll
-            for (int u = 0; u < PER; ++u) x[u] = fmaf(s_in[nbs][r0 + u], scale_log2, -m_ref[nbs]);
+            for (int u = 0; u < PER; ++u) x[u] = fmaf(s_in[nbs][r0 + u], f.half[SCALED ? r0 >> 3 : 0], -m_ref[nbs]);
             if (MASKED >> nbs & 1) {   // entry r of the lane is key jt*BN + 16*(r>>3) + 8*hf + (r&7)
                 const int k0 = jt * BN + 16 * (r0 >> 3) + (r0 & 7);
 #pragma unroll
@@ -699,8 +728,9 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
                 floatx16 s[NB];
                 qk(jt, s);
                 mask_tile(jt, s);
+                const Factors f = factors(jt);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) m_ref[nb] = fmaxf(m_ref[nb], row_max(s[nb]));
+                for (int nb = 0; nb < NB; ++nb) m_ref[nb] = fmaxf(m_ref[nb], row_max(s[nb], f));
             }
             // a row whose keys in this piece all score -inf: as in pass 0
 #pragma unroll
@@ -720,10 +750,11 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
         qk(t_lo, s_cur);
         if (pass == 0) {
             mask_tile(t_lo, s_cur);
+            const Factors f = factors(t_lo);
             // a row whose keys all lie before this piece sees nothing here: a finite reference keeps
             // its weights at exp2(-inf) = 0 instead of NaN (the merge drops pieces with zero sum)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) m_ref[nb] = fmaxf(row_max(s_cur[nb]), -1.0e30f) + kRefShift;
+            for (int nb = 0; nb < NB; ++nb) m_ref[nb] = fmaxf(row_max(s_cur[nb], f), -1.0e30f) + kRefShift;
             if (RECENTRE && fmaxf(fabsf(m_ref[0]), fabsf(m_ref[1])) > kFarRef) redo_flag = 1;
         }
 #pragma unroll
@@ -758,6 +789,7 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
             u32x4_t ka = read_k(k_slot(t_lo + 2), 0);
             u32x4_t va = read_vt(v_slot(t_lo), 0, 0);
             jt = t_lo + 1;
+            if (SCALED) f_next = factors(jt);
             // two steps per trip so that the score and weight buffers swap roles without copies
             auto sweep = [&](auto masked, auto live, int stop) __attribute__((always_inline)) {
                 for (; jt < stop && jt + 1 < t_hi && jt + AHEAD + 1 < j_inside; jt += 2) {
@@ -1088,23 +1120,23 @@ __global__ __launch_bounds__(ORDER_NT) void attn_order_kernel(const AttnTiles td
     order[before] = (uint16_t)tid;
 }
 
-template <bool WANT_LSE, bool SPLIT, bool RECENTRE, bool QUEUE>
+template <bool WANT_LSE, bool SPLIT, bool RECENTRE, bool QUEUE, bool SCALED>
 kvs_status launch_one(const dim3 grid, size_t lds_bytes, hipStream_t st, const AttnTiles &td, const kvs_shape *shape,
                       int tiles, const void *q_sel, const int32_t *sel_pos, const void *k_cache, const void *v_cache,
                       float scale_log2, void *out, float *lse_out, int n_splits, const int4 *split_plan,
-                      const uint16_t *piece_list, float *part_o, float4 *part_ml, int share_units, int32_t *queue)
+                      const uint16_t *piece_list, float *part_o, float4 *part_ml, int share_units, int32_t *queue, const float *key_scale)
 {
     static DeviceOnce attr_once;
     const kvs_status ast = once_per_device(attr_once, [lds_bytes] {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_mfma2_kernel<WANT_LSE, SPLIT, RECENTRE, QUEUE>),
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_mfma2_kernel<WANT_LSE, SPLIT, RECENTRE, QUEUE, SCALED>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes);
         return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_partial_attention: hipFuncSetAttribute: %s", hipGetErrorString(e));
     });
     if (ast != KVS_OK) return ast;
-    hipLaunchKernelGGL((attn_mfma2_kernel<WANT_LSE, SPLIT, RECENTRE, QUEUE>), grid, dim3(NT), lds_bytes, st, td, shape->n_q_heads,
+    hipLaunchKernelGGL((attn_mfma2_kernel<WANT_LSE, SPLIT, RECENTRE, QUEUE, SCALED>), grid, dim3(NT), lds_bytes, st, td, shape->n_q_heads,
                        shape->n_kv_heads, tiles, (const uint16_t *)q_sel, sel_pos, (const uint16_t *)k_cache,
                        (const uint16_t *)v_cache, scale_log2, (uint16_t *)out, lse_out, n_splits, split_plan, piece_list,
-                       part_o, part_ml, share_units, queue);
+                       part_o, part_ml, share_units, queue, key_scale);
     return check_launch("kvs_partial_attention(mfma2)");
 }
 
@@ -1158,10 +1190,13 @@ AttnSplitPlan attention_mfma2_plan(const kvs_shape *shape, const AttnBatch &bd, 
     return AttnSplitPlan{(int)s_max, (int)max_ctx, false};
 }
 
-kvs_status launch_attention_mfma2(const kvs_shape *shape, const AttnBatch &bd, const void *q_sel,
-                                  const int32_t *sel_pos, const void *k_cache, const void *v_cache,
-                                  float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
-                                  const AttnSplitPlan &plan, hipStream_t st)
+namespace {
+
+template <bool SCALED>
+kvs_status launch_large(const kvs_shape *shape, const AttnBatch &bd, const void *q_sel,
+                        const int32_t *sel_pos, const void *k_cache, const void *v_cache,
+                        float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
+                        const AttnSplitPlan &plan, const float *key_scale, hipStream_t st)
 {
     AttnTiles td;
     const int64_t tiles = build_attn_tiles(shape, bd, ROWS, td);
@@ -1201,8 +1236,8 @@ kvs_status launch_attention_mfma2(const kvs_shape *shape, const AttnBatch &bd, c
             if (stt != KVS_OK) return stt;
         }
         const dim3 grid((unsigned)((share_units > 0 || queue ? units : tiles) * shape->n_kv_heads));
-#define KVS_ATTN_WHOLE(LSE, RC, Q) launch_one<LSE, false, RC, Q>(grid, lds_bytes, st, td, shape, (int)tiles, q_sel, sel_pos, k_cache, v_cache, \
-                                                          scale_log2, out, lse_out, 1, nullptr, order, nullptr, nullptr, share_units, queue)
+#define KVS_ATTN_WHOLE(LSE, RC, Q) launch_one<LSE, false, RC, Q, SCALED>(grid, lds_bytes, st, td, shape, (int)tiles, q_sel, sel_pos, k_cache, v_cache, \
+                                                          scale_log2, out, lse_out, 1, nullptr, order, nullptr, nullptr, share_units, queue, key_scale)
         if (queue) {
             if (lse_out) return plan.recentre ? KVS_ATTN_WHOLE(true, true, true) : KVS_ATTN_WHOLE(true, false, true);
             return plan.recentre ? KVS_ATTN_WHOLE(false, true, true) : KVS_ATTN_WHOLE(false, false, true);
@@ -1228,15 +1263,25 @@ kvs_status launch_attention_mfma2(const kvs_shape *shape, const AttnBatch &bd, c
     kvs_status stt = check_launch("kvs_partial_attention(plan)");
     if (stt != KVS_OK) return stt;
     const dim3 grid((unsigned)(tiles * shape->n_kv_heads * n_splits));
-    stt = lse_out ? launch_one<true, true, false, false>(grid, lds_bytes, st, td, shape, (int)tiles, q_sel, sel_pos, k_cache, v_cache,
-                                           scale_log2, out, lse_out, n_splits, split_plan, piece_list, part_o, part_ml, 0, nullptr)
-                  : launch_one<false, true, false, false>(grid, lds_bytes, st, td, shape, (int)tiles, q_sel, sel_pos, k_cache, v_cache,
-                                            scale_log2, out, lse_out, n_splits, split_plan, piece_list, part_o, part_ml, 0, nullptr);
+    stt = lse_out ? launch_one<true, true, false, false, SCALED>(grid, lds_bytes, st, td, shape, (int)tiles, q_sel, sel_pos, k_cache, v_cache,
+                                           scale_log2, out, lse_out, n_splits, split_plan, piece_list, part_o, part_ml, 0, nullptr, key_scale)
+                  : launch_one<false, true, false, false, SCALED>(grid, lds_bytes, st, td, shape, (int)tiles, q_sel, sel_pos, k_cache, v_cache,
+                                            scale_log2, out, lse_out, n_splits, split_plan, piece_list, part_o, part_ml, 0, nullptr, key_scale);
     if (stt != KVS_OK) return stt;
     return launch_attention_merge(n_rows_total, n_splits, (const float *)workspace, ml_base,
                                   (uint16_t *)out + row0 * D, lse_out ? lse_out + row0 : nullptr, st,
                                   AttnMergePlan{split_plan, sel_pos + bd.cu_sel[0], shape->n_q_heads, plan.max_ctx});
 }
 
-} // namespace kvs
+} // namespace
 
+kvs_status launch_attention_mfma2(const kvs_shape *shape, const AttnBatch &bd, const void *q_sel,
+                                  const int32_t *sel_pos, const void *k_cache, const void *v_cache,
+                                  float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
+                                  const AttnSplitPlan &plan, hipStream_t st, const float *key_scale)
+{
+    return key_scale ? launch_large<true>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, key_scale, st)
+                     : launch_large<false>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, nullptr, st);
+}
+
+} // namespace kvs

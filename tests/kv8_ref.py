@@ -78,7 +78,8 @@ def held(codes, scale, block, code):
 
 
 def attention(q, pos, k, v, scale):
-    """q [n, hq, d], pos [n] (negative: sees nothing), k, v [len, hk, d] in 64 bits -> out, lse, sum of |weight * v|, largest sum of |q k|"""
+    """q [n, hq, d], pos [n] (negative: sees nothing), k, v [len, hk, d] in 64 bits
+    -> out, lse, sum of |weight * v|, largest sum of |q k|, largest |v| of each query head"""
     n, hq, d = q.shape
     ln, hk, _ = k.shape
     grp = hq // hk
@@ -98,20 +99,36 @@ def attention(q, pos, k, v, scale):
             out[i, g * grp:(g + 1) * grp] = w @ v[: p + 1, g] / t
             mag[i, g * grp:(g + 1) * grp] = w @ np.abs(v[: p + 1, g]) / t
             lse[i, g * grp:(g + 1) * grp] = (m + np.log(t))[:, 0]
-    return out, lse, mag, dots
+    return out, lse, mag, dots, largest(v, hq)
 
 
-def check_attention(out, lse, ref, dtype, longest, what):
+def largest(v, hq):
+    return np.abs(v).max((0, 2), initial=0.0).repeat(hq // v.shape[1])
+
+
+def joined(parts):
+    """The results of several requests' attention as one's."""
+    return [np.concatenate([p[i] for p in parts]) for i in range(3)] + [max(p[3] for p in parts), np.max([p[4] for p in parts], 0)]
+
+
+def check_attention(out, lse, ref, dtype, longest, what, widened=False):
     """bf16: a weight's rounding, 2^-8 of it, moves the output by at most that share of sum |weight| |v - out| <= 2 mag; the store
     rounds once more.  fp32 everywhere: a score's error is at most (d + 4) roundings of its sum of |q k| (`dots`), its weight's
-    that plus a few units; a sum over n keys is off by at most n roundings of its magnitude, numerator and denominator."""
-    want, want_lse, mag, dots = ref
+    that plus a few units; a sum over n keys is off by at most n roundings of its magnitude, numerator and denominator.
+    Weights of nothing: the row's largest enters the second product as at least 2^-31 of V's scale (the exponents' reference lies at
+    most 31 above the first tile's maximum), bf16 ends at 2^-126, so with scales from 2^-14 up a weight below 2^-126+31+14 of
+    the largest may become 0; n of them move the output by less than n 2^-80 max |v|.
+    widened: V is rounded to bf16 too, 2^-8 of each |v|, and the exponents' reference lies at most 61 above the first tile's maximum:
+    2^-126+61 of the largest; and a product of a weight and a V below 2^-126 may become 0, which against a sum of weights of at least
+    2^-61 is 2^-65 of the output for each key."""
+    want, want_lse, mag, dots, most = ref
     out, lse = out.astype(np.float64), lse.astype(np.float64)
     assert np.isfinite(out).all(), f"{what}: not finite"
     weight = (132 * dots + 64) * 2.0 ** -24
     tol = mag * 2 * (weight + longest * 2.0 ** -24) + 1e-30
     if dtype == "bf16":
-        tol = tol + 2.0 ** -8 * (2 * mag + np.abs(want))
+        tol = tol + 2.0 ** -8 * ((3 if widened else 2) * mag + np.abs(want)) + longest * 2.0 ** (-64 if widened else -80) * most[None, :, None]
+        tol = tol + (longest * 2.0 ** -65 if widened else 0.0)
     else:
         tol = tol + 2.0 ** -23 * np.abs(want)
     over = np.abs(out - want) - tol

@@ -38,7 +38,7 @@ def _case(hq, hk, d, dtype, code, block, reqs, scale=1.0, seed=0, slack=0, what=
     sh = B.make_shape(hq, hk, d, B.BF16 if dtype == "bf16" else B.F32)
     kh, vh = R.held(cache[0], cache[1], block, code), R.held(cache[2], cache[3], block, code)
     parts = [R.attention(q[cu[b]:cu[b + 1]].double().numpy(), pos[cu[b]:cu[b + 1]], kh[off[b]:off[b] + ln[b]], vh[off[b]:off[b] + ln[b]], scale) for b in range(len(ln))]
-    ref = [np.concatenate([p[i] for p in parts]) for i in range(3)] + [max(p[3] for p in parts)]
+    ref = R.joined(parts)
     for want_ws in (True, False):
         name = f"{what} {hq}x{hk}x{d} {dtype} {code}/{block}, {len(ln)} requests of {min(ln)} to {max(ln)}, {len(pos)} tokens, workspace {want_ws}"
         print(name, flush=True)

@@ -139,7 +139,11 @@ def test_the_workspace_never_shrinks_with_the_totals():
     for sh in (_shape(), _shape(hq=28, hk=4), _shape(hq=4, hk=4, d=64, dt=B.F32)):
         for n_sel in (1, 64, 5000):
             sizes = [B.kvs_workspace_size("attention_kv8", sh, 1, n, n_sel) for n in (0, 1, 31, 32, 1000, 4096, 131072, 1 << 21)]
-            assert sizes == sorted(sizes) and sizes[-1] <= 2048 * 32 * (4 * sh.head_dim + 16)
+            assert sizes == sorted(sizes)
+            if n_sel == 1 or sh.dtype == B.F32:            # pieces only; from 7373 rows on there is room for a bf16 copy
+                assert sizes[-1] <= 2048 * 32 * (4 * sh.head_dim + 16)
+            elif n_sel == 5000:
+                assert sizes[-1] >= 512 * sh.n_kv_heads << 21
         for n in (1, 4096, 131072):
             sizes = [B.kvs_workspace_size("attention_kv8", sh, 1, n, n_sel) for n_sel in (0, 1, 2, 63, 64, 5000, 1 << 20, 1 << 40)]
             assert sizes == sorted(sizes)
