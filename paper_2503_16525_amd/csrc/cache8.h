@@ -38,19 +38,19 @@ __device__ __forceinline__ void widen_codes(uint32_t w, float (&x)[4])
     }
 }
 
-// the nearest codes (ties to even) to four numbers
+// The nearest codes (ties to even) to four numbers times `by`, products that pass the largest code by their rounding at most.
 template <int CODE>
-__device__ __forceinline__ uint32_t nearest_codes(float a, float b, float c, float d)
+__device__ __forceinline__ uint32_t nearest_codes(float a, float b, float c, float d, float by)
 {
-    constexpr float top = top_code<CODE>();
-    // (x * (1 / scale) can pass the largest code by its rounding)
-    auto held = [](float x) { return __builtin_amdgcn_fmed3f(x, -top, top); };
+#pragma clang fp contract(off)
     if constexpr (CODE == KVS_E4M3) {
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(held(a), held(b), 0, false);
-        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(held(c), held(d), w, true);
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * by, b * by, 0, false);          // (up to 464 the nearest is 448)
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * by, d * by, w, true);
     } else {
-        auto code = [&](float x) { return (uint32_t)(int)__builtin_rintf(held(x)) & 0xffu; };
-        return code(a) | (code(b) << 8) | (code(c) << 16) | (code(d) << 24);
+        // 1.5 * 2^23 + x, rounded, ends with the whole number nearest to x in two's complement
+        const float m = 12582912.f;
+        const uint32_t x = __float_as_uint(a * by + m), y = __float_as_uint(b * by + m), z = __float_as_uint(c * by + m), w = __float_as_uint(d * by + m);
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w, z, 0x0c0c0400u), __builtin_amdgcn_perm(y, x, 0x0c0c0400u), 0x05040100u);
     }
 }
 

@@ -4,12 +4,17 @@
 // that maximum and once to be divided by it.  They stay in registers in between, so memory sees them once: 2 or 4 bytes
 // an element in, 1 byte out, plus the kept rows' codes where a block's scale grows.
 //
-// The work is a list of tasks: a run (the entries of one block) and a unit (one KV head of K or of V).  A wave holds up to
-// 32 rows of a task, so a task takes a team of 1, 2 or 4 waves (`waves`); larger teams meet in LDS for their maximum.  Without a
-// list a workgroup has one block and its share of the units; with one it has a chunk of the list, whose runs it finds from
-// one load of the positions, and one unit or more.  Which entry a row takes is settled in LDS: the highest that names it,
-// whatever order the entries of a block come in.  (A workgroup for each entry, of which those that do not begin a run end
-// at once, took 35.6 us for 4424 of 32768 rows of 8 heads; this takes STORE_US.)
+// Rows in a row (no list): a workgroup has one block and its share of the units, a unit being one KV head of K or of V.  A wave
+// holds up to 32 rows of a unit, so a unit takes a team of 1, 2 or 4 waves (`waves`), which meet in LDS for their maximum.
+//
+// A list: its entries of one block are a run.  A wave has a few entries of the list, finds the runs that begin there from one
+// load of the positions, and takes 64 pieces of the rows of each, 4 heads of 256 bytes; no wave waits for another.  Which entry a
+// row takes is settled in LDS: the highest that names it, whatever order the entries of a block come in.  A lane has the same
+// piece of up to 8 rows: its maximum runs over the rows first, then over the lanes of its head (no exchange beyond 16 lanes), and the
+// scale is made in every lane that needs it.  What a wave waits for is one trip to memory for the positions, one for the rows
+// and old scales, and where a scale grows one for the codes that it rounds again.  (4424 of 32768 rows of 8 heads: a
+// workgroup for each entry 35.6 us, a chunk of the list and one unit a workgroup 25.8, a wave a run with whole heads one after the
+// other 20, issue bound; this 13.6; one row in each of 64 blocks 3.7.)
 #include "cache8.h"
 
 #include <math.h>
@@ -19,8 +24,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaveRows = 32;
-constexpr int64_t kManyWgs = 4096;
-constexpr int kMaxChunk = 32;          // entries of a chunk: runs that go on behind it are followed
+constexpr int kMaxBlock = 128;
+constexpr int kListRows = 8;           // rows of a run that a lane holds
+constexpr int kMaxChunk = 32;          // entries in which a wave looks for runs; runs that go on behind them are followed
+constexpr int64_t kManyWaves = 16384;  // waves from which they get more entries each
 
 struct StoreArgs {
     const void *k_new, *v_new;
@@ -33,15 +40,105 @@ struct StoreArgs {
     int32_t n_kv_heads, block_log2, waves, units_per_wg, chunk;
 };
 
-__device__ __forceinline__ uint32_t wave_max_bits(uint32_t v)
+// largest of a number's magnitude as bits: magnitudes order as whole numbers, NaN above infinity above the rest
+template <int DTYPE>
+__device__ __forceinline__ uint32_t magnitude_bits(const uint4 w)
 {
+    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+    uint32_t bits = 0;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (DTYPE == KVS_BF16) bits = max(bits, max((ww[j] << 16) & 0x7fffffffu, ww[j] & 0x7fff0000u));
+        else bits = max(bits, ww[j] & 0x7fffffffu);
+    }
+    return bits;
+}
+
+// over each aligned group of LANES (8, 16, 32, 64) lanes
+template <int LANES>
+__device__ __forceinline__ uint32_t head_max_bits(uint32_t v)
+{
+    if constexpr (LANES == 8) {
+        v = max(v, (uint32_t)__shfl_xor((int)v, 4));
+        v = max(v, (uint32_t)__shfl_xor((int)v, 2));
+        return max(v, (uint32_t)__shfl_xor((int)v, 1));
+    }
+    v = max(v, (uint32_t)dpp_i32<0x128>((int)v));
+    v = max(v, (uint32_t)dpp_i32<0x124>((int)v));
+    v = max(v, (uint32_t)dpp_i32<0x122>((int)v));
+    v = max(v, (uint32_t)dpp_i32<0x121>((int)v));
+    if constexpr (LANES >= 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16));
+    if constexpr (LANES >= 64) v = max(v, (uint32_t)__shfl_xor((int)v, 32));
     return v;
 }
 
-template <int DTYPE, int CODE, int D, bool LIST>
-__global__ __launch_bounds__(kThreads) void store_kernel(const StoreArgs a)
+// what becomes of a block's scale, and how its rows are written
+struct NewScale {
+    float scale, inv, ratio;
+    bool odd, again;          // a NaN or infinity is among the rows; kept rows have to be rounded again
+};
+template <int CODE>
+__device__ __forceinline__ NewScale new_scale(uint32_t bits, float old, bool keeps)
+{
+    NewScale n;
+    const float most = __uint_as_float(bits);
+    n.odd = bits >= 0x7f800000u || (keeps && old != old);
+    const float need = most > 0.f ? fmaxf(most * (1.f / top_code<CODE>()), kLeastScale) : 0.f;
+    n.scale = n.odd ? __uint_as_float(0x7fc00000u) : keeps ? fmaxf(old, need) : need;
+    n.inv = n.scale > 0.f ? 1.f / n.scale : 0.f;
+    n.again = keeps && n.scale > 0.f && n.scale != old;
+    n.ratio = n.again ? old / n.scale : 1.f;
+    return n;
+}
+
+// the codes of a 16-byte piece (codes of 0 under a scale that is no number)
+template <int DTYPE, int CODE>
+__device__ __forceinline__ void write_codes(uint8_t *dst, const uint4 w, float by, bool odd)
+{
+    if constexpr (DTYPE == KVS_BF16) {
+        uint2 c;
+        c.x = nearest_codes<CODE>(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y), by);
+        c.y = nearest_codes<CODE>(bf16_lo(w.z), bf16_hi(w.z), bf16_lo(w.w), bf16_hi(w.w), by);
+        *reinterpret_cast<uint2 *>(dst) = odd ? make_uint2(0u, 0u) : c;
+    } else {
+        const uint32_t c = nearest_codes<CODE>(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w), by);
+        *reinterpret_cast<uint32_t *>(dst) = odd ? 0u : c;
+    }
+}
+
+// four codes in steps of a scale that is 1 / ratio times theirs
+template <int CODE>
+__device__ __forceinline__ uint32_t again4(uint32_t codes, float ratio)
+{
+    float x[4];
+    widen_codes<CODE>(CODE == KVS_E4M3 ? numbers_only(codes) : codes, x);
+    return nearest_codes<CODE>(x[0], x[1], x[2], x[3], ratio);
+}
+
+// Kept rows stand for what they stood for, in steps of the new scale: `rows` of them from `to` on, those with src < 0.
+template <int CODE, int D>
+__device__ __forceinline__ void round_again(uint8_t *to, int64_t row_bytes, int rows, const int *src, float ratio, int lane)
+{
+    constexpr int CP = D / 16, N = kWaveRows * CP / kWave;    // 16-byte pieces of a row; of 32 rows, a lane's
+    uint4 held[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int e = lane + i * kWave, r = e / CP;
+        held[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows && src[r] < 0) held[i] = reinterpret_cast<const uint4 *>(to + r * row_bytes)[e % CP];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int e = lane + i * kWave, r = e / CP;
+        if (r >= rows || src[r] >= 0) continue;
+        reinterpret_cast<uint4 *>(to + r * row_bytes)[e % CP] =
+            make_uint4(again4<CODE>(held[i].x, ratio), again4<CODE>(held[i].y, ratio), again4<CODE>(held[i].z, ratio), again4<CODE>(held[i].w, ratio));
+    }
+}
+
+// ---- rows row0 .. row0 + n_sel - 1 ---------------------------------------------------------------------------------
+template <int DTYPE, int CODE, int D>
+__global__ __launch_bounds__(kThreads) void store_rows_kernel(const StoreArgs a)
 {
     constexpr int E = DTYPE == KVS_BF16 ? 8 : 4;           // elements of a 16-byte piece
     constexpr int PPR = D / E;                             // pieces of a row
@@ -50,91 +147,41 @@ __global__ __launch_bounds__(kThreads) void store_kernel(const StoreArgs a)
     __shared__ int src_s[4][kWaveRows];                    // entry that a row of the wave's part takes, -1: the row is kept
     __shared__ uint32_t most_s[2][4];
     __shared__ float old_s[2][4];
-    __shared__ int keeps_s[2][4];
+    __shared__ int keeps_s[4];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int block = 1 << a.block_log2, hk = a.n_kv_heads, units = 2 * hk;
     const int n_teams = 4 / a.waves, team = wave / a.waves, part = wave % a.waves, first_row = part * kWaveRows;
+    const int64_t blk = (a.row0 >> a.block_log2) + blockIdx.x, block0 = blk << a.block_log2;
 
-    // ---- the runs ---------------------------------------------------------------------------------------------------
-    // lane i holds entry chunk0 + i: its block (-1: outside the cache), and whether a run begins there
-    const int64_t chunk0 = LIST ? (int64_t)blockIdx.x * a.chunk : 0;
-    int64_t my_blk = -1;
-    int my_pos = -1;
-    uint64_t begins = 1;
-    int n_runs = 1;
-    if constexpr (LIST) {
-        const int64_t e = chunk0 + lane;
-        my_pos = e < a.n_sel ? a.sel_pos[e] : -1;
-        const int before = lane == 0 && chunk0 > 0 ? a.sel_pos[chunk0 - 1] : -1;
-        auto blk_of = [&](int p) -> int64_t { return p >= 0 && p < a.n_rows ? (int64_t)(p >> a.block_log2) : -1; };
-        my_blk = blk_of(my_pos);
-        int64_t left = __shfl_up((int)my_blk, 1);
-        if (lane == 0) left = blk_of(before);
-        begins = __ballot(my_blk != left || my_blk < 0);
-        const uint64_t mine = __ballot(my_blk >= 0 && lane < a.chunk && my_blk != left);
-        n_runs = __popcll(mine);
-        if (blockIdx.y == 0 && wave == 0 && my_blk >= 0 && lane < a.chunk) {
-            if (a.reused) a.reused[my_pos] = 0;
-            if (a.dev_v) for (int g = 0; g < hk; ++g) a.dev_v[(int64_t)g * a.n_rows + my_pos] = 0.f;
-        }
-        if (n_runs == 0) return;                            // the same in all waves
-    } else if (blockIdx.y == 0) {
-        const int64_t first = max((a.row0 >> a.block_log2) + blockIdx.x, (int64_t)0) << a.block_log2;
+    if (blockIdx.y == 0) {
         for (int e = tid; e < block * (hk + 1); e += kThreads) {
-            const int64_t r = first + (e & (block - 1));
+            const int64_t r = block0 + (e & (block - 1));
             const int g = e >> a.block_log2;
             if (r < a.row0 || r >= a.row0 + a.n_sel) continue;
             if (g < hk) { if (a.dev_v) a.dev_v[(int64_t)g * a.n_rows + r] = 0.f; }
             else if (a.reused) a.reused[r] = 0;
         }
     }
+    int *const src = src_s[wave];
+    const int rows_here = (int)min((int64_t)block, a.n_rows - block0) - first_row;         // from the wave's first row on
+    int mine = 0;
+    if (lane < kWaveRows) {
+        const int64_t e = block0 + first_row + lane - a.row0;
+        mine = first_row + lane < block && e >= 0 && e < a.n_sel ? (int)e : -1;
+        src[lane] = mine;
+    }
+    const bool keeps_part = __ballot(lane < kWaveRows && lane < rows_here && mine < 0) != 0;
+    if (lane == 0) keeps_s[wave] = keeps_part;
+    __syncthreads();
+    bool keeps = false;
+    for (int i = 0; i < a.waves; ++i) keeps |= keeps_s[team * a.waves + i] != 0;
 
     const int u_lo = (int)blockIdx.y * a.units_per_wg, n_units = min(a.units_per_wg, units - u_lo);
-    const int n_tasks = n_runs * n_units;
-    int *const src = src_s[wave];
-    int run_of_src = -1, parity = 0;
-    bool keeps_part = false;
-    int64_t blk = LIST ? 0 : (a.row0 >> a.block_log2) + blockIdx.x;
-    int rows_here = 0;
-    for (int k0 = 0; k0 < n_tasks; k0 += n_teams, parity ^= 1) {
-        const int task = k0 + team;
-        const bool live = task < n_tasks;
-        const int run = live ? task / n_units : 0, u = u_lo + (live ? task - run * n_units : 0);
-        if (live && run != run_of_src) {
-            run_of_src = run;
-            if (lane < kWaveRows) src[lane] = -1;
-            asm volatile("" ::: "memory");                  // (LDS works a wave's accesses off in order)
-            if constexpr (LIST) {
-                // the run-th place where a run of this chunk begins, and where the next one does
-                uint64_t left = __ballot(my_blk >= 0 && lane < a.chunk && ((begins >> lane) & 1));
-                for (int i = 0; i < run; ++i) left &= left - 1;
-                const int at = __builtin_ctzll(left);
-                const uint64_t after = at == 63 ? 0 : begins >> (at + 1);
-                const int end = after ? at + 1 + __builtin_ctzll(after) : 64;
-                blk = __builtin_amdgcn_readlane((int)my_blk, at);
-                const int base = (int)(blk << a.block_log2) + first_row;       // rows are int32 in a list
-                if (lane >= at && lane < end && (uint32_t)(my_pos - base) < (uint32_t)kWaveRows) atomicMax(&src[my_pos - base], (int)(chunk0 + lane));
-                if (end == 64) {
-                    for (int64_t s = chunk0 + 64;; s += 64) {
-                        const int64_t e = s + lane;
-                        const int p = e < a.n_sel ? a.sel_pos[e] : -1;
-                        const bool in = p >= 0 && p < a.n_rows && (p >> a.block_log2) == (int)blk;
-                        const uint64_t out = __ballot(!in);
-                        const int cut = out ? __builtin_ctzll(out) : 64;
-                        if (lane < cut && (uint32_t)(p - base) < (uint32_t)kWaveRows) atomicMax(&src[p - base], (int)e);
-                        if (cut < 64) break;
-                    }
-                }
-            } else if (lane < kWaveRows) {
-                const int64_t e = (blk << a.block_log2) + first_row + lane - a.row0;
-                src[lane] = first_row + lane < block && e >= 0 && e < a.n_sel ? (int)e : -1;
-            }
-            asm volatile("" ::: "memory");
-            rows_here = (int)min((int64_t)block, a.n_rows - (blk << a.block_log2)) - first_row;     // from the wave's first row on
-            keeps_part = __ballot(lane < kWaveRows && lane < rows_here && src[lane & (kWaveRows - 1)] < 0) != 0;
-        }
-
+    int parity = 0;
+    for (int k0 = 0; k0 < n_units; k0 += n_teams, parity ^= 1) {
+        const bool live = k0 + team < n_units;
+        const int u = u_lo + (live ? k0 + team : 0);
         const bool is_v = u >= hk;
         const int g = is_v ? u - hk : u;
         float *const scale_at = (is_v ? a.v_scale : a.k_scale) + blk * hk + g;
@@ -147,87 +194,144 @@ __global__ __launch_bounds__(kThreads) void store_kernel(const StoreArgs a)
         if (live) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int r = i * RPI + sub, e = src[r];
+                const int e = src[i * RPI + sub];
                 w[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (e >= 0) w[i] = stream_load16(from + ((int64_t)e * hk + g) * PPR + piece);
             }
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if constexpr (DTYPE == KVS_BF16) bits = max(bits, max((ww[j] << 16) & 0x7fffffffu, ww[j] & 0x7fff0000u));
-                    else bits = max(bits, ww[j] & 0x7fffffffu);
-                }
-            }
+            for (int i = 0; i < N; ++i) bits = max(bits, magnitude_bits<DTYPE>(w[i]));
         }
-        bits = wave_max_bits(bits);                         // magnitudes order as whole numbers, NaN above infinity above the rest
-        bool keeps = keeps_part;
+        bits = head_max_bits<kWave>(bits);
         if (a.waves > 1) {
             // the old scale is read by the wave that will write the new one, and has arrived before the barrier; two sets in
             // turn: a wave writes to one again only behind the barrier of the round in between
-            if (lane == 0) { most_s[parity][wave] = bits; old_s[parity][wave] = old; keeps_s[parity][wave] = keeps_part; }
+            if (lane == 0) { most_s[parity][wave] = bits; old_s[parity][wave] = old; }
             __syncthreads();
-            for (int i = 0; i < a.waves; ++i) {
-                bits = max(bits, most_s[parity][team * a.waves + i]);
-                keeps |= keeps_s[parity][team * a.waves + i] != 0;
-            }
+            for (int i = 0; i < a.waves; ++i) bits = max(bits, most_s[parity][team * a.waves + i]);
             old = old_s[parity][team * a.waves];
         }
         if (!live) continue;
-
-        const float most = __uint_as_float(bits);
-        const bool odd = bits >= 0x7f800000u || (keeps && old != old);
-        const float need = most > 0.f ? fmaxf(most * (1.f / top_code<CODE>()), kLeastScale) : 0.f;
-        float scale = keeps ? fmaxf(old, need) : need;
-        if (odd) scale = __uint_as_float(0x7fc00000u);
-        const float inv = scale > 0.f ? 1.f / scale : 0.f;   // a NaN scale: codes of 0
+        const NewScale n = new_scale<CODE>(bits, old, keeps);
         const int64_t row_bytes = (int64_t)hk * D;
-        uint8_t *to = (is_v ? a.v : a.k) + (((blk << a.block_log2) + first_row) * hk + g) * D;
+        uint8_t *to = (is_v ? a.v : a.k) + ((block0 + first_row) * hk + g) * D;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int r = i * RPI + sub;
-            if (src[r] < 0) continue;
-            uint8_t *dst = to + r * row_bytes + piece * E;
-            if constexpr (DTYPE == KVS_BF16) {
-                uint2 c;
-                c.x = nearest_codes<CODE>(bf16_lo(w[i].x) * inv, bf16_hi(w[i].x) * inv, bf16_lo(w[i].y) * inv, bf16_hi(w[i].y) * inv);
-                c.y = nearest_codes<CODE>(bf16_lo(w[i].z) * inv, bf16_hi(w[i].z) * inv, bf16_lo(w[i].w) * inv, bf16_hi(w[i].w) * inv);
-                if (odd) c = make_uint2(0u, 0u);
-                *reinterpret_cast<uint2 *>(dst) = c;
-            } else {
-                uint32_t c = nearest_codes<CODE>(__uint_as_float(w[i].x) * inv, __uint_as_float(w[i].y) * inv, __uint_as_float(w[i].z) * inv, __uint_as_float(w[i].w) * inv);
-                if (odd) c = 0u;
-                *reinterpret_cast<uint32_t *>(dst) = c;
+            if (src[r] >= 0) write_codes<DTYPE, CODE>(to + r * row_bytes + piece * E, w[i], n.inv, n.odd);
+        }
+        if (n.again) round_again<CODE, D>(to, row_bytes, rows_here, src, n.ratio, lane);
+        if (lane == 0 && part == 0) *scale_at = n.scale;
+    }
+}
+
+// ---- the rows of a list --------------------------------------------------------------------------------------------
+template <int DTYPE, int CODE, int D>
+__global__ __launch_bounds__(kThreads) void store_list_kernel(const StoreArgs a)
+{
+    constexpr int E = DTYPE == KVS_BF16 ? 8 : 4, PPR = D / E;
+    __shared__ int src_s[4][kMaxBlock];                    // entry that a row of the block takes, -1: the row is kept
+    __shared__ int row_s[4][kMaxBlock];                    // the rows that take one, in order
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hk = a.n_kv_heads, pieces = hk * PPR, columns = (pieces + kWave - 1) / kWave;
+    const bool is_v = (int)blockIdx.y >= columns;
+    const int piece = ((int)blockIdx.y - (is_v ? columns : 0)) * kWave + lane;      // of a row, the lane's
+    const bool inside = piece < pieces;
+    const int g = piece / PPR;                             // its KV head
+    int *const src = src_s[wave], *const row_at = row_s[wave];
+
+    // lane i holds entry chunk0 + i: its block (-1: outside the cache), and whether a run begins there
+    const int64_t chunk0 = ((int64_t)blockIdx.x * 4 + wave) * a.chunk;
+    if (chunk0 >= a.n_sel) return;
+    auto blk_of = [&](int p) -> int { return p >= 0 && p < a.n_rows ? p >> a.block_log2 : -1; };
+    const int my_pos = chunk0 + lane < a.n_sel ? a.sel_pos[chunk0 + lane] : -1;
+    const int before = chunk0 > 0 ? a.sel_pos[chunk0 - 1] : -1;
+    const int my_blk = blk_of(my_pos);
+    int left = __shfl_up(my_blk, 1);
+    if (lane == 0) left = blk_of(before);
+    const uint64_t ends = __ballot(my_blk != left || my_blk < 0);      // where what stands before ends
+    uint64_t runs = __ballot(my_blk >= 0 && lane < a.chunk && my_blk != left);
+    if (blockIdx.y == 0 && my_blk >= 0 && lane < a.chunk) {
+        if (a.reused) a.reused[my_pos] = 0;
+        if (a.dev_v) for (int g = 0; g < hk; ++g) a.dev_v[(int64_t)g * a.n_rows + my_pos] = 0.f;
+    }
+    const uint4 *const from = reinterpret_cast<const uint4 *>(is_v ? a.v_new : a.k_new);
+    const int64_t row_bytes = (int64_t)hk * D;
+    // LDS works a wave's accesses off in order: this only keeps the compiler from changing that order
+    auto in_order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); };
+
+    for (; runs; runs &= runs - 1) {
+        const int at = __builtin_ctzll(runs);
+        const uint64_t after = at == 63 ? 0 : ends >> (at + 1);
+        const int end = after ? at + 1 + __builtin_ctzll(after) : 64;
+        const int blk = __builtin_amdgcn_readlane(my_blk, at);
+        const int64_t block0 = (int64_t)blk << a.block_log2;
+        const int base = (int)block0;                       // positions are 32 bits
+        float *const scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)blk * hk + g;
+        const float old = inside ? *scale_at : 0.f;
+
+        in_order();
+        src[lane] = -1;
+        src[lane + 64] = -1;
+        in_order();
+        if (lane >= at && lane < end) atomicMax(&src[my_pos - base], (int)(chunk0 + lane));
+        if (end == 64) {
+            for (int64_t s = chunk0 + 64;; s += 64) {
+                const int p = s + lane < a.n_sel ? a.sel_pos[s + lane] : -1;
+                const uint64_t out = __ballot(blk_of(p) != blk);
+                const int cut = out ? __builtin_ctzll(out) : 64;
+                if (lane < cut) atomicMax(&src[p - base], (int)(s + lane));
+                if (cut < 64) break;
             }
         }
-        // kept rows stand for what they stood for, in steps of the new scale
-        if (keeps && !odd && scale > 0.f && scale != old) {
-            const float ratio = old / scale;
-            constexpr int CP = D / 16;                       // 16-byte pieces of a row of codes
-            uint4 held[kWaveRows * CP / kWave];
+        in_order();
+        const int rows_here = (int)min((int64_t)1 << a.block_log2, a.n_rows - block0);
+        const uint64_t lo = __ballot(src[lane] >= 0), hi = __ballot(src[lane + 64] >= 0);
+        const uint64_t below = ((uint64_t)1 << lane) - 1;
+        if ((lo >> lane) & 1) row_at[__popcll(lo & below)] = lane;
+        if ((hi >> lane) & 1) row_at[__popcll(lo) + __popcll(hi & below)] = lane + 64;
+        in_order();
+        const int count = __popcll(lo) + __popcll(hi);
+        const bool keeps = count < rows_here;
+        uint8_t *const to = (is_v ? a.v : a.k) + block0 * row_bytes;
+
+        uint4 w[kListRows];
+        uint32_t bits = 0;
+        auto load = [&](int k0) {                           // rows k0 .. k0 + 7 of the run; beyond its end: zeros
 #pragma unroll
-            for (int i = 0; i < kWaveRows * CP / kWave; ++i) {
-                const int e = lane + i * kWave, r = e / CP;
-                held[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (r < rows_here && src[r] < 0) held[i] = reinterpret_cast<const uint4 *>(to + r * row_bytes)[e % CP];
+            for (int j = 0; j < kListRows; ++j) {
+                w[j] = make_uint4(0u, 0u, 0u, 0u);
+                if (k0 + j < count && inside) w[j] = stream_load16(from + (int64_t)src[row_at[k0 + j]] * pieces + piece);
             }
+        };
+        for (int k0 = 0; k0 < count; k0 += kListRows) {
+            load(k0);
 #pragma unroll
-            for (int i = 0; i < kWaveRows * CP / kWave; ++i) {
-                const int e = lane + i * kWave, r = e / CP;
-                if (r >= rows_here || src[r] >= 0) continue;
-                const uint32_t cc[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
-                uint32_t out[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float x[4];
-                    widen_codes<CODE>(CODE == KVS_E4M3 ? numbers_only(cc[j]) : cc[j], x);
-                    out[j] = nearest_codes<CODE>(x[0] * ratio, x[1] * ratio, x[2] * ratio, x[3] * ratio);
-                }
-                reinterpret_cast<uint4 *>(to + r * row_bytes)[e % CP] = make_uint4(out[0], out[1], out[2], out[3]);
-            }
+            for (int j = 0; j < kListRows; ++j) bits = max(bits, magnitude_bits<DTYPE>(w[j]));
         }
-        if (lane == 0 && part == 0) *scale_at = scale;
+        bits = head_max_bits<PPR>(bits);
+        const NewScale n = new_scale<CODE>(bits, old, keeps);
+        for (int k0 = 0; k0 < count; k0 += kListRows) {
+            if (count > kListRows) load(k0);                // (a long run: a second time)
+#pragma unroll
+            for (int j = 0; j < kListRows; ++j)
+                if (k0 + j < count && inside) write_codes<DTYPE, CODE>(to + row_at[k0 + j] * row_bytes + piece * E, w[j], n.inv, n.odd);
+        }
+        if (inside && lane % PPR == 0) *scale_at = n.scale;
+        if (__ballot(n.again && inside) == 0) continue;
+        // Kept rows stand for what they stood for, in steps of the new scale.  The wave's heads have kCodes 16-byte pieces of codes a row.
+        constexpr int kCodes = kWave * E / 16, kAtOnce = kWave / kCodes;
+        const int c = lane % kCodes, from_lane = c * 16 / E;   // a lane that has the scale of that piece's head
+        const float ratio = __shfl(n.ratio, from_lane);
+        const bool wanted = __shfl((int)(n.again && inside), from_lane) != 0;
+        uint8_t *const codes = to + (piece - lane) * E + c * 16;
+#pragma unroll 4
+        for (int r = lane / kCodes; r < rows_here; r += kAtOnce) {
+            if (!wanted || src[r] >= 0) continue;
+            uint4 *const at16 = reinterpret_cast<uint4 *>(codes + r * row_bytes);
+            const uint4 x = *at16;
+            *at16 = make_uint4(again4<CODE>(x.x, ratio), again4<CODE>(x.y, ratio), again4<CODE>(x.z, ratio), again4<CODE>(x.w, ratio));
+        }
     }
 }
 
@@ -266,27 +370,29 @@ extern "C" kvs_status kvs_store_kv8(const kvs_shape *shape, const kvs_cache8 *ca
     const int block = cache->block, waves = block <= kWaveRows ? 1 : block / kWaveRows, teams = 4 / waves, units = 2 * shape->n_kv_heads;
     StoreArgs a = {k_new, v_new, (uint8_t *)cache->k, (uint8_t *)cache->v, cache->k_scale, cache->v_scale, reused, dev_v, sel_pos,
                    row0, n_sel, cache->n_rows, shape->n_kv_heads, __builtin_ctz((unsigned)block), waves, 1, 1};
-    int64_t wgs;
+    dim3 grid;
     if (sel_pos) {
-        // a unit a workgroup; chunks that give a team one run, longer ones once there are more workgroups than the chip holds
-        int64_t chunk = teams;
-        while (chunk < kMaxChunk && (n_sel / chunk) * units > kManyWgs) chunk *= 2;
+        // how many runs the list has is not known here: as many as if its rows were drawn from the cache
+        const double blocks = (double)((cache->n_rows + block - 1) / block), runs = blocks * (1.0 - exp(-(double)n_sel / blocks));
+        const int64_t pieces = (int64_t)shape->n_kv_heads * shape->head_dim * (int64_t)elem_bytes(shape->dtype) / 16, groups = 2 * ((pieces + kWave - 1) / kWave);
+        int64_t chunk = 1;
+        while (chunk < kMaxChunk && (3 * chunk * runs <= (double)n_sel || (n_sel / chunk) * groups > kManyWaves)) chunk *= 2;
         a.chunk = (int)chunk;
-        wgs = (n_sel + chunk - 1) / chunk;
+        grid = dim3((unsigned)((n_sel + 4 * chunk - 1) / (4 * chunk)), (unsigned)groups);
     } else {
         // 1024 workgroups keep the compute units busy, and a block has no more rounds to share
-        wgs = (row0 + n_sel - 1) / block - row0 / block + 1;
+        const int64_t wgs = (row0 + n_sel - 1) / block - row0 / block + 1;
         const int64_t rounds = (units + teams - 1) / teams;
         int64_t split = (1024 + wgs - 1) / wgs;
         if (split > rounds) split = rounds;
         a.units_per_wg = (int)((rounds + split - 1) / split) * teams;
+        grid = dim3((unsigned)wgs, (unsigned)((units + a.units_per_wg - 1) / a.units_per_wg));
     }
-    const dim3 grid((unsigned)wgs, (unsigned)((units + a.units_per_wg - 1) / a.units_per_wg));
     hipStream_t hs = (hipStream_t)stream;
 #define KVS_STORE(DT, C, DD)                                                                                          \
     do {                                                                                                              \
-        if (sel_pos) hipLaunchKernelGGL((store_kernel<DT, C, DD, true>), grid, dim3(kThreads), 0, hs, a);              \
-        else hipLaunchKernelGGL((store_kernel<DT, C, DD, false>), grid, dim3(kThreads), 0, hs, a);                     \
+        if (sel_pos) hipLaunchKernelGGL((store_list_kernel<DT, C, DD>), grid, dim3(kThreads), 0, hs, a);               \
+        else hipLaunchKernelGGL((store_rows_kernel<DT, C, DD>), grid, dim3(kThreads), 0, hs, a);                       \
     } while (0)
 #define KVS_STORE_D(DT, C) do { if (shape->head_dim == 128) KVS_STORE(DT, C, 128); else KVS_STORE(DT, C, 64); } while (0)
     if (shape->dtype == KVS_BF16) { if (cache->code == KVS_E4M3) KVS_STORE_D(KVS_BF16, KVS_E4M3); else KVS_STORE_D(KVS_BF16, KVS_INT8); }
