@@ -7,7 +7,9 @@
 // What bounds it is memory: every element is read and written once, with three flops.  Sine and cosine of a (token,
 // pair) are the same for all heads, so a workgroup takes a few tokens, makes their sines and cosines once, one pair a
 // thread, into LDS (8 bytes a pair), and then streams the tokens' heads: a thread takes a cell of 16 bytes of u and 16 bytes
-// of v (in the interleaved layout 32 bytes in a row), kCells cells at once so that their loads are in flight together.
+// of v (in the interleaved layout, and where channels pass through to another buffer, 32 bytes in a row).  What a cell is is found
+// by multiplications, and a thread has one cell at a time: with divisions and two cells, 131072 rows of 4 heads took 74 us instead
+// of 52 to 54, which is what a copy of their bytes takes; 8192 rows of 32 + 8 heads 39 instead of 30 (5.5 TB/s; 34 with ordinary loads).
 // Both layouts need rotary_dim to be a multiple of two cells' channels (16 in bf16, 8 in fp32); other sizes go to a
 // kernel that takes one pair a thread.
 #include "kvs_internal.h"
@@ -21,7 +23,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = 64;
-constexpr int kCells = 2;             // cells a thread has in flight
 constexpr int kMaxTokens = 32;        // tokens a workgroup takes at most: 16 KiB of sines and cosines
 
 struct Frequencies { double turns[kMaxPairs]; };   // per position
@@ -32,6 +33,13 @@ struct Rows {
     void *out;
     int64_t in_stride, out_stride;      // elements
     int32_t heads;
+};
+
+// x / n for x * n below 2^32
+struct Divisor {
+    uint32_t n, m;
+    explicit Divisor(uint32_t d) : n(d), m(d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0u) {}
+    __device__ __forceinline__ int operator()(int x) const { return n > 1 ? (int)__umulhi((uint32_t)x, m) : x; }
 };
 
 __device__ __forceinline__ float2 turn_of(double turns)
@@ -72,76 +80,58 @@ template <> struct Cell<KVS_F32> {
     }
 };
 
-// cells of one head: `turned` pairs of 16-byte pieces, then, where the output is another buffer, the pieces that pass through
+// cells of one head: pairs of 16-byte pieces, those that turn, then, where the output is another buffer, those that pass through
 template <int DTYPE, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const Frequencies fr, const Rows q, const Rows k, int64_t n_tokens, int tokens_per_wg,
-                                                          int pairs, int cells_q, int cells_k, int passed, int head_dim, float magnitude,
+                                                          const Divisor pairs_d, const Divisor per_token_d, const Divisor per_head_d, int cells_q, int head_dim, float magnitude,
                                                           const int32_t *__restrict__ pos, const int32_t *__restrict__ pos_from)
 {
     constexpr int E = Cell<DTYPE>::E;
     extern __shared__ float2 cs[];                         // [tokens][pairs] (cos, sin), times the magnitude
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, pairs = (int)pairs_d.n;
     const int64_t tok0 = (int64_t)blockIdx.x * tokens_per_wg;
     const int toks = (int)min((int64_t)tokens_per_wg, n_tokens - tok0);
     for (int e = tid; e < toks * pairs; e += kThreads) {
-        const int t = e / pairs, j = e - t * pairs;
+        const int t = pairs_d(e), j = e - t * pairs;
         const float2 x = turn_of(moved(pos, pos_from, tok0 + t) * fr.turns[j]);
         cs[e] = make_float2(x.x * magnitude, x.y * magnitude);
     }
     __syncthreads();
 
-    const int turned = pairs / E, per_head = turned + passed;
-    const int per_token = cells_q + cells_k, all = toks * per_token;
-    for (int base = tid; base < all; base += kThreads * kCells) {
-        uint4 a[kCells], b[kCells];
-        char *to_a[kCells], *to_b[kCells];
-        const float2 *at[kCells];
+    const int turned = pairs / E, per_head = (int)per_head_d.n, per_token = (int)per_token_d.n, all = toks * per_token;
+    for (int c = tid; c < all; c += kThreads) {
+        const int t = per_token_d(c);
+        int cell = c - t * per_token;
+        const bool is_k = cell >= cells_q;
+        if (is_k) cell -= cells_q;
+        const int head = per_head_d(cell), piece = cell - head * per_head;
+        const bool turns = piece < turned;
+        // first channels of the cell's two pieces (2 E turned channels to a cell that turns, so the others begin at 2 E turned)
+        const int c0 = INTERLEAVED || !turns ? 2 * E * piece : E * piece, c1 = INTERLEAVED || !turns ? c0 + E : c0 + pairs;
+        const int64_t row = tok0 + t;
+        constexpr int size = 16 / E;
+        const char *in = (const char *)(is_k ? k.in : q.in) + (row * (is_k ? k.in_stride : q.in_stride) + (int64_t)head * head_dim) * size;
+        char *out = (char *)(is_k ? k.out : q.out) + (row * (is_k ? k.out_stride : q.out_stride) + (int64_t)head * head_dim) * size;
+        const uint4 a = stream_load16(reinterpret_cast<const uint4 *>(in + c0 * size)), b = stream_load16(reinterpret_cast<const uint4 *>(in + c1 * size));
+        uint4 *const to_a = reinterpret_cast<uint4 *>(out + c0 * size), *const to_b = reinterpret_cast<uint4 *>(out + c1 * size);
+        if (!turns) { *to_a = a; *to_b = b; continue; }
+        const float2 *const at = cs + t * pairs + piece * E;
+        float x[E], y[E], xx[E], yy[E];
+        Cell<DTYPE>::widen(a, x);
+        Cell<DTYPE>::widen(b, y);
 #pragma unroll
-        for (int i = 0; i < kCells; ++i) {
-            const int c = base + i * kThreads;
-            to_a[i] = nullptr;
-            if (c < all) {
-                const int t = c / per_token;
-                int cell = c - t * per_token;
-                const bool is_k = cell >= cells_q;
-                if (is_k) cell -= cells_q;
-                const int head = cell / per_head, piece = cell - head * per_head;
-                const bool turns = piece < turned;
-                // first channel of the cell's two pieces (a piece that passes through: of the one)
-                const int c0 = !turns ? 2 * pairs + (piece - turned) * E : INTERLEAVED ? 2 * E * piece : E * piece;
-                const int c1 = !turns ? c0 : INTERLEAVED ? c0 + E : c0 + pairs;
-                const int64_t row = tok0 + t;
-                const int size = 16 / E;
-                const char *in = (const char *)(is_k ? k.in : q.in) + (row * (is_k ? k.in_stride : q.in_stride) + (int64_t)head * head_dim) * size;
-                char *out = (char *)(is_k ? k.out : q.out) + (row * (is_k ? k.out_stride : q.out_stride) + (int64_t)head * head_dim) * size;
-                a[i] = *reinterpret_cast<const uint4 *>(in + c0 * size);
-                b[i] = *reinterpret_cast<const uint4 *>(in + c1 * size);
-                to_a[i] = out + c0 * size;
-                to_b[i] = out + c1 * size;
-                at[i] = turns ? cs + t * pairs + piece * E : nullptr;
-            }
+        for (int e = 0; e < E; ++e) {
+            const float2 r = at[e];
+            // interleaved: pair e is channels 2e, 2e + 1 of the 2E in a row
+            const float u = INTERLEAVED ? (e < E / 2 ? x[2 * e % E] : y[2 * e % E]) : x[e];
+            const float v = INTERLEAVED ? (e < E / 2 ? x[(2 * e + 1) % E] : y[(2 * e + 1) % E]) : y[e];
+            const float uu = u * r.x - v * r.y, vv = v * r.x + u * r.y;
+            if (!INTERLEAVED) { xx[e] = uu; yy[e] = vv; }
+            else if (e < E / 2) { xx[2 * e % E] = uu; xx[(2 * e + 1) % E] = vv; }
+            else { yy[2 * e % E] = uu; yy[(2 * e + 1) % E] = vv; }
         }
-#pragma unroll
-        for (int i = 0; i < kCells; ++i) {
-            if (!to_a[i]) continue;
-            if (!at[i]) { *reinterpret_cast<uint4 *>(to_a[i]) = a[i]; continue; }
-            float x[E], y[E], xx[E], yy[E];
-            Cell<DTYPE>::widen(a[i], x);
-            Cell<DTYPE>::widen(b[i], y);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float2 r = at[i][e];
-                // interleaved: pair e is channels 2e, 2e + 1 of the 2E in a row
-                const float u = INTERLEAVED ? (e < E / 2 ? x[2 * e % E] : y[2 * e % E]) : x[e];
-                const float v = INTERLEAVED ? (e < E / 2 ? x[(2 * e + 1) % E] : y[(2 * e + 1) % E]) : y[e];
-                const float uu = u * r.x - v * r.y, vv = v * r.x + u * r.y;
-                if (!INTERLEAVED) { xx[e] = uu; yy[e] = vv; }
-                else if (e < E / 2) { xx[2 * e % E] = uu; xx[(2 * e + 1) % E] = vv; }
-                else { yy[2 * e % E] = uu; yy[(2 * e + 1) % E] = vv; }
-            }
-            *reinterpret_cast<uint4 *>(to_a[i]) = Cell<DTYPE>::round(xx);
-            *reinterpret_cast<uint4 *>(to_b[i]) = Cell<DTYPE>::round(yy);
-        }
+        *to_a = Cell<DTYPE>::round(xx);
+        *to_b = Cell<DTYPE>::round(yy);
     }
 }
 
@@ -278,10 +268,10 @@ extern "C" kvs_status kvs_rotary(const kvs_shape *shape, const kvs_rotary_spec *
     auto in_place = [](const Rows &x) { return x.in == x.out; };
     const bool same = (!rows[0].heads || in_place(rows[0])) && (!rows[1].heads || in_place(rows[1]));
     if (pairs % e == 0) {
-        const int passed = same ? 0 : left / e, per_head = pairs / e + passed;
+        const int per_head = pairs / e + (same ? 0 : left / (2 * e));
         const int cells_q = rows[0].heads * per_head, cells_k = rows[1].heads * per_head, per_token = cells_q + cells_k;
-        // as many tokens as give every thread its kCells cells, as long as that leaves two workgroups a compute unit
-        int toks = (kThreads * kCells + per_token - 1) / per_token;
+        // as many tokens as give every thread a cell, as long as that leaves two workgroups a compute unit
+        int toks = (kThreads + per_token - 1) / per_token;
         if (toks > kMaxTokens) toks = kMaxTokens;
         if (toks > n_tokens / 512) toks = (int)(n_tokens / 512);
         if (toks < 1) toks = 1;
@@ -289,8 +279,8 @@ extern "C" kvs_status kvs_rotary(const kvs_shape *shape, const kvs_rotary_spec *
         if (wgs > 0x7fffffff) return fail(KVS_EINVAL, "kvs_rotary: too many rows");
         const size_t lds = (size_t)toks * pairs * sizeof(float2);
 #define KVS_ROT(DT, IL)                                                                                                              \
-        hipLaunchKernelGGL((rotary_kernel<DT, IL>), dim3((unsigned)wgs), dim3(kThreads), lds, hs, fr, rows[0], rows[1], n_tokens, toks, pairs, \
-                           cells_q, cells_k, passed, d, magnitude, pos, pos_from)
+        hipLaunchKernelGGL((rotary_kernel<DT, IL>), dim3((unsigned)wgs), dim3(kThreads), lds, hs, fr, rows[0], rows[1], n_tokens, toks,       \
+                           Divisor(pairs), Divisor(per_token), Divisor(per_head), cells_q, d, magnitude, pos, pos_from)
         const bool il = spec->layout == KVS_ROTARY_INTERLEAVED;
         if (bf16) { if (il) KVS_ROT(KVS_BF16, true); else KVS_ROT(KVS_BF16, false); }
         else { if (il) KVS_ROT(KVS_F32, true); else KVS_ROT(KVS_F32, false); }
