@@ -16,9 +16,8 @@
 // (global to LDS, 16 bytes a lane, no registers), two tiles deep and without a barrier; at the end the waves meet in LDS.
 // Launches of too few workgroups cut the key ranges into pieces, which a second kernel merges.
 //
-// A lane's V operand is 8 keys of one channel, but a row of codes lies along the channels: a lane reads D/32 neighbouring
-// channels of each of 8 keys and permutes bytes, and channel D/32 * m + db stands at matrix row m of product db, which
-// costs nothing (the output's order is undone where it is stored).
+// A lane's V operand is 8 keys of one channel, but a row of codes lies along the channels: the LDS reads that transpose
+// bytes among 16 lanes give it those (64 bits a lane, from 8 rows of 16 bytes).
 #include "cache8.h"
 #include "attention.h"
 
@@ -91,6 +90,22 @@ __device__ __forceinline__ void split3(const float (&x)[8], u32x4_t (&part)[3])
     }
 }
 
+__device__ __forceinline__ float max_of_halves(float x)      // of lanes i and i + 32
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2_t *lds_i32x2;
+
+// Byte `lane % 16` of eight rows of 16 bytes, the rows at which the lanes 16 i .. 16 i + 15 point, two lanes a row (at its halves).
+__device__ __forceinline__ u32x2_t column8(const char *at)
+{
+    return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)at));
+}
+
 typedef const __attribute__((address_space(4))) float *scalar_f32;    // read by all lanes at one address: scalar loads
 
 template <int DTYPE, int CODE, int D>
@@ -128,26 +143,20 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     const int rq = min(row_block * kRows + ln, rows - 1);
     const int t_sel = rq / grp, hh = rq - t_sel * grp;
     int pos = sel_pos[sel_lo + t_sel];
-    pos = pos < 0 ? -1 : min(pos, ctx_len - 1);
-    int pmin = pos, pmax = pos;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        pmin = min(pmin, __shfl_xor(pmin, o));
-        pmax = max(pmax, __shfl_xor(pmax, o));
-    }
-    pmin = __builtin_amdgcn_readfirstlane(pmin);
-    pmax = __builtin_amdgcn_readfirstlane(pmax);
-
     // keys are counted from the 16-row boundary at or before the context: x = key + shift
     const int shift = (int)(td.ctx_off[b] & (kAlign - 1));
     const int64_t row0 = td.ctx_off[b] - shift;
-    const int xpos = pos < 0 ? -1 : pos + shift;            // last x that the row sees; the first is `shift`
-    const int64_t n_tiles = pmax < 0 ? 0 : ((int64_t)pmax + shift) / kKeys + 1;
-    const int64_t t_lo = (int64_t)piece * td.piece_tiles;
-    const int64_t t_hi = min(n_tiles, t_lo + td.piece_tiles);
-    const int mine = (int)max((int64_t)0, (t_hi - t_lo - wave + kWaves - 1) / kWaves);      // tiles t_lo + wave + 4 i
+    const int64_t t_lo = (int64_t)piece * td.piece_tiles, t_most = t_lo + td.piece_tiles;
+    // the wave's tiles are t_lo + wave + kWaves i, as many as lie below x (and the piece's end)
+    auto tiles_below = [&](int64_t x) -> int {
+        const int64_t end = min((x + kKeys - 1) / kKeys, t_most);
+        return (int)max((int64_t)0, (end - t_lo - wave + kWaves - 1) / kWaves);
+    };
 
-    // ---- Q as the B operand: k-step 2i + s takes channels 32i + 16hf + 8s .. +7, as the K rows are read below ---
+    // ---- Q as the B operand: k-step 2i + s takes channels 32i + 16hf + 8s .. +7, as the K rows are read below.  A negative
+    // scale's sign goes into Q, so that the largest score is the largest product's -------------------------------
+    const bool negative = scale_log2 < 0.f;
+    const float scale_abs = fabsf(scale_log2);
     bf16x8 qreg[NP][D / 16];
     {
         const int64_t at = ((sel_lo + t_sel) * n_q_heads + g * grp + hh) * (int64_t)D + 16 * hf;
@@ -155,10 +164,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
         for (int ks = 0; ks < D / 16; ++ks) {
             const int c = 32 * (ks >> 1) + 8 * (ks & 1);
             if constexpr (DTYPE == KVS_BF16) {
-                qreg[0][ks] = as_bf16x8(*reinterpret_cast<const u32x4_t *>((const uint16_t *)q_sel + at + c));
+                const u32x4_t w = *reinterpret_cast<const u32x4_t *>((const uint16_t *)q_sel + at + c);
+                qreg[0][ks] = as_bf16x8(w ^ (negative ? 0x80008000u : 0u));
             } else {
                 const float4 lo = *reinterpret_cast<const float4 *>((const float *)q_sel + at + c), hi = *reinterpret_cast<const float4 *>((const float *)q_sel + at + c + 4);
-                const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = negative ? -x[j] : x[j];
                 u32x4_t part[3];
                 split3(x, part);
 #pragma unroll
@@ -215,6 +227,24 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
         return s;
     };
 
+    // The first two tiles are asked for before anybody knows how far the rows see: as if they saw the whole context.
+    const int whole = tiles_below(ctx_len > 0 ? (int64_t)ctx_len + shift : 0);
+    if (whole > 0) stage(t_lo + wave, 0);
+    if (whole > 1) stage(t_lo + wave + kWaves, 1);
+    Scales next = {};
+    if (whole > 0) next = scales_of(t_lo + wave);
+    pos = pos < 0 ? -1 : min(pos, ctx_len - 1);
+    int pmin = pos, pmax = pos;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        pmin = min(pmin, __shfl_xor(pmin, o));
+        pmax = max(pmax, __shfl_xor(pmax, o));
+    }
+    pmin = __builtin_amdgcn_readfirstlane(pmin);
+    pmax = __builtin_amdgcn_readfirstlane(pmax);
+    const int xpos = pos < 0 ? -1 : pos + shift;            // last x that the row sees; the first is `shift`
+    const int mine = tiles_below(pmax < 0 ? 0 : (int64_t)pmax + shift + 1);
+
     // ---- running state ------------------------------------------------------------------------------------------
     floatx16 o_acc[NDB];
 #pragma unroll
@@ -227,16 +257,12 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     // K row of matrix row ln: bits 2 and 3 swapped, so that accumulator entry r is key 16 (r >> 3) + 8 hf + (r & 7)
     const int krow = (ln & ~12) | ((ln & 4) << 1) | ((ln & 8) >> 1);
 
-    if (mine > 0) stage(t_lo + wave, 0);
-    if (mine > 1) stage(t_lo + wave + kWaves, 1);
-    Scales next = {};
-    if (mine > 0) next = scales_of(t_lo + wave);
     for (int i = 0; i < mine; ++i) {
         const int64_t t = t_lo + wave + (int64_t)kWaves * i;
         const Scales sc = next;
         if (i + 1 < mine) next = scales_of(t + kWaves);
         // this tile has landed; the next one's loads may still be on their way
-        if (i + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * NL) : "memory");
+        if (i + 1 < mine || (i == 0 && whole > 1)) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * NL) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         char *const kt = my_lds + (i & 1) * (2 * TILE_B);
         char *const vt = kt + TILE_B;
@@ -265,19 +291,28 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(hi), qreg[p][2 * c + 1], s, 0, 0, 0);
             }
         }
-        bool seen[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        float f[2] = {sc.k[0] * scale_abs, sc.k[1] * scale_abs};
+        auto seen = [&](int r) {
             const int x = x0 + 16 * (r >> 3) + 8 * hf + (r & 7);
-            seen[r] = !masked || (x >= shift && x <= xpos);
-            const float y = s[r] * (sc.k[r >> 3] * scale_log2);
-            s[r] = seen[r] ? y : -INFINITY;                 // behind the scale, which may be a NaN
-        }
-        float mx = s[0];
+            return x >= shift && x <= xpos;
+        };
+        if (masked) {
 #pragma unroll
-        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float m_new = fmaxf(m_run, mx);
+            for (int r = 0; r < 16; ++r) {
+                const float y = s[r] * f[r >> 3];
+                s[r] = seen(r) ? y : -INFINITY;              // behind the scale, which may be a NaN
+            }
+            f[0] = f[1] = 1.f;
+        }
+        float m_new = m_run;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            float mx = s[8 * a];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[8 * a + j]);
+            m_new = fmaxf(m_new, mx * f[a]);
+        }
+        m_new = max_of_halves(m_new);
         const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
         u32x4_t pop[2][NP];
@@ -287,9 +322,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
             float y[8], group = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float p = __builtin_amdgcn_exp2f(s[8 * a + j] - m_new);
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * a + j], f[a], -m_new));
                 group += p;
-                y[j] = seen[8 * a + j] ? p * sc.v[a] : 0.f;
+                y[j] = p * sc.v[a];
+            }
+            if (masked && !(fabsf(sc.v[a]) < INFINITY)) {    // 0 times a broken block's scale
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = seen(8 * a + j) ? y[j] : 0.f;
             }
             psum += group;
             if constexpr (DTYPE == KVS_BF16) {
@@ -322,22 +361,12 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
 
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-            uint32_t lo[8], hi[8];                          // channels 0, 1 and 2, 3 of the lane's four, key by key
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int key = 16 * a + 8 * hf + j;
-                const int chunk = NDB == 4 ? ln >> 2 : ln >> 3, in_chunk = NDB == 4 ? (ln & 3) * 4 : (ln & 7) * 2;
-                const char *p = vt + key * D + (chunk ^ swz(key)) * 16 + in_chunk;
-                const uint32_t w = NDB == 4 ? *reinterpret_cast<const uint32_t *>(p) : (uint32_t) * reinterpret_cast<const uint16_t *>(p);
-                lo[j] = pair_of<CODE, false>(w);
-                hi[j] = NDB == 4 ? pair_of<CODE, true>(w) : 0u;
-            }
+            const int key = 16 * a + 8 * hf + ((ln & 15) >> 1);          // the row that the lane points at, for the lanes of its 16
+            const char *from = vt + key * D + (ln & 1) * 8;
 #pragma unroll
             for (int db = 0; db < NDB; ++db) {
-                const uint32_t *from = db < 2 ? lo : hi;
-                const uint32_t sel = (db & 1) ? 0x07060302u : 0x05040100u;
-                const u32x4_t va = {__builtin_amdgcn_perm(from[1], from[0], sel), __builtin_amdgcn_perm(from[3], from[2], sel),
-                                    __builtin_amdgcn_perm(from[5], from[4], sel), __builtin_amdgcn_perm(from[7], from[6], sel)};
+                const u32x2_t w = column8(from + ((2 * db + (ln >> 4)) ^ swz(key)) * 16);      // channel 32 db + ln, keys 16 a + 8 hf .. + 7
+                const u32x4_t va = {pair_of<CODE, false>(w.x), pair_of<CODE, true>(w.x), pair_of<CODE, false>(w.y), pair_of<CODE, true>(w.y)};
 #pragma unroll
                 for (int p = 0; p < NP; ++p) o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va), as_bf16x8(pop[a][p]), o_acc[db], 0, 0, 0);
             }
@@ -347,6 +376,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
             stage(t + 2 * kWaves, i & 1);
         }
     }
+
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // tiles that no row sees may still be on their way into LDS
 
     // ---- the waves meet --------------------------------------------------------------------------------------------
     {
@@ -361,12 +392,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
         const float f = __builtin_amdgcn_exp2f(m_run - top);
         float *mine_o = reinterpret_cast<float *>(my_lds) + ln * D;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int m = 8 * (r >> 2) + 4 * hf + (r & 3);   // channels NDB m .. : at place m ^ row, so that rows use different banks
-            float *p = mine_o + (m ^ ln) * NDB;
-            if constexpr (NDB == 4) *reinterpret_cast<float4 *>(p) = make_float4(o_acc[0][r] * f, o_acc[1][r] * f, o_acc[2][r] * f, o_acc[3][r] * f);
-            else *reinterpret_cast<float2 *>(p) = make_float2(o_acc[0][r] * f, o_acc[1][r] * f);
-        }
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c4 = 8 * db + 2 * q + hf;          // channels 4 c4 .. + 3: at place c4 ^ row, so that rows use different banks
+                *reinterpret_cast<float4 *>(mine_o + 4 * (c4 ^ (ln & (D / 4 - 1)))) =
+                    make_float4(o_acc[db][4 * q] * f, o_acc[db][4 * q + 1] * f, o_acc[db][4 * q + 2] * f, o_acc[db][4 * q + 3] * f);
+            }
     }
     __syncthreads();
     constexpr int CPT = D / 8;                               // channels a thread stores
@@ -390,10 +422,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     for (int w = 0; w < kWaves; ++w) {
         const float *from = reinterpret_cast<const float *>(lds + w * WAVE_B) + row * D;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float *p = from + ((4 * part + k) ^ row) * NDB;
-#pragma unroll
-            for (int c = 0; c < NDB; ++c) o[k * NDB + c] += p[c];
+        for (int k = 0; k < CPT / 4; ++k) {
+            const float4 y = *reinterpret_cast<const float4 *>(from + 4 * ((CPT / 4 * part + k) ^ (row & (D / 4 - 1))));
+            o[4 * k] += y.x; o[4 * k + 1] += y.y; o[4 * k + 2] += y.z; o[4 * k + 3] += y.w;
         }
     }
     const int t2 = row_q / grp, h2 = row_q - t2 * grp;
