@@ -33,10 +33,10 @@ constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kRows = 32;              // rows of a unit
 constexpr int kKeys = 32;              // keys of a tile
 constexpr int kAlign = 16;             // cache rows that tiles are aligned to: no block is shorter
-constexpr int kSplitBelow = 1024;      // workgroups below which key ranges are cut
-constexpr int kTargetWgs = 1024;
+constexpr float kSlack = 8.f;          // powers of two that a score may lie above its reference
 constexpr int kMinPieceTiles = 8;      // tiles of a piece: two for each wave
 constexpr int kMaxPieces = 512;
+constexpr int64_t kMaxCutWgs = 2048;   // workgroups at most where key ranges are cut: four for every place on the chip
 
 // The launch's requests.  Workgroup = (unit, KV head); a unit is a block of 32 rows of one request and one piece of its keys.
 struct Table {
@@ -106,6 +106,13 @@ __device__ __forceinline__ u32x2_t column8(const char *at)
     return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)at));
 }
 
+// The NaN that both NaN codes of e4m3 widen to (0xffc0) is the largest pattern there is: it becomes the negative of the largest number.
+__device__ __forceinline__ u32x4_t numbers_of_bf16(u32x4_t v)
+{
+    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(u32x4_t, __builtin_elementwise_min(__builtin_bit_cast(u16x8, v), (u16x8)(0xc3e0)));
+}
+
 typedef const __attribute__((address_space(4))) float *scalar_f32;    // read by all lanes at one address: scalar loads
 
 template <int DTYPE, int CODE, int D>
@@ -133,7 +140,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     const int unit = (int)(blockIdx.x / n_kv_heads);
     const int b = request_of(td.unit_begin, td.n_req, unit);
     const int in_req = unit - td.unit_begin[b];
-    const int pieces = td.pieces[b], piece = in_req % pieces, row_block = in_req / pieces;
+    const int pieces = td.pieces[b], row_blocks = (td.unit_begin[b + 1] - td.unit_begin[b]) / pieces;
+    // A piece's row blocks run side by side, which share its keys in L2, and the last rows, which see most, begin.
+    const int piece = in_req / row_blocks, row_block = row_blocks - 1 - in_req % row_blocks;
     const int grp = n_q_heads / n_kv_heads;
     const int ctx_len = td.ctx_len[b];
     const int rows = td.n_sel[b] * grp;                     // the host keeps this below 2^31
@@ -193,8 +202,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     auto load_1k = [&](uint32_t dst, uint32_t off, const uint8_t *base) {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(base) : "memory");
     };
-    auto stage = [&](int64_t t, int slot) {
-        const int64_t first = row0 + t * kKeys;
+    // Rows and scales of the wave's tiles lie at constant steps: kWaves tiles are 128 rows, a multiple of every block.
+    const int64_t first_row = row0 + (t_lo + wave) * kKeys;
+    auto stage = [&](int64_t first, int slot) {
         const int64_t at = (first * n_kv_heads + g) * D;
         const uint32_t dst = lds_base + (uint32_t)slot * (2 * TILE_B);
         if (first + kKeys <= n_rows) {
@@ -213,26 +223,23 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
             }
         }
     };
-    const scalar_f32 ks_p = (scalar_f32)(uintptr_t)k_scale, vs_p = (scalar_f32)(uintptr_t)v_scale;
-    const int64_t last_block = (n_rows - 1) >> block_log2;
+    static_assert(kWaves * kKeys % 128 == 0, "a multiple of the largest block");
     struct Scales { float k[2], v[2]; };
-    auto scales_of = [&](int64_t t) {
-        Scales s;
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            const int64_t blk = min((row0 + t * kKeys + kAlign * a) >> block_log2, last_block);
-            s.k[a] = ks_p[blk * n_kv_heads + g];
-            s.v[a] = vs_p[blk * n_kv_heads + g];
-        }
-        return s;
+    const int64_t scale_step = ((int64_t)(kWaves * kKeys) >> block_log2) * n_kv_heads;
+    const int64_t scale_at = (first_row >> block_log2) * n_kv_heads + g;
+    const int second_half = (int)((first_row + kAlign) >> block_log2) != (int)(first_row >> block_log2) ? n_kv_heads : 0;
+    const scalar_f32 ks_p = (scalar_f32)(uintptr_t)k_scale + scale_at, vs_p = (scalar_f32)(uintptr_t)v_scale + scale_at;
+    auto scales_of = [&](int i, int64_t first) {
+        const int64_t lo = i * scale_step, hi = lo + (first + kAlign < n_rows ? second_half : 0);
+        return Scales{{ks_p[lo], ks_p[hi]}, {vs_p[lo], vs_p[hi]}};
     };
 
     // The first two tiles are asked for before anybody knows how far the rows see: as if they saw the whole context.
     const int whole = tiles_below(ctx_len > 0 ? (int64_t)ctx_len + shift : 0);
-    if (whole > 0) stage(t_lo + wave, 0);
-    if (whole > 1) stage(t_lo + wave + kWaves, 1);
+    if (whole > 0) stage(first_row, 0);
+    if (whole > 1) stage(first_row + kWaves * kKeys, 1);
     Scales next = {};
-    if (whole > 0) next = scales_of(t_lo + wave);
+    if (whole > 0) next = scales_of(0, first_row);
     pos = pos < 0 ? -1 : min(pos, ctx_len - 1);
     int pmin = pos, pmax = pos;
 #pragma unroll
@@ -251,28 +258,29 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o_acc[db][r] = 0.f;
-    float m_run = kLowest;     // running maximum of the scores times log2 e, the same in both half-waves
+    float m_run = kLowest;     // reference of the weights: a former maximum of the scores times log2 e, the same in both half-waves
     float l_run = 0.f;         // this half-wave's share of the sum of weights
     float l_rnd = 0.f;         // the same of the weights as the second product sees them (bf16)
     // K row of matrix row ln: bits 2 and 3 swapped, so that accumulator entry r is key 16 (r >> 3) + 8 hf + (r & 7)
     const int krow = (ln & ~12) | ((ln & 4) << 1) | ((ln & 8) >> 1);
 
-    for (int i = 0; i < mine; ++i) {
-        const int64_t t = t_lo + wave + (int64_t)kWaves * i;
+    int x0 = (int)((t_lo + wave) * kKeys);                   // (contexts are shorter than 2^31)
+    int64_t tile_row = first_row;
+    for (int i = 0; i < mine; ++i, x0 += kWaves * kKeys, tile_row += kWaves * kKeys) {
         const Scales sc = next;
-        if (i + 1 < mine) next = scales_of(t + kWaves);
+        if (i + 1 < mine) next = scales_of(i + 1, tile_row + kWaves * kKeys);
         // this tile has landed; the next one's loads may still be on their way
         if (i + 1 < mine || (i == 0 && whole > 1)) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * NL) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         char *const kt = my_lds + (i & 1) * (2 * TILE_B);
         char *const vt = kt + TILE_B;
-        const int x0 = (int)(t * kKeys);                     // (contexts are shorter than 2^31)
         const bool masked = x0 < shift || x0 + kKeys - 1 > pmin + shift || pmin < 0;
 
-        // Memory that was never stored to may hold NaN codes: in rows that are masked, and in blocks of scale 0.
-        if (CODE == KVS_E4M3 && (masked || sc.k[0] == 0.f || sc.k[1] == 0.f || sc.v[0] == 0.f || sc.v[1] == 0.f)) {
+        // Memory that was never stored to may hold NaN codes: in rows that are masked, and in blocks of scale 0.  Masked scores
+        // are replaced whatever they are, and V's codes become numbers behind their conversion.
+        if (CODE == KVS_E4M3 && (sc.k[0] == 0.f || sc.k[1] == 0.f)) {
 #pragma unroll
-            for (int e = 0; e < 2 * TILE_B / 1024; ++e) {
+            for (int e = 0; e < TILE_B / 1024; ++e) {
                 u32x4_t *w = reinterpret_cast<u32x4_t *>(kt) + e * kWave + lane;
                 u32x4_t c = *w;
                 c.x = numbers_only(c.x); c.y = numbers_only(c.y); c.z = numbers_only(c.z); c.w = numbers_only(c.w);
@@ -292,29 +300,45 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
             }
         }
         float f[2] = {sc.k[0] * scale_abs, sc.k[1] * scale_abs};
-        auto seen = [&](int r) {
-            const int x = x0 + 16 * (r >> 3) + 8 * hf + (r & 7);
-            return x >= shift && x <= xpos;
-        };
+        const int first = shift - x0 - 8 * hf, last = xpos - x0 - 8 * hf;     // entries 16 (r >> 3) + (r & 7) from `first` to `last` are seen
+        auto entry = [](int r) { return 16 * (r >> 3) + (r & 7); };
         if (masked) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float y = s[r] * f[r >> 3];
-                s[r] = seen(r) ? y : -INFINITY;              // behind the scale, which may be a NaN
+            for (int a = 0; a < 2; ++a) {
+                if (!(f[a] > 0.f && f[a] < INFINITY)) {      // 0 or NaN times the -infinity of what is masked
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[8 * a + j] *= f[a];
+                    f[a] = 1.f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[8 * a + j] = entry(8 * a + j) <= last ? s[8 * a + j] : -INFINITY;
             }
-            f[0] = f[1] = 1.f;
+            if (x0 < shift) {                                // a context's first tile
+#pragma unroll
+                for (int r = 0; r < 8; ++r) s[r] = entry(r) >= first ? s[r] : -INFINITY;
+            }
         }
-        float m_new = m_run;
+        float mx_tile = -INFINITY;
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
             float mx = s[8 * a];
 #pragma unroll
             for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[8 * a + j]);
-            m_new = fmaxf(m_new, mx * f[a]);
+            mx_tile = fmaxf(mx_tile, mx * f[a]);
         }
-        m_new = max_of_halves(m_new);
-        const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
-        m_run = m_new;
+        mx_tile = max_of_halves(mx_tile);
+        // The reference that weights are relative to moves only once a score is kSlack above it (in powers of two): weights of up
+        // to 2^kSlack lose nothing, and sums are seldom scaled behind a row's first tiles.
+        if (__builtin_amdgcn_ballot_w64(mx_tile > m_run + kSlack) != 0) {
+            const float m_new = fmaxf(m_run, mx_tile), corr = __builtin_amdgcn_exp2f(m_run - m_new);
+            m_run = m_new;
+            l_run *= corr;
+            l_rnd *= corr;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o_acc[db][r] *= corr;
+        }
         u32x4_t pop[2][NP];
         float psum = 0.f, rsum = 0.f;
 #pragma unroll
@@ -322,13 +346,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
             float y[8], group = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * a + j], f[a], -m_new));
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * a + j], f[a], -m_run));
                 group += p;
                 y[j] = p * sc.v[a];
             }
             if (masked && !(fabsf(sc.v[a]) < INFINITY)) {    // 0 times a broken block's scale
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = seen(8 * a + j) ? y[j] : 0.f;
+                for (int j = 0; j < 8; ++j) y[j] = entry(8 * a + j) <= last && entry(8 * a + j) >= first ? y[j] : 0.f;
             }
             psum += group;
             if constexpr (DTYPE == KVS_BF16) {
@@ -348,32 +372,32 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
                 split3(y, pop[a]);
             }
         }
-        if (__builtin_amdgcn_ballot_w64(corr != 1.0f) != 0) {
-            l_run *= corr;
-            l_rnd *= corr;
-#pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o_acc[db][r] *= corr;
-        }
         l_run += psum;
         l_rnd += rsum;
 
+        const bool dirty = CODE == KVS_E4M3 && (masked || sc.v[0] == 0.f || sc.v[1] == 0.f);
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
             const int key = 16 * a + 8 * hf + ((ln & 15) >> 1);          // the row that the lane points at, for the lanes of its 16
             const char *from = vt + key * D + (ln & 1) * 8;
+            u32x4_t va[NDB];                                 // channel 32 db + ln, keys 16 a + 8 hf .. + 7
 #pragma unroll
             for (int db = 0; db < NDB; ++db) {
-                const u32x2_t w = column8(from + ((2 * db + (ln >> 4)) ^ swz(key)) * 16);      // channel 32 db + ln, keys 16 a + 8 hf .. + 7
-                const u32x4_t va = {pair_of<CODE, false>(w.x), pair_of<CODE, true>(w.x), pair_of<CODE, false>(w.y), pair_of<CODE, true>(w.y)};
-#pragma unroll
-                for (int p = 0; p < NP; ++p) o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va), as_bf16x8(pop[a][p]), o_acc[db], 0, 0, 0);
+                const u32x2_t w = column8(from + ((2 * db + (ln >> 4)) ^ swz(key)) * 16);
+                va[db] = u32x4_t{pair_of<CODE, false>(w.x), pair_of<CODE, true>(w.x), pair_of<CODE, false>(w.y), pair_of<CODE, true>(w.y)};
             }
+            if (dirty) {
+#pragma unroll
+                for (int db = 0; db < NDB; ++db) va[db] = numbers_of_bf16(va[db]);
+            }
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va[db]), as_bf16x8(pop[a][p]), o_acc[db], 0, 0, 0);
         }
         if (i + 2 < mine) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // what lay in the slot has been read
-            stage(t + 2 * kWaves, i & 1);
+            stage(tile_row + 2 * kWaves * kKeys, i & 1);
         }
     }
 
@@ -536,30 +560,56 @@ struct Plan { int64_t piece_tiles, slots; };
 inline int64_t tiles_of(int64_t ctx_len) { return (ctx_len + kAlign - 1 + kKeys - 1) / kKeys; }    // wherever in a block it begins
 inline int64_t blocks_of(int64_t n_sel, int grp) { return (n_sel * grp + kRows - 1) / kRows; }
 
+// The piece with the least estimated time, of those whose slots the workspace holds.  Microseconds, measured: a workgroup
+// takes kTile for a tile with two workgroups a CU (0.6 of it alone), kStart besides, and all together read the caches at
+// kBytes a microsecond, row blocks of the same keys from L2; what is left over at the end is on average half a piece; the merge costs
+// its launch and its slots, written and read.
 Plan plan_pieces(const kvs_shape *shape, int32_t n_req, const int64_t *ctx_len, const int64_t *cu_sel, size_t workspace_bytes)
 {
+    constexpr double kPlaces = 512, kTile = 0.40, kStart = 4.0, kBytes = 4.9e6, kMerge = 4.0;
     const int grp = shape->n_q_heads / shape->n_kv_heads, hk = shape->n_kv_heads;
-    int64_t units = 0, tiles = 0;
+    const double tile_bytes = 2.0 * kKeys * shape->head_dim, tile_us = kTile * shape->head_dim / 128 * (shape->dtype == KVS_F32 ? 3 : 1);
+    double wgs1 = 0, load = 0, bytes = 0;
+    int64_t longest = 0, rows_at_most = 0;
     for (int32_t b = 0; b < n_req; ++b) {
-        const int64_t n = blocks_of(cu_sel[b + 1] - cu_sel[b], grp);
-        units += n * hk;
-        tiles += n * hk * tiles_of(ctx_len[b]);
+        const int64_t n = cu_sel[b + 1] - cu_sel[b];
+        if (n == 0) continue;
+        const double nb = (double)blocks_of(n, grp), tiles = (double)tiles_of(ctx_len[b]);
+        wgs1 += nb * hk;
+        load += (nb > 1 ? (nb + 1) / 2 : 1) * hk * tiles;            // rows spread over their context see half of it
+        bytes += hk * tiles * tile_bytes;
+        if (tiles_of(ctx_len[b]) > longest) longest = tiles_of(ctx_len[b]);
+        rows_at_most += n * shape->n_q_heads;
     }
-    if (units >= kSplitBelow) return {0, 0};
-    int64_t piece = (tiles + kTargetWgs - 1) / kTargetWgs;
-    if (piece < kMinPieceTiles) piece = kMinPieceTiles;
-    for (;; piece *= 2) {
-        piece = (piece + kWaves - 1) / kWaves * kWaves;
-        int64_t slots = 0, most = 1;
+    if (wgs1 > (double)kMaxCutWgs || longest <= kMinPieceTiles) return {0, 0};
+    Plan best = {0, 0};
+    double best_us = 1e30;
+    for (int64_t cuts = 1; cuts <= kMaxPieces; cuts += (cuts + 3) / 4) {
+        int64_t piece = ((longest + cuts - 1) / cuts + kWaves - 1) / kWaves * kWaves;
+        if (piece < kMinPieceTiles) piece = kMinPieceTiles;
+        int64_t slots = 0;
+        double wgs = 0;
         for (int32_t b = 0; b < n_req; ++b) {
             const int64_t n = cu_sel[b + 1] - cu_sel[b];
-            const int64_t p = n ? (tiles_of(ctx_len[b]) + piece - 1) / piece : 1;
+            if (n == 0) continue;
+            const int64_t p = (tiles_of(ctx_len[b]) + piece - 1) / piece;
             if (p > 1) slots += n * shape->n_q_heads * p;
-            if (p > most) most = p;
+            wgs += (double)(blocks_of(n, grp) * (p > 1 ? p : 1) * hk);
         }
-        if (most <= 1) return {0, 0};
-        if (most <= kMaxPieces && (size_t)slots * slot_bytes(shape->head_dim) <= workspace_bytes) return {piece, slots};
+        if (cuts > 1 && ((size_t)slots * slot_bytes(shape->head_dim) > workspace_bytes || wgs > (double)kMaxCutWgs)) break;
+        const double busy = wgs < kPlaces ? wgs : kPlaces;
+        const double each = tile_us * (wgs <= kPlaces / 2 ? 0.6 : 1.0);
+        const double shared = bytes / kBytes / (load / busy);          // what a tile takes if the caches' bytes bound the call
+        const double t = each > shared ? each : shared;
+        double us = wgs <= kPlaces ? (double)piece * t + kStart : load / kPlaces * t + kStart * wgs / kPlaces + 0.5 * (double)piece * t;
+        if (slots) us += kMerge + 2 * (double)slots * (double)slot_bytes(shape->head_dim) / kBytes;
+        if (us < best_us) {
+            best_us = us;
+            best = slots ? Plan{piece, slots} : Plan{0, 0};
+        }
+        if (piece == kMinPieceTiles) break;
     }
+    return best;
 }
 
 // ---- many rows a key: a bf16 copy --------------------------------------------------------------------------------
@@ -730,11 +780,11 @@ kvs_status launch(const kvs_shape *shape, const kvs_cache8 *c, const Table &td, 
 
 size_t attention8_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t n_rows_total, int64_t n_sel_total)
 {
-    // a launch that is cut has fewer than kSplitBelow units, and its pieces are at most kTargetWgs and one more a unit; 32 rows each
+    // a launch that is cut has at most kMaxCutWgs workgroups, of 32 rows each
     if (check_shape(shape) != KVS_OK || n_sel_total <= 0) return 256;
     int64_t pieces = tiles_of(n_rows_total) / kMinPieceTiles + 1;
     if (pieces > kMaxPieces) pieces = kMaxPieces;
-    const int64_t most = (int64_t)kRows * (kSplitBelow + kTargetWgs);
+    const int64_t most = (int64_t)kRows * kMaxCutWgs;
     int64_t slots = most;
     if (n_sel_total < most && n_sel_total * shape->n_q_heads < most) slots = n_sel_total * shape->n_q_heads * pieces < most ? n_sel_total * shape->n_q_heads * pieces : most;
     size_t bytes = ((size_t)slots * slot_bytes(shape->head_dim) + 255) / 256 * 256;
