@@ -72,18 +72,20 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t w)
     }
 }
 
-// Three bf16 that add up to an fp32 number (24 bits in three times 8), for eight numbers.
-__device__ __forceinline__ void split3(const float (&x)[8], u32x4_t (&part)[3])
+// PARTS bf16 that add up to eight fp32 numbers each: to 16 of their bits with two, to all 24 with three.
+template <int PARTS>
+__device__ __forceinline__ void split(const float (&x)[8], u32x4_t (&part)[PARTS])
 {
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = x[i];
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
+    for (int p = 0; p < PARTS; ++p) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             w[i] = pack2(y[2 * i], y[2 * i + 1]);
+            if (p == PARTS - 1) continue;
             y[2 * i] -= bf16_lo(w[i]);
             y[2 * i + 1] -= bf16_hi(w[i]);
         }
@@ -116,14 +118,16 @@ __device__ __forceinline__ u32x4_t numbers_of_bf16(u32x4_t v)
 
 typedef const __attribute__((address_space(4))) float *scalar_f32;    // read by all lanes at one address: scalar loads
 
-template <int DTYPE, int CODE, int D>
+// PARTS: bf16 numbers that a weight enters the second product as (bf16 only; fp32's are three)
+template <int DTYPE, int CODE, int D, int PARTS>
 __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     const Table td, int n_q_heads, int n_kv_heads, int64_t n_rows, int block_log2,
     const uint8_t *__restrict__ k_codes, const uint8_t *__restrict__ v_codes, const float *__restrict__ k_scale, const float *__restrict__ v_scale,
     const void *__restrict__ q_sel, const int32_t *__restrict__ sel_pos, float scale_log2,
     void *__restrict__ out, float *__restrict__ lse_out, float *__restrict__ part_o, float4 *__restrict__ part_ml)
 {
-    constexpr int NP = DTYPE == KVS_F32 ? 3 : 1;            // bf16 numbers that Q and the weights enter as
+    constexpr int NQ = DTYPE == KVS_F32 ? 3 : 1;            // bf16 numbers that Q enters as
+    constexpr int NP = DTYPE == KVS_F32 ? 3 : PARTS;        // ... and the weights
     constexpr int NDB = D / 32;                             // products of the second kind, channels a lane reads at once
     constexpr int CPR = D / 16;                             // 16-byte chunks of a row
     constexpr int RPL = kWave / CPR;                        // rows a load moves
@@ -169,7 +173,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     // scale's sign goes into Q, so that the largest score is the largest product's -------------------------------
     const bool negative = scale_log2 < 0.f;
     const float scale_abs = fabsf(scale_log2);
-    bf16x8 qreg[NP][D / 16];
+    bf16x8 qreg[NQ][D / 16];
     {
         const int64_t at = ((sel_lo + t_sel) * n_q_heads + g * grp + hh) * (int64_t)D + 16 * hf;
 #pragma unroll
@@ -184,9 +188,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = negative ? -x[j] : x[j];
                 u32x4_t part[3];
-                split3(x, part);
+                split(x, part);
 #pragma unroll
-                for (int p = 0; p < NP; ++p) qreg[p][ks] = as_bf16x8(part[p]);
+                for (int p = 0; p < NQ; ++p) qreg[p][ks] = as_bf16x8(part[p]);
             }
         }
     }
@@ -307,7 +311,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
             const u32x4_t lo = {pair_of<CODE, false>(w.x), pair_of<CODE, true>(w.x), pair_of<CODE, false>(w.y), pair_of<CODE, true>(w.y)};
             const u32x4_t hi = {pair_of<CODE, false>(w.z), pair_of<CODE, true>(w.z), pair_of<CODE, false>(w.w), pair_of<CODE, true>(w.w)};
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
+            for (int p = 0; p < NQ; ++p) {
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(lo), qreg[p][2 * c], s, 0, 0, 0);
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(hi), qreg[p][2 * c + 1], s, 0, 0, 0);
             }
@@ -369,7 +373,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
                 for (int j = 0; j < 8; ++j) y[j] = entry(8 * a + j) <= last && entry(8 * a + j) >= first ? y[j] : 0.f;
             }
             psum += group;
-            if constexpr (DTYPE == KVS_BF16) {
+            if constexpr (NP == 1) {
                 // The normaliser is made of the rounded weights: numerator and denominator then carry the same rounding, and a
                 // row that one key dominates returns that key's V to within the output's own rounding.
                 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -383,7 +387,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
                 // (scales below 2^-80 would bring weights below what bf16 holds)
                 rsum += sc.v[a] > 8.271806e-25f ? rounded * __builtin_amdgcn_rcpf(sc.v[a]) : group;
             } else {
-                split3(y, pop[a]);
+                split(y, pop[a]);
             }
         }
         l_run += psum;
@@ -413,7 +417,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     // ---- the waves meet --------------------------------------------------------------------------------------------
     {
         const float l = l_run + __shfl_xor(l_run, 32), lr = l_rnd + __shfl_xor(l_rnd, 32);
-        if (hf == 0) ml_s[wave][ln] = make_float4(m_run, l, DTYPE == KVS_BF16 ? lr : l, 0.f);
+        if (hf == 0) ml_s[wave][ln] = make_float4(m_run, l, NP == 1 ? lr : l, 0.f);
     }
     __syncthreads();
     {
@@ -666,9 +670,17 @@ Plan plan_pieces(const kvs_shape *shape, int32_t n_req, const int64_t *ctx_len, 
 // With hundreds of rows a key and KV head the matrix cores bound the call, and right behind them the vector instructions, and
 // above every wave widens all keys that it multiplies with: 96 instructions beside the 16 matrix products of a tile.  Such
 // launches widen the contexts once, into the workspace, and go to the bf16 kernel of 256 rows (attention_mfma2.hip).  K
-// goes there as its codes, which bf16 holds exactly, with factors of the scores for every 16 rows; V as code * scale,
-// rounded to bf16 as a cache in bf16 would hold it.
+// goes there as its codes and V as codes times the power of two below its scale, which bf16 holds exactly; for every 16 rows
+// and KV head there is a factor of the scores, and the rest of V's scale, in [1, 2), as a summand of the exponents, with its
+// inverse for the sums of weights (attn_mfma2_kernel's SCALED).
 constexpr int kCopyThreads = 256;
+
+// A normal number's significand, in [1, 2); 1 for all others.
+__device__ __forceinline__ float rest_of_scale(float s)
+{
+    const float a = fabsf(s);
+    return a >= kLeastScale && a < INFINITY ? __uint_as_float((__float_as_uint(s) & 0x7fffffu) | 0x3f800000u) : 1.f;
+}
 
 struct CopyRanges {
     int64_t row[kAttnMaxReq];              // first row of request b, a multiple of 16
@@ -680,7 +692,7 @@ template <int CODE>
 __global__ __launch_bounds__(kCopyThreads) void copy8_kernel(const CopyRanges cr, int n_kv_heads, int64_t n_rows, int64_t first_row, int64_t end_row, int block_log2,
                                                              const uint4 *__restrict__ k_codes, const uint4 *__restrict__ v_codes,
                                                              const float *__restrict__ k_scale, const float *__restrict__ v_scale, float scale_log2,
-                                                             uint4 *__restrict__ k_out, uint4 *__restrict__ v_out, float *__restrict__ factors)
+                                                             uint4 *__restrict__ k_out, uint4 *__restrict__ v_out, float4 *__restrict__ factors)
 {
     constexpr int kChunks = 128 / 16;
     const int b = request_of(cr.begin, cr.n_req, (int)blockIdx.x);
@@ -690,13 +702,15 @@ __global__ __launch_bounds__(kCopyThreads) void copy8_kernel(const CopyRanges cr
     for (int g = threadIdx.x; g < n_kv_heads; g += kCopyThreads) {
         // (positive and finite, whatever the scale: a block that stands for zeros has codes of 0, a broken one NaN in K)
         const float f = k_scale[scales + g] * scale_log2;
-        factors[((row0 - first_row) / kAlign) * n_kv_heads + g] = f >= 7.888609e-31f && f < INFINITY ? f : 7.888609e-31f;
+        const float m = rest_of_scale(v_scale[scales + g]);
+        factors[((row0 - first_row) / kAlign) * n_kv_heads + g] = make_float4(f >= 7.888609e-31f && f < INFINITY ? f : 7.888609e-31f, __log2f(m), 1.f / m, 0.f);
     }
     const int per_row = n_kv_heads * kChunks;
     for (int e = threadIdx.x; e < rows * per_row; e += kCopyThreads) {
         const int c = e % per_row;
         const int64_t from = row0 * per_row + e, to = ((row0 - first_row) * per_row + e) * 2;
         const float ks = k_scale[scales + c / kChunks], vs = v_scale[scales + c / kChunks];
+        const float v_by = rest_of_scale(vs) == 1.f ? vs : __uint_as_float(__float_as_uint(vs) & 0xff800000u);
         const uint4 k = stream_load16(k_codes + from), v = stream_load16(v_codes + from);
         const bool broken = !(fabsf(ks) < INFINITY) || !(fabsf(vs) < INFINITY);
         const uint32_t kw[4] = {k.x, k.y, k.z, k.w}, vw[4] = {v.x, v.y, v.z, v.w};
@@ -708,8 +722,8 @@ __global__ __launch_bounds__(kCopyThreads) void copy8_kernel(const CopyRanges cr
             ko[2 * i + 1] = broken ? 0x7fc07fc0u : ks > 0.f ? pair_of<CODE, true>(kc) : 0u;
             float x[4];
             widen_codes<CODE>(vc, x);
-            vo[2 * i] = broken ? 0u : pack2(x[0] * vs, x[1] * vs);
-            vo[2 * i + 1] = broken ? 0u : pack2(x[2] * vs, x[3] * vs);
+            vo[2 * i] = broken ? 0u : pack2(x[0] * v_by, x[1] * v_by);
+            vo[2 * i + 1] = broken ? 0u : pack2(x[2] * v_by, x[3] * v_by);
         }
         k_out[to] = make_uint4(ko[0], ko[1], ko[2], ko[3]);
         k_out[to + 1] = make_uint4(ko[4], ko[5], ko[6], ko[7]);
@@ -734,7 +748,7 @@ constexpr int64_t kCopyPad = 8;            // factors behind the last row's: wha
 inline size_t copy_bytes(const kvs_shape *shape, int64_t rows)
 {
     const int64_t groups = (rows + kAlign - 1) / kAlign;
-    return (size_t)(groups * kAlign * shape->n_kv_heads * 128 * 4 + (groups + kCopyPad) * shape->n_kv_heads * 4 + 512);
+    return (size_t)(groups * kAlign * shape->n_kv_heads * 128 * 4 + (groups + kCopyPad) * shape->n_kv_heads * (int64_t)sizeof(float4) + 512);
 }
 
 // Whether a copy for the bf16 kernel is worth its bytes.  Measured, of what rows in the middle of their contexts take: the kernel above
@@ -794,7 +808,7 @@ kvs_status launch_from_copy(const kvs_shape *shape, const kvs_cache8 *c, int32_t
     const int64_t rows = (hi - lo + kAlign - 1) / kAlign * kAlign;
     char *at = (char *)workspace + left;
     uint4 *k_copy = (uint4 *)at, *v_copy = (uint4 *)(at + rows * shape->n_kv_heads * 256);
-    float *factors = (float *)(at + rows * shape->n_kv_heads * 512);
+    float4 *factors = (float4 *)(at + rows * shape->n_kv_heads * 512);
     const float scale_log2 = scale * 1.4426950408889634f;
     const dim3 grid((unsigned)groups), threads(kCopyThreads);
 #define KVS_COPY(C) hipLaunchKernelGGL((copy8_kernel<C>), grid, threads, 0, hs, cr, shape->n_kv_heads, c->n_rows, lo, lo + rows, __builtin_ctz((unsigned)c->block), \
@@ -811,18 +825,18 @@ kvs_status launch_from_copy(const kvs_shape *shape, const kvs_cache8 *c, int32_t
     return check_launch("kvs_attention_kv8(rows)");
 }
 
-template <int DTYPE, int CODE, int D>
+template <int DTYPE, int CODE, int D, int PARTS>
 kvs_status launch(const kvs_shape *shape, const kvs_cache8 *c, const Table &td, int64_t wgs, const void *q_sel, const int32_t *sel_pos, float scale,
                   void *out, float *lse_out, float *part_o, float4 *part_ml, hipStream_t hs)
 {
     static DeviceOnce once;
     constexpr int lds = kWaves * 4 * kKeys * D;
     const kvs_status st = once_per_device(once, [&]() -> kvs_status {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention8_kernel<DTYPE, CODE, D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention8_kernel<DTYPE, CODE, D, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_attention_kv8: %s", hipGetErrorString(e));
     });
     if (st != KVS_OK) return st;
-    hipLaunchKernelGGL((attention8_kernel<DTYPE, CODE, D>), dim3((unsigned)wgs), dim3(kThreads), lds, hs, td, shape->n_q_heads, shape->n_kv_heads, c->n_rows,
+    hipLaunchKernelGGL((attention8_kernel<DTYPE, CODE, D, PARTS>), dim3((unsigned)wgs), dim3(kThreads), lds, hs, td, shape->n_q_heads, shape->n_kv_heads, c->n_rows,
                        __builtin_ctz((unsigned)c->block), (const uint8_t *)c->k, (const uint8_t *)c->v, c->k_scale, c->v_scale, q_sel, sel_pos,
                        scale * 1.4426950408889634f, out, lse_out, part_o, part_ml);
     return check_launch("kvs_attention_kv8");
@@ -923,10 +937,17 @@ extern "C" kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8
         float4 *ml = reinterpret_cast<float4 *>(workspace);
         float *po = reinterpret_cast<float *>(ml + plan.slots);
         const int64_t wgs = units * shape->n_kv_heads, items = n_sel * shape->n_q_heads;
+        // Weights of launches that the caches' bytes bound enter the second product as two bf16, which costs up to 4% there (131072
+        // keys 35.3 -> 36.7 us, 64 of 4096 to 16384 the same); with several blocks a request it would be 8 to 11%.
+        bool one_block = true;
+        for (int i = 0; i < nr; ++i) one_block = one_block && blocks_of(cu_sel[b0 + i + 1] - cu_sel[b0 + i], grp) <= 1;
         const bool e4m3 = cache->code == KVS_E4M3, wide = shape->head_dim == 128, bf16 = shape->dtype == KVS_BF16;
-#define KVS_A8(DT, C, DD) launch<DT, C, DD>(shape, cache, td, wgs, q_sel, sel_pos, scale, out, lse_out, po, ml, hs)
-        if (bf16) st = e4m3 ? (wide ? KVS_A8(KVS_BF16, KVS_E4M3, 128) : KVS_A8(KVS_BF16, KVS_E4M3, 64)) : (wide ? KVS_A8(KVS_BF16, KVS_INT8, 128) : KVS_A8(KVS_BF16, KVS_INT8, 64));
-        else st = e4m3 ? (wide ? KVS_A8(KVS_F32, KVS_E4M3, 128) : KVS_A8(KVS_F32, KVS_E4M3, 64)) : (wide ? KVS_A8(KVS_F32, KVS_INT8, 128) : KVS_A8(KVS_F32, KVS_INT8, 64));
+#define KVS_A8(DT, C, DD, PP) launch<DT, C, DD, PP>(shape, cache, td, wgs, q_sel, sel_pos, scale, out, lse_out, po, ml, hs)
+#define KVS_A8_OF(DT, PP) (e4m3 ? (wide ? KVS_A8(DT, KVS_E4M3, 128, PP) : KVS_A8(DT, KVS_E4M3, 64, PP)) : (wide ? KVS_A8(DT, KVS_INT8, 128, PP) : KVS_A8(DT, KVS_INT8, 64, PP)))
+        if (!bf16) st = KVS_A8_OF(KVS_F32, 3);
+        else if (one_block) st = KVS_A8_OF(KVS_BF16, 2);
+        else st = KVS_A8_OF(KVS_BF16, 1);
+#undef KVS_A8_OF
 #undef KVS_A8
         if (st != KVS_OK) return st;
         if (!plan.piece_tiles) continue;

@@ -242,7 +242,9 @@ __device__ __forceinline__ void plan_shares(const AttnTiles &td, int grp, int to
 // RECENTRE: the softmax reference is not fixed for the sweep; see recentre below, and AttnSplitPlan for when.
 // QUEUE: the workgroup draws its tiles; see attn_queue_kernel.
 // SCALED: K holds codes, whose scores are multiplied by a factor for each 16 keys and KV head (key_scale, all positive and finite; the
-// contexts begin at multiples of 16 rows); scale_log2 is not read.  Two scalar loads a step, a step ahead.
+// contexts begin at multiples of 16 rows); scale_log2 is not read.  V holds codes times powers of two, and the rest of its scale, 1 to 2,
+// goes into the weights through a summand of their exponents; their sums, of the weights without it, are made of the rounded
+// weights times its inverse.  Two scalar loads a step, a step ahead.
 template <bool WANT_LSE, bool SPLIT, bool RECENTRE, bool QUEUE, bool SCALED>
 __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     const AttnTiles td, int n_q_heads, int n_kv_heads, int total_tiles,
@@ -250,7 +252,7 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache,
     float scale_log2, uint16_t *__restrict__ out, float *__restrict__ lse_out,
     int n_splits, const int4 *__restrict__ split_plan, const uint16_t *__restrict__ piece_list,
-    float *__restrict__ part_o, float4 *__restrict__ part_ml, int share_units, int32_t *__restrict__ queue, const float *__restrict__ key_scale)
+    float *__restrict__ part_o, float4 *__restrict__ part_ml, int share_units, int32_t *__restrict__ queue, const float4 *__restrict__ key_scale)
 {
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];   // K ring, then V^T ring
     __shared__ int wg_max_pos[NWAVES];
@@ -512,15 +514,21 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
                 }
         }
     };
-    // What a score of tile jt is multiplied with: one number, or one for each half of the tile's keys.
-    struct Factors { float half[SCALED ? 2 : 1]; };
+    // What a score of tile jt is multiplied with: one number, or one for each half of the tile's keys, where the exponent has a
+    // summand too, which the weights' sums do not see.
+    struct Factors { float half[SCALED ? 2 : 1], add[SCALED ? 2 : 1], inv[SCALED ? 2 : 1]; };
     typedef const __attribute__((address_space(4))) float *scalar_f32;
-    const scalar_f32 factor_at = (scalar_f32)(uintptr_t)(SCALED ? key_scale + (ctx_off >> 4) * n_kv_heads + g : nullptr);
+    const scalar_f32 factor_at = (scalar_f32)(uintptr_t)(SCALED ? key_scale + (ctx_off >> 4) * n_kv_heads + g : nullptr);      // float4 {half, add, inv, -}
     auto factors = [&](int jt) -> Factors {
         Factors f;
         if constexpr (SCALED) {
-            f.half[0] = factor_at[2 * jt * n_kv_heads];
-            f.half[1] = factor_at[(2 * jt + 1) * n_kv_heads];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const scalar_f32 at = factor_at + 4 * (int64_t)(2 * jt + a) * n_kv_heads;
+                f.half[a] = at[0];
+                f.add[a] = at[1];
+                f.inv[a] = at[2];
+            }
         } else {
             f.half[0] = scale_log2;
         }
@@ -550,16 +558,21 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     // the whole pass, so the output accumulators are touched by MFMAs only and can stay in the
     // accumulation registers; see the comment at the pass loop for why that is safe.
     auto softmax4 = [&](const floatx16 &s, const Factors &f, int nb, int r0, u32x4_t (&pop)[2]) {
-        const float by = f.half[SCALED ? r0 >> 3 : 0];
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 0], by, -m_ref[nb]));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 1], by, -m_ref[nb]));
-        const float e2 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 2], by, -m_ref[nb]));
-        const float e3 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 3], by, -m_ref[nb]));
+        const float by = f.half[SCALED ? r0 >> 3 : 0], add = SCALED ? f.add[r0 >> 3] - m_ref[nb] : -m_ref[nb];
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 0], by, add));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 1], by, add));
+        const float e2 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 2], by, add));
+        const float e3 = __builtin_amdgcn_exp2f(fmaf(s[r0 + 3], by, add));
         const uint32_t w0 = pack2(e0, e1), w1 = pack2(e2, e3);
         pop[r0 >> 3][(r0 & 7) >> 1] = w0;
         pop[r0 >> 3][((r0 & 7) >> 1) + 1] = w1;
+        if constexpr (SCALED) {
+            l_run[nb] = fmaf(add_rounded_pair(w1, add_rounded_pair(w0, 0.f)), f.inv[r0 >> 3], l_run[nb]);
+            if (WANT_LSE) l_exact[nb] = fmaf((e0 + e1) + (e2 + e3), f.inv[r0 >> 3], l_exact[nb]);
+        } else {
         l_run[nb] = add_rounded_pair(w1, add_rounded_pair(w0, l_run[nb]));
         if (WANT_LSE) l_exact[nb] += (e0 + e1) + (e2 + e3);
+        }
     };
     auto softmax = [&](int jt, floatx16 (&s)[NB], u32x4_t (&pop)[NB][2]) {
         mask_tile(jt, s);
@@ -666,7 +679,7 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
             if (FIRST == 0) s_out[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ka), qreg[0][i], i == 0 ? zero : s_out[0], 0, 0, 0);
             float x[PER], e[PER];
 #pragma unroll
-            for (int u = 0; u < PER; ++u) x[u] = fmaf(s_in[nbs][r0 + u], f.half[SCALED ? r0 >> 3 : 0], -m_ref[nbs]);
+            for (int u = 0; u < PER; ++u) x[u] = fmaf(s_in[nbs][r0 + u], f.half[SCALED ? r0 >> 3 : 0], SCALED ? f.add[r0 >> 3] - m_ref[nbs] : -m_ref[nbs]);
             if (MASKED >> nbs & 1) {   // entry r of the lane is key jt*BN + 16*(r>>3) + 8*hf + (r&7)
                 const int k0 = jt * BN + 16 * (r0 >> 3) + (r0 & 7);
 #pragma unroll
@@ -678,9 +691,17 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
             if (FIRST == 0) o_acc[db][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va), as_bf16x8(p_in[0][a]), o_acc[db][0], 0, 0, 0);
 #pragma unroll
             for (int u = 0; u < PER; u += 2) p_out[nbs][r0 >> 3][((r0 & 7) + u) >> 1] = pack2(e[u], e[u + 1]);
+            if constexpr (SCALED) {
+                float sum = 0.f;
+#pragma unroll
+                for (int u = 0; u < PER; u += 2) sum = add_rounded_pair(p_out[nbs][r0 >> 3][((r0 & 7) + u) >> 1], sum);
+                l_run[nbs] = fmaf(sum, f.inv[r0 >> 3], l_run[nbs]);
+                if (WANT_LSE) l_exact[nbs] = fmaf(FIRST == 0 ? (e[0] + e[1]) + (e[PER - 2] + e[PER - 1]) : e[0] + e[1], f.inv[r0 >> 3], l_exact[nbs]);
+            } else {
 #pragma unroll
             for (int u = 0; u < PER; u += 2) l_run[nbs] = add_rounded_pair(p_out[nbs][r0 >> 3][((r0 & 7) + u) >> 1], l_run[nbs]);
             if (WANT_LSE) l_exact[nbs] += FIRST == 0 ? (e[0] + e[1]) + (e[PER - 2] + e[PER - 1]) : e[0] + e[1];
+            }
             o_acc[db][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va), as_bf16x8(p_in[1][a]), o_acc[db][1], 0, 0, 0);
             ka = ka_n;
             va = va_n;
@@ -1124,7 +1145,7 @@ template <bool WANT_LSE, bool SPLIT, bool RECENTRE, bool QUEUE, bool SCALED>
 kvs_status launch_one(const dim3 grid, size_t lds_bytes, hipStream_t st, const AttnTiles &td, const kvs_shape *shape,
                       int tiles, const void *q_sel, const int32_t *sel_pos, const void *k_cache, const void *v_cache,
                       float scale_log2, void *out, float *lse_out, int n_splits, const int4 *split_plan,
-                      const uint16_t *piece_list, float *part_o, float4 *part_ml, int share_units, int32_t *queue, const float *key_scale)
+                      const uint16_t *piece_list, float *part_o, float4 *part_ml, int share_units, int32_t *queue, const float4 *key_scale)
 {
     static DeviceOnce attr_once;
     const kvs_status ast = once_per_device(attr_once, [lds_bytes] {
@@ -1196,7 +1217,7 @@ template <bool SCALED>
 kvs_status launch_large(const kvs_shape *shape, const AttnBatch &bd, const void *q_sel,
                         const int32_t *sel_pos, const void *k_cache, const void *v_cache,
                         float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
-                        const AttnSplitPlan &plan, const float *key_scale, hipStream_t st)
+                        const AttnSplitPlan &plan, const float4 *key_scale, hipStream_t st)
 {
     AttnTiles td;
     const int64_t tiles = build_attn_tiles(shape, bd, ROWS, td);
@@ -1278,7 +1299,7 @@ kvs_status launch_large(const kvs_shape *shape, const AttnBatch &bd, const void 
 kvs_status launch_attention_mfma2(const kvs_shape *shape, const AttnBatch &bd, const void *q_sel,
                                   const int32_t *sel_pos, const void *k_cache, const void *v_cache,
                                   float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
-                                  const AttnSplitPlan &plan, hipStream_t st, const float *key_scale)
+                                  const AttnSplitPlan &plan, hipStream_t st, const float4 *key_scale)
 {
     return key_scale ? launch_large<true>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, key_scale, st)
                      : launch_large<false>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, nullptr, st);
