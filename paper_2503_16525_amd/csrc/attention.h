@@ -115,15 +115,20 @@ constexpr int kAttnPlanMaxTiles = 2048;    // row tiles a planned launch may hav
 // the pieces in the workspace
 constexpr size_t kAttnPlanBytes = 16 + 2 * (size_t)kAttnSplitMax * kAttnPlanMaxTiles;
 static_assert(kAttnSplitMax * kAttnPlanMaxTiles <= 65536, "piece ids are 16 bits");
+// A cache that was held in 8 bits (attention8.hip), whose K is codes and whose V is codes times powers of two: for every 16 rows of a
+// KV head (g * stride + row / 16) the factor of their scores, times scale * log2 e; what their exponents are raised by, 0 to 1
+// (the part of a weight that V does not hold); its power of two's inverse; nothing.
+struct KeyFactors {
+    const float4 *at;
+    int64_t stride;
+};
 // 64 query rows per wave (two MFMAs per LDS operand), one wave per SIMD, 256-row tiles.  The plan
-// comes from attention_mfma2_plan, which needs the workspace size.  key_scale: a cache that was held in 8 bits (attention8.hip):
-// float4[rows / 16, n_kv_heads], and in each the factor of the scores of 16 rows, times scale * log2 e; what their exponents are
-// raised by, 0 to 1 (the part of a weight that V does not hold); its power of two's inverse; nothing.
+// comes from attention_mfma2_plan, which needs the workspace size.
 AttnSplitPlan attention_mfma2_plan(const kvs_shape *shape, const AttnBatch &bd, size_t workspace_bytes);
 kvs_status launch_attention_mfma2(const kvs_shape *shape, const AttnBatch &bd, const void *q_sel,
                                   const int32_t *sel_pos, const void *k_cache, const void *v_cache,
                                   float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
-                                  const AttnSplitPlan &plan, hipStream_t st, const float4 *key_scale = nullptr);
+                                  const AttnSplitPlan &plan, hipStream_t st, const KeyFactors &key_scale = {nullptr, 0});
 // Whether a launch goes to that kernel, and then how.
 bool attention_takes_large(const kvs_shape *shape, const AttnBatch &bd, size_t workspace_bytes, AttnSplitPlan *plan);
 

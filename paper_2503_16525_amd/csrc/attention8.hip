@@ -692,7 +692,7 @@ template <int CODE>
 __global__ __launch_bounds__(kCopyThreads) void copy8_kernel(const CopyRanges cr, int n_kv_heads, int64_t n_rows, int64_t first_row, int64_t end_row, int block_log2,
                                                              const uint4 *__restrict__ k_codes, const uint4 *__restrict__ v_codes,
                                                              const float *__restrict__ k_scale, const float *__restrict__ v_scale, float scale_log2,
-                                                             uint4 *__restrict__ k_out, uint4 *__restrict__ v_out, float4 *__restrict__ factors)
+                                                             uint4 *__restrict__ k_out, uint4 *__restrict__ v_out, float4 *__restrict__ factors, int64_t factor_stride)
 {
     constexpr int kChunks = 128 / 16;
     const int b = request_of(cr.begin, cr.n_req, (int)blockIdx.x);
@@ -703,7 +703,7 @@ __global__ __launch_bounds__(kCopyThreads) void copy8_kernel(const CopyRanges cr
         // (positive and finite, whatever the scale: a block that stands for zeros has codes of 0, a broken one NaN in K)
         const float f = k_scale[scales + g] * scale_log2;
         const float m = rest_of_scale(v_scale[scales + g]);
-        factors[((row0 - first_row) / kAlign) * n_kv_heads + g] = make_float4(f >= 7.888609e-31f && f < INFINITY ? f : 7.888609e-31f, __log2f(m), 1.f / m, 0.f);
+        factors[g * factor_stride + (row0 - first_row) / kAlign] = make_float4(f >= 7.888609e-31f && f < INFINITY ? f : 7.888609e-31f, __log2f(m), 1.f / m, 0.f);
     }
     const int per_row = n_kv_heads * kChunks;
     for (int e = threadIdx.x; e < rows * per_row; e += kCopyThreads) {
@@ -809,15 +809,16 @@ kvs_status launch_from_copy(const kvs_shape *shape, const kvs_cache8 *c, int32_t
     char *at = (char *)workspace + left;
     uint4 *k_copy = (uint4 *)at, *v_copy = (uint4 *)(at + rows * shape->n_kv_heads * 256);
     float4 *factors = (float4 *)(at + rows * shape->n_kv_heads * 512);
+    const int64_t stride = rows / kAlign + kCopyPad;
     const float scale_log2 = scale * 1.4426950408889634f;
     const dim3 grid((unsigned)groups), threads(kCopyThreads);
 #define KVS_COPY(C) hipLaunchKernelGGL((copy8_kernel<C>), grid, threads, 0, hs, cr, shape->n_kv_heads, c->n_rows, lo, lo + rows, __builtin_ctz((unsigned)c->block), \
-                                       (const uint4 *)c->k, (const uint4 *)c->v, c->k_scale, c->v_scale, scale_log2, k_copy, v_copy, factors)
+                                       (const uint4 *)c->k, (const uint4 *)c->v, c->k_scale, c->v_scale, scale_log2, k_copy, v_copy, factors, stride)
     if (c->code == KVS_E4M3) KVS_COPY(KVS_E4M3); else KVS_COPY(KVS_INT8);
 #undef KVS_COPY
     kvs_status st = check_launch("kvs_attention_kv8(copy)");
     if (st != KVS_OK) return st;
-    st = launch_attention_mfma2(shape, bd, q_sel, sel_pos, k_copy, v_copy, scale, out, lse_out, left ? workspace : nullptr, left, plan, hs, factors);
+    st = launch_attention_mfma2(shape, bd, q_sel, sel_pos, k_copy, v_copy, scale, out, lse_out, left ? workspace : nullptr, left, plan, hs, {factors, stride});
     if (st != KVS_OK) return st;
     const int64_t n_sel = cu_sel[n_req] - cu_sel[0];
     hipLaunchKernelGGL(empty_rows_kernel, dim3((unsigned)((n_sel + kWaves - 1) / kWaves)), dim3(kThreads), 0, hs, n_sel, shape->n_q_heads, sel_pos + cu_sel[0],

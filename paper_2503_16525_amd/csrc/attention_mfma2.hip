@@ -252,7 +252,7 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache,
     float scale_log2, uint16_t *__restrict__ out, float *__restrict__ lse_out,
     int n_splits, const int4 *__restrict__ split_plan, const uint16_t *__restrict__ piece_list,
-    float *__restrict__ part_o, float4 *__restrict__ part_ml, int share_units, int32_t *__restrict__ queue, const float4 *__restrict__ key_scale)
+    float *__restrict__ part_o, float4 *__restrict__ part_ml, int share_units, int32_t *__restrict__ queue, const KeyFactors key_scale)
 {
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];   // K ring, then V^T ring
     __shared__ int wg_max_pos[NWAVES];
@@ -518,13 +518,13 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     // summand too, which the weights' sums do not see.
     struct Factors { float half[SCALED ? 2 : 1], add[SCALED ? 2 : 1], inv[SCALED ? 2 : 1]; };
     typedef const __attribute__((address_space(4))) float *scalar_f32;
-    const scalar_f32 factor_at = (scalar_f32)(uintptr_t)(SCALED ? key_scale + (ctx_off >> 4) * n_kv_heads + g : nullptr);      // float4 {half, add, inv, -}
+    const scalar_f32 factor_at = (scalar_f32)(uintptr_t)(SCALED ? key_scale.at + g * key_scale.stride + (ctx_off >> 4) : nullptr);      // float4 {half, add, inv, -}
     auto factors = [&](int jt) -> Factors {
         Factors f;
         if constexpr (SCALED) {
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
-                const scalar_f32 at = factor_at + 4 * (int64_t)(2 * jt + a) * n_kv_heads;
+                const scalar_f32 at = factor_at + 4 * (2 * jt + a);
                 f.half[a] = at[0];
                 f.add[a] = at[1];
                 f.inv[a] = at[2];
@@ -661,6 +661,7 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
         const Factors f = SCALED ? f_next : factors(jt);
         if (SCALED) f_next = factors(jt + 1);
         const uint32_t ks = k_slot(jt + 1), vs = v_slot(jt - 1), ks_next = k_slot(jt + 2), vs_next = v_slot(jt);
+        float half_run = 0.f, half_exact = 0.f;   // SCALED: the sums of the half's weights so far
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             // source order of the slice: next slice's LDS operands, then one MFMA at a time, each
@@ -692,11 +693,14 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
 #pragma unroll
             for (int u = 0; u < PER; u += 2) p_out[nbs][r0 >> 3][((r0 & 7) + u) >> 1] = pack2(e[u], e[u + 1]);
             if constexpr (SCALED) {
-                float sum = 0.f;
+                if ((r0 & 7) == 0) half_run = half_exact = 0.f;
 #pragma unroll
-                for (int u = 0; u < PER; u += 2) sum = add_rounded_pair(p_out[nbs][r0 >> 3][((r0 & 7) + u) >> 1], sum);
-                l_run[nbs] = fmaf(sum, f.inv[r0 >> 3], l_run[nbs]);
-                if (WANT_LSE) l_exact[nbs] = fmaf(FIRST == 0 ? (e[0] + e[1]) + (e[PER - 2] + e[PER - 1]) : e[0] + e[1], f.inv[r0 >> 3], l_exact[nbs]);
+                for (int u = 0; u < PER; u += 2) half_run = add_rounded_pair(p_out[nbs][r0 >> 3][((r0 & 7) + u) >> 1], half_run);
+                if (WANT_LSE) half_exact += FIRST == 0 ? (e[0] + e[1]) + (e[PER - 2] + e[PER - 1]) : e[0] + e[1];
+                if ((r0 & 7) + PER == 8) {
+                    l_run[nbs] = fmaf(half_run, f.inv[r0 >> 3], l_run[nbs]);
+                    if (WANT_LSE) l_exact[nbs] = fmaf(half_exact, f.inv[r0 >> 3], l_exact[nbs]);
+                }
             } else {
 #pragma unroll
             for (int u = 0; u < PER; u += 2) l_run[nbs] = add_rounded_pair(p_out[nbs][r0 >> 3][((r0 & 7) + u) >> 1], l_run[nbs]);
@@ -1145,7 +1149,7 @@ template <bool WANT_LSE, bool SPLIT, bool RECENTRE, bool QUEUE, bool SCALED>
 kvs_status launch_one(const dim3 grid, size_t lds_bytes, hipStream_t st, const AttnTiles &td, const kvs_shape *shape,
                       int tiles, const void *q_sel, const int32_t *sel_pos, const void *k_cache, const void *v_cache,
                       float scale_log2, void *out, float *lse_out, int n_splits, const int4 *split_plan,
-                      const uint16_t *piece_list, float *part_o, float4 *part_ml, int share_units, int32_t *queue, const float4 *key_scale)
+                      const uint16_t *piece_list, float *part_o, float4 *part_ml, int share_units, int32_t *queue, const KeyFactors &key_scale)
 {
     static DeviceOnce attr_once;
     const kvs_status ast = once_per_device(attr_once, [lds_bytes] {
@@ -1217,7 +1221,7 @@ template <bool SCALED>
 kvs_status launch_large(const kvs_shape *shape, const AttnBatch &bd, const void *q_sel,
                         const int32_t *sel_pos, const void *k_cache, const void *v_cache,
                         float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
-                        const AttnSplitPlan &plan, const float4 *key_scale, hipStream_t st)
+                        const AttnSplitPlan &plan, const KeyFactors &key_scale, hipStream_t st)
 {
     AttnTiles td;
     const int64_t tiles = build_attn_tiles(shape, bd, ROWS, td);
@@ -1299,10 +1303,10 @@ kvs_status launch_large(const kvs_shape *shape, const AttnBatch &bd, const void 
 kvs_status launch_attention_mfma2(const kvs_shape *shape, const AttnBatch &bd, const void *q_sel,
                                   const int32_t *sel_pos, const void *k_cache, const void *v_cache,
                                   float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes,
-                                  const AttnSplitPlan &plan, hipStream_t st, const float4 *key_scale)
+                                  const AttnSplitPlan &plan, hipStream_t st, const KeyFactors &key_scale)
 {
-    return key_scale ? launch_large<true>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, key_scale, st)
-                     : launch_large<false>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, nullptr, st);
+    return key_scale.at ? launch_large<true>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, key_scale, st)
+                        : launch_large<false>(shape, bd, q_sel, sel_pos, k_cache, v_cache, scale, out, lse_out, workspace, workspace_bytes, plan, key_scale, st);
 }
 
 } // namespace kvs
