@@ -333,8 +333,14 @@ def _rows_at(t: Optional[torch.Tensor], dev: int, dtype: torch.dtype, n: int, he
 _TYPES = {F32: torch.float32, BF16: torch.bfloat16}
 
 
+def _type(shape: Shape) -> torch.dtype:
+    if shape.dtype not in _TYPES:
+        raise ValueError(f"unknown dtype {shape.dtype}")
+    return _TYPES[shape.dtype]
+
+
 def kvs_rotary(shape: Shape, spec: RotarySpec, pos, pos_from, q, k, q_out, k_out, stream=None) -> None:
-    n, dev, dt, d = pos.numel(), _device(), _TYPES[shape.dtype], shape.head_dim
+    n, dev, dt, d = pos.numel(), _device(), _type(shape), shape.head_dim
     qp, qs = _rows_at(q, dev, dt, n, shape.n_q_heads, d, "q")
     qo, qos = _rows_at(q_out, dev, dt, n, shape.n_q_heads, d, "q_out")
     kp, ks = _rows_at(k, dev, dt, n, shape.n_kv_heads, d, "k")
@@ -370,6 +376,8 @@ class Cache8:
     @classmethod
     def empty(cls, shape: Shape, n_rows: int, block: int, code: int = E4M3, device="cuda") -> "Cache8":
         """A cache of n_rows rows that holds nothing."""
+        if block <= 0:
+            raise ValueError("a block holds 16, 32, 64 or 128 tokens")
         dt = torch.float8_e4m3fn if code == E4M3 else torch.int8
         k, v = (torch.zeros((n_rows, shape.n_kv_heads, shape.head_dim), dtype=torch.uint8, device=device).view(dt) for _ in range(2))
         ks, vs = (torch.zeros((-(-n_rows // block), shape.n_kv_heads), device=device) for _ in range(2))
@@ -385,7 +393,7 @@ def _cache8(cache: Cache8, shape: Shape, dev: int) -> _Cache8:
 
 
 def kvs_store_kv8(shape: Shape, cache: Cache8, k_new, v_new, sel_pos, row0: int = 0, reused=None, dev_v=None, stream=None) -> None:
-    n, dev, dt = k_new.shape[0], _device(), _TYPES[shape.dtype]
+    n, dev, dt = k_new.shape[0], _device(), _type(shape)
     cells = n * shape.n_kv_heads * shape.head_dim
     rc = load().kvs_store_kv8(shape, _cache8(cache, shape, dev), _at(k_new, dev, dt, cells, "k_new"), _at(v_new, dev, dt, cells, "v_new"),
                               _at(sel_pos, dev, torch.int32, n, "sel_pos"), row0, n, _at(reused, dev, torch.uint8, cache.n_rows, "reused"),
@@ -396,7 +404,7 @@ def kvs_store_kv8(shape: Shape, cache: Cache8, k_new, v_new, sel_pos, row0: int 
 
 def kvs_deviation_kv8(shape: Shape, cache: Cache8, row0: int, n_tokens: int, k_fresh, v_fresh, reused, alpha, mode: int,
                       dev_k, dev_v, score, stream=None) -> None:
-    dev, dt, f32 = _device(), _TYPES[shape.dtype], torch.float32
+    dev, dt, f32 = _device(), _type(shape), torch.float32
     heads = n_tokens * shape.n_kv_heads
     cells = heads * shape.head_dim
     rc = load().kvs_deviation_kv8(shape, _cache8(cache, shape, dev), row0, n_tokens, _at(k_fresh, dev, dt, cells, "k_fresh"),
@@ -412,7 +420,7 @@ def kvs_attention_kv8(shape: Shape, cache: Cache8, ctx_off: Sequence[int], ctx_l
     co, cl, cs = _i64(ctx_off), _i64(ctx_len), _i64(cu_sel)
     if co.n != cl.n or cs.n != co.n + 1:
         raise ValueError("ctx_off/ctx_len need one entry per request and cu_sel one more")
-    n, dev, dt = int(cs.data[-1]), _device(), _TYPES[shape.dtype]
+    n, dev, dt = int(cs.data[-1]), _device(), _type(shape)
     heads = n * shape.n_q_heads
     cells = heads * shape.head_dim
     ws, ws_bytes = None, 0

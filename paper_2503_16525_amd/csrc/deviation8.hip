@@ -142,7 +142,7 @@ kvs_status launch(const DevArgs &a, bool has_k, hipStream_t hs)
     const bool few = a.n_tokens < kFewBelow;
     const int tok = few ? kTokFew : kTok;
     const int64_t wgs = (a.n_tokens + tok - 1) / tok;
-    if (wgs > 0x7fffffff) return fail(KVS_EINVAL, "kvs_deviation_kv8: too many tokens");
+    if (wgs > kMostWgs) return fail(KVS_EUNSUPPORTED, "kvs_deviation_kv8: %lld tokens in one call", (long long)a.n_tokens);
     const size_t lds = sizeof(float) * a.n_kv_heads * tok * 2;
 #define KVS_DEV8(HASK, TOK) hipLaunchKernelGGL((deviation8_kernel<DTYPE, CODE, D, HASK, TOK>), dim3((unsigned)wgs), dim3(kThreads), lds, hs, a)
     if (has_k) { if (few) KVS_DEV8(true, kTokFew); else KVS_DEV8(true, kTok); }

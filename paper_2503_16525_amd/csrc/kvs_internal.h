@@ -96,6 +96,7 @@ static_assert(kKeyHistCopies == 1, "key_hist_count adds to the one histogram");
 kvs_status launch_select_from_hist(const FusedScratch &fs, int32_t n, int32_t k, int32_t *idx_out, hipStream_t stream);
 
 constexpr int kWave = 64;
+constexpr int64_t kMostWgs = 0xffffff;   // of 256 threads: a launch has fewer than 2^32
 
 // monotone map fp32 -> uint32 (larger score <=> larger key); -0 is first folded onto +0.  Real
 // scores never map below 2^22 (-inf maps to 0x007fffff; only NaN patterns go lower).

@@ -276,7 +276,7 @@ extern "C" kvs_status kvs_rotary(const kvs_shape *shape, const kvs_rotary_spec *
         if (toks > n_tokens / 512) toks = (int)(n_tokens / 512);
         if (toks < 1) toks = 1;
         const int64_t wgs = (n_tokens + toks - 1) / toks;
-        if (wgs > 0x7fffffff) return fail(KVS_EINVAL, "kvs_rotary: too many rows");
+        if (wgs > kMostWgs) return fail(KVS_EUNSUPPORTED, "kvs_rotary: %lld rows in one call", (long long)n_tokens);
         const size_t lds = (size_t)toks * pairs * sizeof(float2);
 #define KVS_ROT(DT, IL)                                                                                                              \
         hipLaunchKernelGGL((rotary_kernel<DT, IL>), dim3((unsigned)wgs), dim3(kThreads), lds, hs, fr, rows[0], rows[1], n_tokens, toks,       \
@@ -290,12 +290,18 @@ extern "C" kvs_status kvs_rotary(const kvs_shape *shape, const kvs_rotary_spec *
     for (int i = 0; i < 2; ++i) {
         if (!rows[i].heads) continue;
         const int per_head = pairs + (in_place(rows[i]) ? 0 : left);
-        const int64_t items = n_tokens * rows[i].heads * per_head, wgs = (items + kThreads - 1) / kThreads;
-        if (wgs > 0x7fffffff) return fail(KVS_EINVAL, "kvs_rotary: too many rows");
         const int il = spec->layout == KVS_ROTARY_INTERLEAVED;
-        if (bf16) hipLaunchKernelGGL((rotary_pairs_kernel<KVS_BF16>), dim3((unsigned)wgs), dim3(kThreads), 0, hs, fr, rows[i], items, pairs, per_head, d, il, magnitude, pos, pos_from);
-        else hipLaunchKernelGGL((rotary_pairs_kernel<KVS_F32>), dim3((unsigned)wgs), dim3(kThreads), 0, hs, fr, rows[i], items, pairs, per_head, d, il, magnitude, pos, pos_from);
-        if ((st = check_launch("kvs_rotary")) != KVS_OK) return st;
+        const int64_t most = kMostWgs * kThreads / (rows[i].heads * per_head);          // rows of a launch
+        for (int64_t t0 = 0; t0 < n_tokens; t0 += most) {
+            const int64_t n = n_tokens - t0 < most ? n_tokens - t0 : most, items = n * rows[i].heads * per_head, wgs = (items + kThreads - 1) / kThreads;
+            Rows x = rows[i];
+            x.in = (const char *)x.in + t0 * x.in_stride * (int64_t)size;
+            x.out = (char *)x.out + t0 * x.out_stride * (int64_t)size;
+            const int32_t *from = pos_from ? pos_from + t0 : nullptr;
+            if (bf16) hipLaunchKernelGGL((rotary_pairs_kernel<KVS_BF16>), dim3((unsigned)wgs), dim3(kThreads), 0, hs, fr, x, items, pairs, per_head, d, il, magnitude, pos + t0, from);
+            else hipLaunchKernelGGL((rotary_pairs_kernel<KVS_F32>), dim3((unsigned)wgs), dim3(kThreads), 0, hs, fr, x, items, pairs, per_head, d, il, magnitude, pos + t0, from);
+            if ((st = check_launch("kvs_rotary")) != KVS_OK) return st;
+        }
     }
     return KVS_OK;
 }

@@ -388,6 +388,7 @@ extern "C" kvs_status kvs_store_kv8(const kvs_shape *shape, const kvs_cache8 *ca
         a.units_per_wg = (int)((rounds + split - 1) / split) * teams;
         grid = dim3((unsigned)wgs, (unsigned)((units + a.units_per_wg - 1) / a.units_per_wg));
     }
+    if (grid.x > (unsigned)kMostWgs) return fail(KVS_EUNSUPPORTED, "kvs_store_kv8: %lld rows in one call", (long long)n_sel);
     hipStream_t hs = (hipStream_t)stream;
 #define KVS_STORE(DT, C, DD)                                                                                          \
     do {                                                                                                              \

@@ -246,3 +246,19 @@ def test_rotary_behind_32_bits():
         B.kvs_rotary(sh, spec, pos[at:at + 50], None, q[at:at + 50], None, want, None)
         torch.cuda.synchronize()
         assert torch.equal(out[at:at + 50], want), at
+
+
+def test_rotary_of_more_pairs_than_a_launch_has_threads():
+    """A turned part of 100 channels goes by single pairs: 900000 rows of 64 heads are 4.5e9 of them and of the channels passed through."""
+    n, hq, d = 900_000, 64, 128
+    sh, spec = B.make_shape(hq, hq, d, B.BF16), B.rotary_spec(100)
+    q = torch.empty((n, hq, d), dtype=torch.bfloat16, device="cuda").normal_()
+    pos, old = torch.arange(n, dtype=torch.int32).cuda(), (torch.arange(n, dtype=torch.int32) % 1013).cuda()
+    out = torch.full_like(q, 7.0)
+    B.kvs_rotary(sh, spec, pos, old, q, None, out, None)
+    for at in (0, 430_000, 860_320, n - 50):               # a launch has 860370 of them
+        want = torch.empty((50 if at != 860_320 else 100, hq, d), dtype=torch.bfloat16, device="cuda")
+        part = slice(at, at + want.shape[0])
+        B.kvs_rotary(sh, spec, pos[part], old[part], q[part], None, want, None)
+        torch.cuda.synchronize()
+        assert torch.equal(out[part], want), at
