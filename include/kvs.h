@@ -513,9 +513,10 @@ KVS_API kvs_status kvs_deviation_kv8(const kvs_shape *shape, const kvs_cache8 *c
  *            size asked for has room for that from 7373 rows (tokens times query heads) on; what a key adds to an output
  *            there is lost below 2^-65.  Less workspace means fewer pieces and no widening.  One call's until that call has ended on its stream.
  * Codes enter the matrix cores as the bf16 numbers that they are, exactly; K's scales multiply the scores in fp32.
- * bf16: softmax weights enter the second product times V's scales and rounded to bf16, in widened contexts both factors are
- * rounded.  fp32: Q and these products enter as three bf16 numbers each, which together hold all their bits, and
- * everything else is fp32.
+ * bf16: softmax weights enter the second product times V's scales, as two bf16 numbers that hold 16 of their bits where no
+ * request has more than 32 rows a KV head (tokens times the query heads that share it), rounded to one elsewhere.
+ * fp32: Q and these products enter as three bf16 numbers each, which together hold all their bits, and everything else is
+ * fp32.  Sums of values beyond 2^110 may become infinite.
  */
 KVS_API kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8 *cache, int32_t batch,
                                      const int64_t *ctx_off, const int64_t *ctx_len, const int64_t *cu_sel,
