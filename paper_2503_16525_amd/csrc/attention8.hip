@@ -621,9 +621,9 @@ inline int64_t blocks_of(int64_t n_sel, int grp) { return (n_sel * grp + kRows -
 
 // The piece with the least estimated time, of those whose slots the workspace holds.  In microseconds, as measured: a workgroup
 // takes kAlone for a tile, kTile beside a second one on its CU, and kStart besides; the caches are read at kBytes a microsecond,
-// row blocks of the same keys from L2, and an eighth slower by one workgroup a CU; behind the average workgroup's end the longest
-// go on by themselves; a merge costs its launch and its slots, written and read.  Rows of several blocks are taken to be
-// spread over their context, and to see half of it.
+// row blocks of the same keys from L2, and an eighth slower by one workgroup a CU; reading and computing hide each other less
+// the closer they are; behind the average workgroup's end the longest go on by themselves; a merge costs its launch and its
+// slots, written and read.  Rows of several blocks are taken to be spread over their context, and to see half of it.
 Plan plan_pieces(const kvs_shape *shape, int32_t n_req, const int64_t *ctx_len, const int64_t *cu_sel, size_t workspace_bytes)
 {
     constexpr double kPlaces = 512, kAlone = 0.32, kTile = 0.38, kStart = 4.0, kBytes = 4.9e6, kMerge = 5.0, kSlotBytes = 2e6;
@@ -660,8 +660,8 @@ Plan plan_pieces(const kvs_shape *shape, int32_t n_req, const int64_t *ctx_len, 
         const double places = busy < kPlaces ? busy : kPlaces;
         const double second = busy <= kPlaces / 2 ? 0 : (places - kPlaces / 2) / (kPlaces / 2);         // CUs with a second workgroup
         const double reading = bytes / (kBytes * (0.88 + 0.12 * second)), computing = load / places * (kAlone + (kTile - kAlone) * second);
-        const double tail = busy <= kPlaces ? (double)piece - load / busy : (double)piece * (slots ? 0.5 : 0.25);
-        double us = (reading > computing ? reading : computing) + (tail > 0 ? tail * kAlone : 0) + kStart * (busy > kPlaces ? busy / kPlaces : 1);
+        const double tail = busy <= kPlaces ? (double)piece - load / busy : (double)piece * (slots ? 0.35 : 0.25);
+        double us = cbrt(reading * reading * reading + computing * computing * computing) + (tail > 0 ? tail * kAlone : 0) + kStart * (busy > kPlaces ? busy / kPlaces : 1);
         if (slots) us += kMerge + 2 * (double)slots * (double)slot_bytes(shape->head_dim) / kSlotBytes;
         if (us < best_us) {
             best_us = us;
