@@ -12,9 +12,10 @@
 // row takes is settled in LDS: the highest that names it, whatever order the entries of a block come in.  A lane has the same
 // piece of up to 8 rows: its maximum runs over the rows first, then over the lanes of its head (no exchange beyond 16 lanes), and the
 // scale is made in every lane that needs it.  What a wave waits for is one trip to memory for the positions, one for the rows
-// and old scales, and where a scale grows one for the codes that it rounds again.  (4424 of 32768 rows of 8 heads: a
-// workgroup for each entry 35.6 us, a chunk of the list and one unit a workgroup 25.8, a wave a run with whole heads one after the
-// other 20, issue bound; this 13.6; one row in each of 64 blocks 3.7.)
+// and old scales, and where a scale grows one or two for the codes that it rounds again, head by head with all lanes.  (4424 of 32768
+// rows of 8 heads, blocks of 32: a workgroup for each entry 35.6 us, a chunk of the list and one unit a workgroup 25.8, a wave a run
+// with whole heads one after the other 20, issue bound; this 12.5, with loads that do not stay in the caches 14.6; where scales grow 15.5, with
+// the rows rounded again for all heads of the wave at once 19.7.  One row in each of 64 blocks 3.7, in blocks of 128 whose scales grow 11, 31 so.)
 #include "cache8.h"
 
 #include <math.h>
@@ -26,6 +27,7 @@ constexpr int kThreads = 256;
 constexpr int kWaveRows = 32;
 constexpr int kMaxBlock = 128;
 constexpr int kListRows = 8;           // rows of a run that a lane holds
+constexpr int kAgain = 2;              // 16-byte pieces of kept rows that a lane holds
 constexpr int kMaxChunk = 32;          // entries in which a wave looks for runs; runs that go on behind them are followed
 constexpr int64_t kManyWaves = 16384;  // waves from which they get more entries each
 
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void store_list_kernel(const StoreArgs a)
 #pragma unroll
             for (int j = 0; j < kListRows; ++j) {
                 w[j] = make_uint4(0u, 0u, 0u, 0u);
-                if (k0 + j < count && inside) w[j] = stream_load16(from + (int64_t)src[row_at[k0 + j]] * pieces + piece);
+                if (k0 + j < count && inside) w[j] = from[(int64_t)src[row_at[k0 + j]] * pieces + piece];
             }
         };
         for (int k0 = 0; k0 < count; k0 += kListRows) {
@@ -318,19 +320,28 @@ __global__ __launch_bounds__(kThreads) void store_list_kernel(const StoreArgs a)
                 if (k0 + j < count && inside) write_codes<DTYPE, CODE>(to + row_at[k0 + j] * row_bytes + piece * E, w[j], n.inv, n.odd);
         }
         if (inside && lane % PPR == 0) *scale_at = n.scale;
-        if (__ballot(n.again && inside) == 0) continue;
-        // Kept rows stand for what they stood for, in steps of the new scale.  The wave's heads have kCodes 16-byte pieces of codes a row.
-        constexpr int kCodes = kWave * E / 16, kAtOnce = kWave / kCodes;
-        const int c = lane % kCodes, from_lane = c * 16 / E;   // a lane that has the scale of that piece's head
-        const float ratio = __shfl(n.ratio, from_lane);
-        const bool wanted = __shfl((int)(n.again && inside), from_lane) != 0;
-        uint8_t *const codes = to + (piece - lane) * E + c * 16;
-#pragma unroll 4
-        for (int r = lane / kCodes; r < rows_here; r += kAtOnce) {
-            if (!wanted || src[r] >= 0) continue;
-            uint4 *const at16 = reinterpret_cast<uint4 *>(codes + r * row_bytes);
-            const uint4 x = *at16;
-            *at16 = make_uint4(again4<CODE>(x.x, ratio), again4<CODE>(x.y, ratio), again4<CODE>(x.z, ratio), again4<CODE>(x.w, ratio));
+        // Kept rows stand for what they stood for, in steps of the new scale: head by head, 64 pieces of 16 codes of it at once.
+        constexpr int kCodes = D / 16, kAtOnce = kWave / kCodes;
+        for (uint64_t need = __ballot(n.again && inside && lane % PPR == 0); need; need &= need - 1) {
+            const int of = __builtin_ctzll(need);
+            const float ratio = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.ratio), of));
+            uint8_t *const codes = to + (piece - lane + of) * E + (lane % kCodes) * 16;
+            for (int r0 = lane / kCodes; r0 < rows_here; r0 += kAgain * kAtOnce) {
+                uint4 x[kAgain];
+#pragma unroll
+                for (int j = 0; j < kAgain; ++j) {
+                    const int r = r0 + j * kAtOnce;
+                    x[j] = make_uint4(0u, 0u, 0u, 0u);
+                    if (r < rows_here && src[r] < 0) x[j] = *reinterpret_cast<const uint4 *>(codes + r * row_bytes);
+                }
+#pragma unroll
+                for (int j = 0; j < kAgain; ++j) {
+                    const int r = r0 + j * kAtOnce;
+                    if (r < rows_here && src[r] < 0)
+                        *reinterpret_cast<uint4 *>(codes + r * row_bytes) =
+                            make_uint4(again4<CODE>(x[j].x, ratio), again4<CODE>(x[j].y, ratio), again4<CODE>(x[j].z, ratio), again4<CODE>(x[j].w, ratio));
+                }
+            }
         }
     }
 }
