@@ -15,7 +15,7 @@
 // waves take the same 32 rows and every fourth tile, each with LDS slots of its own that its loads go to directly
 // (global to LDS, 16 bytes a lane, no registers), two tiles deep and without a barrier; at the end the waves meet in LDS.
 // Launches of too few workgroups cut the key ranges into pieces, which a second kernel merges.  (One row of 8 query heads each over
-// 131072 keys of 4 KV heads: 30 us and 6 for the merge, 4.5 TB/s in the first; 64 contexts of 4096 to 16384, 8 KV heads: 270 us,
+// 131072 keys of 4 KV heads: 30 us and 4.4 for the merge, 4.5 TB/s in the first; 64 contexts of 4096 to 16384, 8 KV heads: 270 us,
 // 5.0 TB/s.)
 //
 // With many rows the vector instructions do: a tile's 215 (e4m3: 64 conversions, 16 exponentials, 16 fused multiply-adds, and
