@@ -40,7 +40,7 @@ constexpr int kRows = 32;              // rows of a unit
 constexpr int kKeys = 32;              // keys of a tile
 constexpr int kAlign = 16;             // cache rows that tiles are aligned to: no block is shorter
 constexpr float kSlack = 8.f;          // powers of two that a score may lie above its reference
-constexpr int kMinPieceTiles = 8;      // tiles of a piece: two for each wave
+constexpr int kMinPieceTiles = 4;      // tiles of a piece: one for each wave (with two, one row of 600 keys of 8 heads 10.1 us instead of 8.1, 4000 keys 9.8 and 8.6)
 constexpr int kMaxPieces = 512;
 constexpr int64_t kMaxCutWgs = 2048;   // workgroups at most where key ranges are cut: four for every place on the chip
 
@@ -627,8 +627,9 @@ inline int64_t blocks_of(int64_t n_sel, int grp) { return (n_sel * grp + kRows -
 // The piece with the least estimated time, of those whose slots the workspace holds.  In microseconds, as measured: a workgroup
 // takes kAlone for a tile, kTile beside a second one on its CU, and kStart besides; the caches are read at kBytes a microsecond,
 // row blocks of the same keys from L2, and an eighth slower by one workgroup a CU; reading and computing hide each other less
-// the closer they are; behind the average workgroup's end the longest go on by themselves; a merge costs its launch and its
-// slots, written and read.  Rows of several blocks are taken to be spread over their context, and to see half of it.
+// the closer they are; behind the average workgroup's end the longest go on by themselves; a merge costs its launch (2 in a
+// full queue, 5 where the device waits for the host) and its slots, written and read.  Rows of several blocks are taken to be
+// spread over their context, and to see half of it.
 Plan plan_pieces(const kvs_shape *shape, int32_t n_req, const int64_t *ctx_len, const int64_t *cu_sel, size_t workspace_bytes)
 {
     constexpr double kPlaces = 512, kAlone = 0.32, kTile = 0.38, kStart = 4.0, kBytes = 4.9e6, kMerge = 5.0, kSlotBytes = 2e6;
