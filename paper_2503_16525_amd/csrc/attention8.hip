@@ -47,11 +47,12 @@ constexpr int64_t kMaxCutWgs = 2048;   // workgroups at most where key ranges ar
 // The launch's requests.  Workgroup = (unit, KV head); a unit is a block of 32 rows of one request and one piece of its keys.
 struct Table {
     int64_t ctx_off[kAttnMaxReq];
-    int64_t sel_lo[kAttnMaxReq];           // first selected token
-    int64_t slot_lo[kAttnMaxReq];          // first slot in the workspace
-    int32_t ctx_len[kAttnMaxReq], n_sel[kAttnMaxReq], pieces[kAttnMaxReq];
+    int64_t sel0;                          // selected tokens before the launch
+    int32_t ctx_len[kAttnMaxReq];
     int32_t unit_begin[kAttnMaxReq + 1];
     int32_t sel_begin[kAttnMaxReq + 1];    // selected tokens before the request, in this launch
+    int32_t slot_begin[kAttnMaxReq];       // slots in the workspace before it: fewer than 32 kMaxCutWgs
+    int32_t pieces[kAttnMaxReq];
     int32_t n_req, piece_tiles;
     int32_t interleaved;                   // unit u is unit u / n_req of request u % n_req, where that exists
 };
@@ -158,8 +159,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     const int piece = in_req / row_blocks, row_block = row_blocks - 1 - in_req % row_blocks;
     const int grp = n_q_heads / n_kv_heads;
     const int ctx_len = td.ctx_len[b];
-    const int rows = td.n_sel[b] * grp;                     // the host keeps this below 2^31
-    const int64_t sel_lo = td.sel_lo[b];
+    const int rows = (td.sel_begin[b + 1] - td.sel_begin[b]) * grp;      // the host keeps this below 2^31
+    const int64_t sel_lo = td.sel0 + td.sel_begin[b];
 
     // ---- this lane's row (both half-waves hold the same 32) ------------------------------------------------
     const int rq = min(row_block * kRows + ln, rows - 1);
@@ -471,7 +472,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
     const int t2 = row_q / grp, h2 = row_q - t2 * grp;
     const int64_t at = (sel_lo + t2) * n_q_heads + g * grp + h2;
     if (pieces > 1) {
-        const int64_t slot = td.slot_lo[b] + ((int64_t)t2 * n_q_heads + g * grp + h2) * pieces + piece;
+        const int64_t slot = td.slot_begin[b] + ((int64_t)t2 * n_q_heads + g * grp + h2) * pieces + piece;
         if (part == 0) part_ml[slot] = make_float4(top, l, lr, 0.f);
         if (l != 0.f) {                                      // (the merge passes over a piece without keys)
             float4 *dst = reinterpret_cast<float4 *>(part_o + slot * D + part * CPT);
@@ -514,7 +515,7 @@ __global__ __launch_bounds__(kThreads) void merge8_kernel(const Table td, int n_
     const int pieces = td.pieces[b];
     if (pieces <= 1) return;                                 // stored as it is by its only workgroup
     const int64_t local = item - (int64_t)td.sel_begin[b] * n_q_heads;
-    const int64_t slot = td.slot_lo[b] + local * pieces;
+    const int64_t slot = td.slot_begin[b] + local * pieces;
     static_assert(kMaxPieces == 2 * kThreads, "two records a thread");
     float4 x[2];
     float top = kLowest;
@@ -565,7 +566,7 @@ __global__ __launch_bounds__(kThreads) void merge8_kernel(const Table td, int n_
         const float4 y = sum_s[i][lane];
         o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
     }
-    const int64_t at = td.sel_lo[b] * n_q_heads + local;
+    const int64_t at = td.sel0 * n_q_heads + item;
     const float inv = 1.f / lr;
     if (l != 0.f) { o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv; }
     else o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -588,7 +589,7 @@ __global__ __launch_bounds__(kThreads) void merge8_rows_kernel(const Table td, i
     const int pieces = td.pieces[b];
     if (pieces <= 1) return;
     const int64_t local = item - (int64_t)td.sel_begin[b] * n_q_heads;
-    const int64_t slot = td.slot_lo[b] + local * pieces;
+    const int64_t slot = td.slot_begin[b] + local * pieces;
     const float4 *from = reinterpret_cast<const float4 *>(part_o + slot * D) + c;
     float4 x[kFewPieces], y[kFewPieces];
     float top = kLowest;
@@ -607,7 +608,7 @@ __global__ __launch_bounds__(kThreads) void merge8_rows_kernel(const Table td, i
         lr += x[p].z * f;
         if (x[p].y != 0.f) { o.x += f * y[p].x; o.y += f * y[p].y; o.z += f * y[p].z; o.w += f * y[p].w; }       // (a piece without keys has left no sums)
     }
-    const int64_t at = td.sel_lo[b] * n_q_heads + local;
+    const int64_t at = td.sel0 * n_q_heads + item;
     const float inv = 1.f / lr;
     if (l != 0.f) { o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv; }
     else o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -918,6 +919,7 @@ extern "C" kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8
         const Plan plan = plan_pieces(shape, nr, ctx_len + b0, cu_sel + b0, workspace_bytes);
         Table td = {};
         td.n_req = nr;
+        td.sel0 = cu_sel[b0];
         td.piece_tiles = plan.piece_tiles ? (int32_t)plan.piece_tiles : 0x7fffffff;
         int64_t units = 0, slot = 0, most = 0;
         int32_t most_pieces = 1;
@@ -928,10 +930,8 @@ extern "C" kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8
             const int64_t n = cu_sel[b0 + i + 1] - cu_sel[b0 + i];
             const int64_t p = n && plan.piece_tiles ? (tiles_of(ctx_len[b0 + i]) + plan.piece_tiles - 1) / plan.piece_tiles : 1;
             td.ctx_off[i] = ctx_off[b0 + i];
-            td.sel_lo[i] = cu_sel[b0 + i];
-            td.slot_lo[i] = slot;
+            td.slot_begin[i] = (int32_t)slot;
             td.ctx_len[i] = (int32_t)ctx_len[b0 + i];
-            td.n_sel[i] = (int32_t)n;
             td.pieces[i] = (int32_t)(p > 1 ? p : 1);
             if (p > 1) slot += n * shape->n_q_heads * p;
             const int64_t own = blocks_of(n, grp) * td.pieces[i];
