@@ -457,10 +457,13 @@ typedef struct {
  * rows in place of reused ones.
  *
  * sel_pos == NULL  row row0 + s takes k_new[s], v_new[s]           for s in [0, n_sel)
- * sel_pos != NULL  row sel_pos[s] takes them (row0 is not read).  Entries of one block have to stand together in the list
- *                  (an ascending list does that, one that keeps every request's rows together in any order of the
- *                  requests too); inside a block any order goes, and of equal entries the last one counts.  Entries
- *                  outside [0, n_rows) are skipped; they count as a block of their own.
+ * sel_pos != NULL  row sel_pos[s] takes them (row0 is not read).  Entries outside [0, n_rows) are skipped, wherever they stand (the
+ *                  places of a padded batch that hold no token).  The others of one block have to stand together in the list: an
+ *                  ascending list does that, and one that keeps every request's rows together in any order of the
+ *                  requests if no two requests share a block (requests that do are stored in ascending order of their
+ *                  rows, or by a call each).  The call cannot see a list that breaks this: the codes and scales of a block
+ *                  whose entries stand apart are then not to be used.  Inside a block any order goes, and of equal
+ *                  entries the last one counts.
  *
  * For each block that takes a row, each KV head, K and V apart, with top = 448 (KVS_E4M3) or 127 (KVS_INT8), in fp32:
  *     need  = max |x| over the rows that the block takes * (1 / top), at least 2^-126 (0 if they are all zero)

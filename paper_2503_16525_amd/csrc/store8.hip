@@ -7,8 +7,10 @@
 // Rows in a row (no list): a workgroup has one block and its share of the units, a unit being one KV head of K or of V.  A wave
 // holds up to 32 rows of a unit, so a unit takes a team of 1, 2 or 4 waves (`waves`), which meet in LDS for their maximum.
 //
-// A list: its entries of one block are a run.  A wave has a few entries of the list, finds the runs that begin there from one
-// load of the positions, and takes 64 pieces of the rows of each, 4 heads of 256 bytes; no wave waits for another.  Which entry a
+// A list: its entries of one block, and skipped ones between them, are a run.  A wave has a few entries of the list, finds the runs that begin there from one
+// load of the positions, and takes 64 pieces of the rows of each, 4 heads of 256 bytes; no wave waits for another.  Skipped entries
+// end no run: the wave of the last one before a stretch of them looks through it (0.9 us for 512 entries; 1000 rows and 3096 of them 11.1 us, 10.1 where
+// they ended it), and the wave that begins behind it looks back.  Which entry a
 // row takes is settled in LDS: the highest that names it, whatever order the entries of a block come in.  A lane has the same
 // piece of up to 8 rows: its maximum runs over the rows first, then over the lanes of its head (no exchange beyond 16 lanes), and the
 // scale is made in every lane that needs it.  What a wave waits for is one trip to memory for the positions, one for the rows
@@ -20,6 +22,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace kvs {
 namespace {
 
@@ -29,6 +33,7 @@ constexpr int kMaxBlock = 128;
 constexpr int kListRows = 8;           // rows of a run that a lane holds
 constexpr int kAgain = 2;              // 16-byte pieces of kept rows that a lane holds
 constexpr int kMaxChunk = 32;          // entries in which a wave looks for runs; runs that go on behind them are followed
+constexpr int kSkips = 8;              // times 64 entries asked for at once where a list is followed far (16: a wave a SIMD fewer, 4424 of 32768 rows 5 % slower)
 constexpr int64_t kManyWaves = 16384;  // waves from which they get more entries each
 
 struct StoreArgs {
@@ -242,17 +247,31 @@ __global__ __launch_bounds__(kThreads) void store_list_kernel(const StoreArgs a)
     const int g = piece / PPR;                             // its KV head
     int *const src = src_s[wave], *const row_at = row_s[wave];
 
-    // lane i holds entry chunk0 + i: its block (-1: outside the cache), and whether a run begins there
+    // lane i holds entry chunk0 + i: its block (-1: skipped, outside the cache), and whether a run begins there
     const int64_t chunk0 = ((int64_t)blockIdx.x * 4 + wave) * a.chunk;
     if (chunk0 >= a.n_sel) return;
     auto blk_of = [&](int p) -> int { return p >= 0 && p < a.n_rows ? p >> a.block_log2 : -1; };
     const int my_pos = chunk0 + lane < a.n_sel ? a.sel_pos[chunk0 + lane] : -1;
-    const int before = chunk0 > 0 ? a.sel_pos[chunk0 - 1] : -1;
+    int before = __builtin_amdgcn_readfirstlane(blk_of(chunk0 > 0 ? a.sel_pos[chunk0 - 1] : -1));
     const int my_blk = blk_of(my_pos);
-    int left = __shfl_up(my_blk, 1);
-    if (lane == 0) left = blk_of(before);
-    const uint64_t ends = __ballot(my_blk != left || my_blk < 0);      // where what stands before ends
-    uint64_t runs = __ballot(my_blk >= 0 && lane < a.chunk && my_blk != left);
+    const uint64_t taken = __ballot(my_blk >= 0), own = ((uint64_t)1 << a.chunk) - 1;
+    // Skipped entries end no run: what counts is the block of the last entry before that is not one.
+    for (int64_t s = chunk0 - 1; (taken & own) && before < 0 && s > 0; s -= kSkips * kWave) {
+        const int32_t *const at = a.sel_pos + (s - kWave);         // (before the list's begin where nothing is read)
+        const int there = (int)min(s, (int64_t)(kSkips * kWave));
+        int p[kSkips];
+#pragma unroll
+        for (int j = 0; j < kSkips; ++j) p[j] = j * kWave + 63 - lane < there ? at[lane - j * kWave] : -1;
+#pragma unroll
+        for (int j = 0; j < kSkips; ++j) {
+            const uint64_t some = __ballot(blk_of(p[j]) >= 0);
+            if (some && before < 0) before = __builtin_amdgcn_readlane(blk_of(p[j]), 63 - __builtin_clzll(some));
+        }
+    }
+    const uint64_t left_of = taken & (((uint64_t)1 << lane) - 1);
+    const int left_blk = __shfl(my_blk, left_of ? 63 - __builtin_clzll(left_of) : 0), left = left_of ? left_blk : before;
+    const uint64_t begins = __ballot(my_blk >= 0 && my_blk != left);
+    uint64_t runs = begins & own;
     if (blockIdx.y == 0 && my_blk >= 0 && lane < a.chunk) {
         if (a.reused) a.reused[my_pos] = 0;
         if (a.dev_v) for (int g = 0; g < hk; ++g) a.dev_v[(int64_t)g * a.n_rows + my_pos] = 0.f;
@@ -264,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void store_list_kernel(const StoreArgs a)
 
     for (; runs; runs &= runs - 1) {
         const int at = __builtin_ctzll(runs);
-        const uint64_t after = at == 63 ? 0 : ends >> (at + 1);
+        const uint64_t after = at == 63 ? 0 : begins >> (at + 1);
         const int end = after ? at + 1 + __builtin_ctzll(after) : 64;
         const int blk = __builtin_amdgcn_readlane(my_blk, at);
         const int64_t block0 = (int64_t)blk << a.block_log2;
@@ -276,16 +295,26 @@ __global__ __launch_bounds__(kThreads) void store_list_kernel(const StoreArgs a)
         src[lane] = -1;
         src[lane + 64] = -1;
         in_order();
-        if (lane >= at && lane < end) atomicMax(&src[my_pos - base], (int)(chunk0 + lane));
-        if (end == 64) {
-            for (int64_t s = chunk0 + 64;; s += 64) {
-                const int p = s + lane < a.n_sel ? a.sel_pos[s + lane] : -1;
-                const uint64_t out = __ballot(blk_of(p) != blk);
-                const int cut = out ? __builtin_ctzll(out) : 64;
-                if (lane < cut) atomicMax(&src[p - base], (int)(s + lane));
-                if (cut < 64) break;
+        if (lane >= at && lane < end && my_blk >= 0) atomicMax(&src[my_pos - base], (int)(chunk0 + lane));
+        // the run's entries among the n times 64 from s on; whether it may go on behind them
+        auto follow = [&](int64_t s, auto n) -> bool {
+            const int32_t *const at = a.sel_pos + s;
+            const int there = (int)min(a.n_sel - s, (int64_t)(n * kWave));
+            int p[n];
+            bool on = true;
+#pragma unroll
+            for (int j = 0; j < n; ++j) p[j] = j * kWave + lane < there ? at[j * kWave + lane] : -1;
+#pragma unroll
+            for (int j = 0; j < n; ++j) {
+                const int b = blk_of(p[j]);
+                const uint64_t out = __ballot(b >= 0 && b != blk);
+                if (on && lane < (out ? __builtin_ctzll(out) : 64) && b >= 0) atomicMax(&src[p[j] - base], (int)(s + j * kWave + lane));
+                on = on && !out;
             }
-        }
+            return on && s + n * kWave < a.n_sel;
+        };
+        if (end == 64 && chunk0 + 64 < a.n_sel && follow(chunk0 + 64, std::integral_constant<int, 1>{}))
+            for (int64_t s = chunk0 + 128; follow(s, std::integral_constant<int, kSkips>{});) s += kSkips * kWave;
         in_order();
         const int rows_here = (int)min((int64_t)1 << a.block_log2, a.n_rows - block0);
         const uint64_t lo = __ballot(src[lane] >= 0), hi = __ballot(src[lane + 64] >= 0);
