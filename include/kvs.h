@@ -433,7 +433,7 @@ KVS_API kvs_status kvs_rotary(const kvs_shape *shape, const kvs_rotary_spec *spe
  * requests that begin with a block of their own share no scale with another request.  No scale is negative.  A scale of 0
  * marks a block that holds nothing but zeros (whatever its codes): set the scales of a block to 0 before its first use and
  * before another request takes it over.  A scale that is NaN marks a block that a NaN or infinity was stored into: rows that
- * see one of its keys become NaN, no others.
+ * see one of its keys become NaN, their log-sum-exps too, no others.
  *
  * KVS_E4M3 codes are OCP 8-bit floats with 3 mantissa bits (largest 448), KVS_INT8 codes whole numbers from -127 to 127.
  * A store writes no other codes; e4m3's two NaN codes, where memory that was never stored to holds them, do not reach

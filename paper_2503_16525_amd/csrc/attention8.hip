@@ -324,7 +324,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
             }
         }
         if constexpr (V_EARLY) { v_operands(0); v_operands(1); }
-        float f[2] = {sc.k[0] * scale_abs, sc.k[1] * scale_abs};
+        // (a broken block's V makes the scores NaN too, as the widened contexts' K does: sums and log-sum-exps then say so)
+        float f[2] = {__builtin_fmaf(sc.v[0], 0.f, sc.k[0] * scale_abs), __builtin_fmaf(sc.v[1], 0.f, sc.k[1] * scale_abs)};
         const int first = shift - x0 - 8 * hf, last = xpos - x0 - 8 * hf;     // entries 16 (r >> 3) + (r & 7) from `first` to `last` are seen
         auto entry = [](int r) { return 16 * (r >> 3) + (r & 7); };
         if (masked) {
