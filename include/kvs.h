@@ -509,12 +509,14 @@ KVS_API kvs_status kvs_deviation_kv8(const kvs_shape *shape, const kvs_cache8 *c
  *
  * q_sel, out [dev] [n_sel, n_q_heads, head_dim]      lse_out [dev] fp32[n_sel, n_q_heads] or NULL (natural log)
  * scale      any finite number
- * workspace  [dev] optional (NULL / 0 is valid), 256-byte aligned, kvs_workspace_size("attention_kv8", shape, batch, cache
- *            rows, n_sel) bytes.  Launches that would leave units idle cut their key ranges into pieces and merge them.
+ * workspace  [dev] optional (NULL / 0 is valid), 256-byte aligned, kvs_workspace_size("attention_kv8", shape, batch, rows, n_sel)
+ *            bytes, rows being those of its contexts together, or the cache's if they are fewer.  Launches that would leave units
+ *            idle cut their key ranges into pieces and merge them.
  *            Launches of so many rows that it pays (bf16, head_dim 128, scale > 0, contexts that begin at multiples of
- *            16 rows) widen their contexts to bf16 in it, 4 bytes an element of K, and go on as kvs_partial_attention; the
- *            size asked for has room for that from 7373 rows (tokens times query heads) on; what a key adds to an output
- *            there is lost below 2^-65.  Less workspace means fewer pieces and no widening.  One call's until that call has ended on its stream.
+ *            16 rows) widen the rows that their contexts hold to bf16 in it, once where contexts share them, 4 bytes an
+ *            element of K, and go on as kvs_partial_attention; the size asked for has room for that from 7373 rows (tokens
+ *            times query heads) on; what a key adds to an output there is lost below 2^-65.  Less workspace means fewer pieces and no
+ *            widening.  One call's until that call has ended on its stream.
  * Codes enter the matrix cores as the bf16 numbers that they are, exactly; K's scales multiply the scores in fp32.
  * bf16: softmax weights enter the second product times V's scales, as two bf16 numbers that hold 16 of their bits where no
  * request has more than 32 rows a KV head (tokens times the query heads that share it), rounded to one elsewhere.

@@ -696,33 +696,36 @@ __device__ __forceinline__ float rest_of_scale(float s)
     return a >= kLeastScale && a < INFINITY ? __uint_as_float((__float_as_uint(s) & 0x7fffffu) | 0x3f800000u) : 1.f;
 }
 
+// The rows that the requests of a launch see, as ranges that share no row (requests may see the same rows), and the copy holds one range
+// behind the other.
 struct CopyRanges {
-    int64_t row[kAttnMaxReq];              // first row of request b, a multiple of 16
-    int32_t begin[kAttnMaxReq + 1];        // groups of 16 rows before it in the launch
-    int32_t n_req;
+    int64_t row[kAttnMaxReq];              // first row of range i, a multiple of 16
+    int32_t begin[kAttnMaxReq + 1];        // groups of 16 rows before it in the copy
+    int32_t n;
 };
 
 template <int CODE>
-__global__ __launch_bounds__(kCopyThreads) void copy8_kernel(const CopyRanges cr, int n_kv_heads, int64_t n_rows, int64_t first_row, int64_t end_row, int block_log2,
+__global__ __launch_bounds__(kCopyThreads) void copy8_kernel(const CopyRanges cr, int n_kv_heads, int64_t n_rows, int block_log2,
                                                              const uint4 *__restrict__ k_codes, const uint4 *__restrict__ v_codes,
                                                              const float *__restrict__ k_scale, const float *__restrict__ v_scale, float scale_log2,
                                                              uint4 *__restrict__ k_out, uint4 *__restrict__ v_out, float4 *__restrict__ factors, int64_t factor_stride)
 {
     constexpr int kChunks = 128 / 16;
-    const int b = request_of(cr.begin, cr.n_req, (int)blockIdx.x);
-    const int64_t row0 = cr.row[b] + ((int64_t)blockIdx.x - cr.begin[b]) * kAlign;      // the workgroup's 16 rows: one block of scales
+    const int64_t group = blockIdx.x;                                                   // of the copy
+    const int b = request_of(cr.begin, cr.n, (int)group);
+    const int64_t row0 = cr.row[b] + (group - cr.begin[b]) * kAlign;                    // the workgroup's 16 rows: one block of scales
     const int64_t scales = (min(row0, n_rows - 1) >> block_log2) * n_kv_heads;
-    const int rows = (int)min((int64_t)kAlign, min(n_rows, end_row) - row0);            // (none where only the factors of a tile's second half are wanted)
+    const int rows = (int)min((int64_t)kAlign, n_rows - row0);                          // (none where only the factors of a tile's second half are wanted)
     for (int g = threadIdx.x; g < n_kv_heads; g += kCopyThreads) {
         // (positive and finite, whatever the scale: a block that stands for zeros has codes of 0, a broken one NaN in K)
         const float f = k_scale[scales + g] * scale_log2;
         const float m = rest_of_scale(v_scale[scales + g]);
-        factors[g * factor_stride + (row0 - first_row) / kAlign] = make_float4(f >= 7.888609e-31f && f < INFINITY ? f : 7.888609e-31f, __log2f(m), 1.f / m, 0.f);
+        factors[g * factor_stride + group] = make_float4(f >= 7.888609e-31f && f < INFINITY ? f : 7.888609e-31f, __log2f(m), 1.f / m, 0.f);
     }
     const int per_row = n_kv_heads * kChunks;
     for (int e = threadIdx.x; e < rows * per_row; e += kCopyThreads) {
         const int c = e % per_row;
-        const int64_t from = row0 * per_row + e, to = ((row0 - first_row) * per_row + e) * 2;
+        const int64_t from = row0 * per_row + e, to = (group * kAlign * per_row + e) * 2;
         const float ks = k_scale[scales + c / kChunks], vs = v_scale[scales + c / kChunks];
         const float v_by = rest_of_scale(vs) == 1.f ? vs : __uint_as_float(__float_as_uint(vs) & 0xff800000u);
         const uint4 k = stream_load16(k_codes + from), v = stream_load16(v_codes + from);
@@ -759,10 +762,15 @@ __global__ __launch_bounds__(kThreads) void empty_rows_kernel(int64_t n_sel, int
 
 constexpr int64_t kCopyMinRows = 7373;     // selected rows over all query heads: 48 tiles of 256, 0.6 full, as the bf16 kernel asks for
 constexpr int64_t kCopyPad = 8;            // factors behind the last row's: what a step ahead asks for
-inline size_t copy_bytes(const kvs_shape *shape, int64_t rows)
+inline size_t copy_bytes(const kvs_shape *shape, int64_t groups)
 {
-    const int64_t groups = (rows + kAlign - 1) / kAlign;
     return (size_t)(groups * kAlign * shape->n_kv_heads * 128 * 4 + (groups + kCopyPad) * shape->n_kv_heads * (int64_t)sizeof(float4) + 512);
+}
+// Groups that the ranges of a launch have at most, for requests of `rows` rows together: each ends with a part of one, and one more.
+inline int64_t copy_groups(int32_t batch, int64_t rows)
+{
+    const int64_t n = batch < 1 ? 1 : batch < kAttnMaxReq ? batch : kAttnMaxReq;
+    return (rows + kAlign - 1) / kAlign + 2 * n;
 }
 
 // Whether a copy for the bf16 kernel is worth its bytes.  Measured, of what rows in the middle of their contexts take: the kernel above
@@ -793,40 +801,51 @@ kvs_status launch_from_copy(const kvs_shape *shape, const kvs_cache8 *c, int32_t
 {
     CopyRanges cr = {};
     AttnBatch bd = {};
-    int64_t lo = INT64_MAX, hi = 0, groups = 0;
+    int order[kAttnMaxReq];                // the requests that select tokens, by their first row
+    int n_live = 0;
     for (int b = 0; b < n_req; ++b) {
         if (cu_sel[b + 1] == cu_sel[b]) continue;
-        if (ctx_off[b] < lo) lo = ctx_off[b];
-        if (ctx_off[b] + ctx_len[b] > hi) hi = ctx_off[b] + ctx_len[b];
+        int j = n_live++;
+        while (j > 0 && ctx_off[order[j - 1]] > ctx_off[b]) { order[j] = order[j - 1]; --j; }
+        order[j] = b;
     }
-    for (int b = 0; b < kAttnMaxReq; ++b) {
-        const bool live = b < n_req && cu_sel[b + 1] > cu_sel[b];
-        cr.begin[b] = (int32_t)groups;
-        cr.row[b] = live ? ctx_off[b] : 0;
-        bd.ctx_off[b] = live ? ctx_off[b] - lo : 0;
-        bd.ctx_len[b] = live ? ctx_len[b] : 0;
-        bd.cu_sel[b] = cu_sel[b < n_req ? b : n_req];
-        if (live) groups += (ctx_len[b] + 2 * kAlign - 1) / (2 * kAlign) * 2;       // whole tiles of 32 keys have factors
-        if (groups > 0x7fffff) return KVS_OK;
+    int64_t groups = 0, end = -1;          // of the copy so far; the last range's, in the cache, a multiple of 16
+    auto close = [&] { if (cr.n > 0) groups += (end - cr.row[cr.n - 1]) / kAlign + 1; };   // (whole tiles of 32 keys have factors)
+    for (int i = 0; i < n_live; ++i) {
+        const int b = order[i];
+        const int64_t to = (ctx_off[b] + ctx_len[b] + kAlign - 1) / kAlign * kAlign;
+        if (cr.n == 0 || ctx_off[b] > end) {
+            close();
+            if (groups > 0x7fffff) return KVS_OK;
+            cr.row[cr.n] = ctx_off[b];
+            cr.begin[cr.n++] = (int32_t)groups;
+            end = to;
+        } else if (to > end) {
+            end = to;
+        }
+        bd.ctx_off[b] = groups * kAlign + ctx_off[b] - cr.row[cr.n - 1];
+        bd.ctx_len[b] = ctx_len[b];
     }
-    cr.begin[kAttnMaxReq] = (int32_t)groups;
-    bd.cu_sel[kAttnMaxReq] = cu_sel[n_req];
+    close();
+    if (groups > 0x7fffff) return KVS_OK;
+    for (int b = cr.n; b <= kAttnMaxReq; ++b) cr.begin[b] = (int32_t)groups;
+    for (int b = 0; b <= kAttnMaxReq; ++b) bd.cu_sel[b] = cu_sel[b < n_req ? b : n_req];
     bd.sel_begin = cu_sel[0];
-    cr.n_req = bd.n_req = n_req;
-    const size_t need = copy_bytes(shape, hi - lo);
+    bd.n_req = n_req;
+    const size_t need = copy_bytes(shape, groups);
     if (workspace_bytes < need + 256) return KVS_OK;
     const size_t left = (workspace_bytes - need) / 256 * 256;        // the bf16 kernel's, in front of the copy
     AttnSplitPlan plan;
     if (!attention_takes_large(shape, bd, left, &plan)) return KVS_OK;
     *taken = true;
-    const int64_t rows = (hi - lo + kAlign - 1) / kAlign * kAlign;
+    const int64_t rows = groups * kAlign;
     char *at = (char *)workspace + left;
     uint4 *k_copy = (uint4 *)at, *v_copy = (uint4 *)(at + rows * shape->n_kv_heads * 256);
     float4 *factors = (float4 *)(at + rows * shape->n_kv_heads * 512);
-    const int64_t stride = rows / kAlign + kCopyPad;
+    const int64_t stride = groups + kCopyPad;
     const float scale_log2 = scale * 1.4426950408889634f;
     const dim3 grid((unsigned)groups), threads(kCopyThreads);
-#define KVS_COPY(C) hipLaunchKernelGGL((copy8_kernel<C>), grid, threads, 0, hs, cr, shape->n_kv_heads, c->n_rows, lo, lo + rows, __builtin_ctz((unsigned)c->block), \
+#define KVS_COPY(C) hipLaunchKernelGGL((copy8_kernel<C>), grid, threads, 0, hs, cr, shape->n_kv_heads, c->n_rows, __builtin_ctz((unsigned)c->block), \
                                        (const uint4 *)c->k, (const uint4 *)c->v, c->k_scale, c->v_scale, scale_log2, k_copy, v_copy, factors, stride)
     if (c->code == KVS_E4M3) KVS_COPY(KVS_E4M3); else KVS_COPY(KVS_INT8);
 #undef KVS_COPY
@@ -870,7 +889,7 @@ size_t attention8_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t
     if (n_sel_total < most && n_sel_total * shape->n_q_heads < most) slots = n_sel_total * shape->n_q_heads * pieces < most ? n_sel_total * shape->n_q_heads * pieces : most;
     size_t bytes = ((size_t)slots * slot_bytes(shape->head_dim) + 255) / 256 * 256;
     if (shape->dtype == KVS_BF16 && shape->head_dim == 128 && n_sel_total >= kCopyMinRows / shape->n_q_heads) {
-        const size_t copy = (copy_bytes(shape, n_rows_total) + attention_workspace_bytes(shape, batch, n_rows_total, n_sel_total) + 511) / 256 * 256;
+        const size_t copy = (copy_bytes(shape, copy_groups(batch, n_rows_total)) + attention_workspace_bytes(shape, batch, n_rows_total, n_sel_total) + 511) / 256 * 256;
         if (copy > bytes) bytes = copy;
     }
     return bytes;
