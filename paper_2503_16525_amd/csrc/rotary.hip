@@ -212,12 +212,24 @@ Frequencies frequencies(const kvs_rotary_spec &sp)
     return fr;
 }
 
-// the bytes that `n` rows of `row` elements touch, from the first to the last
-struct Span { uintptr_t lo, hi; };
-Span span_of(const void *p, int64_t n, int64_t stride, int64_t row, size_t size)
+// n rows of `row` bytes, `stride` bytes apart
+struct Slab { uintptr_t at; int64_t stride, row; };
+Slab slab_of(const void *p, int64_t stride, const Rows &x, int head_dim, size_t size)
 {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    return {a, a + (uintptr_t)(((n - 1) * stride + row) * (int64_t)size)};
+    return {reinterpret_cast<uintptr_t>(p), stride * (int64_t)size, (int64_t)x.heads * head_dim * (int64_t)size};
+}
+
+// Whether two of them have a byte in common.  With one stride that is exact: rows may lie beside each other in one buffer.  With two, what
+// lies between the other's first and last row is taken to.
+bool overlap(const Slab &a, const Slab &b, int64_t n)
+{
+    const uintptr_t a_end = a.at + (uintptr_t)((n - 1) * a.stride + a.row), b_end = b.at + (uintptr_t)((n - 1) * b.stride + b.row);
+    if (a_end <= b.at || b_end <= a.at) return false;
+    if (n == 1 || a.stride != b.stride) return true;
+    // row j of b begins d bytes behind row j + k of a, which exists for some j if -n < k < n
+    const int64_t apart = (int64_t)(b.at - a.at), k = apart >= 0 ? apart / a.stride : -((-apart + a.stride - 1) / a.stride), d = apart - k * a.stride;
+    auto exists = [n](int64_t rows) { return rows > -n && rows < n; };
+    return (d < a.row && exists(k)) || (d + b.row > a.stride && exists(k + 1));
 }
 
 kvs_status check_rows(const char *name, const Rows &x, int64_t n, int head_dim, size_t size)
@@ -230,9 +242,6 @@ kvs_status check_rows(const char *name, const Rows &x, int64_t n, int head_dim, 
                     (long long)x.out_stride, name, (long long)row, (long long)step);
     const int64_t most = x.in_stride > x.out_stride ? x.in_stride : x.out_stride;
     if (n > ((int64_t)1 << 46) / most) return fail(KVS_EINVAL, "kvs_rotary: %lld rows %lld elements apart", (long long)n, (long long)most);
-    const Span a = span_of(x.in, n, x.in_stride, row, size), b = span_of(x.out, n, x.out_stride, row, size);
-    if (a.lo < b.hi && b.lo < a.hi && !(x.in == x.out && x.in_stride == x.out_stride))
-        return fail(KVS_EINVAL, "kvs_rotary: %s_out overlaps %s without being in place", name, name);
     return KVS_OK;
 }
 
@@ -258,6 +267,18 @@ extern "C" kvs_status kvs_rotary(const kvs_shape *shape, const kvs_rotary_spec *
     for (int i = 0; i < 2; ++i) {
         if (!rows[i].in) { rows[i].heads = 0; continue; }
         if ((st = check_rows(i ? "k" : "q", rows[i], n_tokens, d, size)) != KVS_OK) return st;
+    }
+    const char *const names[2] = {"q", "k"};
+    for (int i = 0; i < 2; ++i) {
+        if (!rows[i].heads) continue;
+        const Slab out = slab_of(rows[i].out, rows[i].out_stride, rows[i], d, size);
+        for (int j = 0; j < 2; ++j) {
+            if (!rows[j].heads) continue;
+            const Slab in = slab_of(rows[j].in, rows[j].in_stride, rows[j], d, size), other = slab_of(rows[j].out, rows[j].out_stride, rows[j], d, size);
+            const bool in_place = i == j && in.at == out.at && (n_tokens == 1 || in.stride == out.stride);
+            if (!in_place && overlap(out, in, n_tokens)) return fail(KVS_EINVAL, "kvs_rotary: %s_out overlaps %s without being in place", names[i], names[j]);
+            if (i < j && overlap(out, other, n_tokens)) return fail(KVS_EINVAL, "kvs_rotary: %s_out overlaps %s_out", names[i], names[j]);
+        }
     }
     const Frequencies fr = frequencies(*spec);
     const int pairs = spec->rotary_dim / 2, e = 16 / (int)size, left = d - spec->rotary_dim;
