@@ -403,7 +403,7 @@ KVS_API kvs_status kvs_project_qkv(const kvs_shape *shape, int32_t hidden, const
  * pos             [dev] int32[n_tokens], any value        pos_from [dev] int32[n_tokens] or NULL (0: fresh rows)
  * q, q_out        [dev] n_tokens rows of n_q_heads * head_dim elements, q_stride and q_out_stride elements apart, each at
  *                 least a row long and a multiple of 16 bytes: a slice of a fused projection's buffer will do
- * k, k_out        the same with n_kv_heads.  q or k may be NULL (with its output), not both
+ * k, k_out        the same with n_kv_heads.  q or k may be NULL (with its output), not both; up to 4095 heads together
  * In place (the same pointer and stride) is allowed; an output may not overlap an input or output in any other way.  Rows may lie
  * beside each other in one buffer, slices of its columns, where their strides are the same; rows of another stride between a buffer's first
  * and last are refused.

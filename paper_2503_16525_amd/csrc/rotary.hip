@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = 64;
+constexpr int kMostHeads = 4095;      // of Q and K together
 constexpr int kMaxTokens = 32;        // tokens a workgroup takes at most: 16 KiB of sines and cosines
 
 struct Frequencies { double turns[kMaxPairs]; };   // per position
@@ -257,6 +258,8 @@ extern "C" kvs_status kvs_rotary(const kvs_shape *shape, const kvs_rotary_spec *
     kvs_status st = check_shape(shape);
     if (st != KVS_OK) return st;
     const int d = shape->head_dim;
+    // a token's cells, at most 16 a head, stay below 2^16 (Divisor)
+    if ((int64_t)shape->n_q_heads + shape->n_kv_heads > kMostHeads) return fail(KVS_EUNSUPPORTED, "kvs_rotary: more than %d heads", kMostHeads);
     if ((st = check_spec(spec, d)) != KVS_OK) return st;
     if (n_tokens < 0) return fail(KVS_EINVAL, "kvs_rotary: n_tokens < 0");
     if (n_tokens == 0) return KVS_OK;
