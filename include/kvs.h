@@ -390,8 +390,8 @@ KVS_API kvs_status kvs_project_qkv(const kvs_shape *shape, int32_t hidden, const
  *     KVS_ROTARY_PLAIN       f_j
  *     KVS_ROTARY_LINEAR      f_j / factor                         (position interpolation)
  *     KVS_ROTARY_NTK         base * factor^(rotary_dim / (rotary_dim - 2)) in place of base; rotary_dim > 2
- *     KVS_ROTARY_RAMP        f_j (1 - w) + f_j / factor * w, w rising from 0 to 1 over the pairs from floor(at(high)) to
- *                            ceil(at(low)), at(t) = rotary_dim * ln(original / (2 pi t)) / (2 ln base): pairs that turn more
+ *     KVS_ROTARY_RAMP        f_j (1 - w) + f_j / factor * w, w rising from 0 to 1 over the pairs from floor(at(high)), at least 0,
+ *                            to ceil(at(low)), at most rotary_dim - 1, at(t) = rotary_dim * ln(original / (2 pi t)) / (2 ln base): pairs that turn more
  *                            than `high` times within the original length keep their frequency, those under `low` turns are
  *                            interpolated (YaRN, arXiv 2309.00071; its magnitude 0.1 ln(factor) + 1 is the caller's)
  *     KVS_ROTARY_WAVELENGTH  f_j w + f_j / factor * (1 - w), w rising from 0 to 1 with the turns original * f_j / (2 pi)
@@ -472,8 +472,10 @@ typedef struct {
  *     scale = max(need, old scale), or need alone if all of the block's rows in the cache are taken
  *     code  = nearest code (ties to even) to x * (1 / scale)      for the rows taken
  *     code  = nearest code to code * (old scale / scale)          for the other rows, where the scale has changed
- * Kept rows are therefore rounded again only when a larger value comes into their block.  If one of the rows taken holds
- * a NaN or infinity, or a row is kept and the old scale is NaN, the scale becomes NaN.
+ * Kept rows are therefore rounded again only when a larger value comes into their block, by half a step at most each time: a block of
+ * normal values that is filled a row at a time ends 1.1 to 1.4 times as far from its rows, in norm, as one stored at once (2 to 5
+ * growths), one whose rows grow 17-fold over it 2.4 times (28).  If one of the rows taken holds a NaN or infinity, or a row is kept
+ * and the old scale is NaN, the scale becomes NaN.
  *
  * k_new, v_new  [dev] [n_sel, n_kv_heads, head_dim] in the shape's dtype
  * reused, dev_v [dev] uint8[n_rows], fp32[n_kv_heads, n_rows], each may be NULL: cleared for the rows taken, as in

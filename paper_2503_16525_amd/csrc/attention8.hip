@@ -15,12 +15,13 @@
 // waves take the same 32 rows and every fourth tile, each with LDS slots of its own that its loads go to directly
 // (global to LDS, 16 bytes a lane, no registers), two tiles deep and without a barrier; at the end the waves meet in LDS.
 // Launches of too few workgroups cut the key ranges into pieces, which a second kernel merges.  (One row of 8 query heads each over
-// 131072 keys of 4 KV heads: 30 us and 4.4 for the merge, 4.5 TB/s in the first; 64 contexts of 4096 to 16384, 8 KV heads: 270 us,
-// 5.0 TB/s.)
+// 131072 keys of 4 KV heads: 30 us and 4.4 for the merge, 4.5 TB/s in the first; 64 contexts of 4096 to 16384, 8 KV heads: 265 us,
+// 5.1 TB/s.)
 //
-// With many rows the vector instructions do: a tile's 215 (e4m3: 64 conversions, 16 exponentials, 16 fused multiply-adds, and
-// 8 comparisons more where it is masked) beside 16 matrix instructions.  int8 has no conversion of its own and takes 128 more.  (800
-// rows of 32 query heads over 16000 keys: 172 us, 0.61 PFLOP/s of what the rows see.)
+// With many rows the vector instructions do: a tile's 224 (e4m3: 64 conversions, 16 exponentials, 16 fused multiply-adds, and
+// 8 comparisons more where it is masked; a wave's beginning and end in it, at 64 tiles a wave) beside 16 matrix instructions.  int8 has no
+// conversion of its own and takes 128 more.  (800 rows of 32 query heads over 16000 keys: 153 to 172 us by box, 0.69 to 0.61 PFLOP/s of
+// what the rows see; vector pipes busy 55 % of it, matrix pipes 27.)
 //
 // A lane's V operand is 8 keys of one channel, but a row of codes lies along the channels: the LDS reads that transpose
 // bytes among 16 lanes give it those (64 bits a lane, from 8 rows of 16 bytes).
@@ -40,7 +41,7 @@ constexpr int kRows = 32;              // rows of a unit
 constexpr int kKeys = 32;              // keys of a tile
 constexpr int kAlign = 16;             // cache rows that tiles are aligned to: no block is shorter
 constexpr float kSlack = 8.f;          // powers of two that a score may lie above its reference
-constexpr int kMinPieceTiles = 4;      // tiles of a piece: one for each wave (with two, one row of 600 keys of 8 heads 10.1 us instead of 8.1, 4000 keys 9.8 and 8.6)
+constexpr int kMinPieceTiles = 4;      // tiles of a piece: one for each wave (with two, one row of 600 keys of 8 heads 9.9 us instead of 8.0, 4000 keys 9.9 and 8.6, in a graph)
 constexpr int kMaxPieces = 512;
 constexpr int64_t kMaxCutWgs = 2048;   // workgroups at most where key ranges are cut: four for every place on the chip
 
@@ -501,7 +502,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention8_kernel(
 // out = sum_p w_p O_p / sum_p w_p l_p with w_p = 2^(m_p - max m).  A workgroup takes 32 channels of one row: its threads make the
 // pieces' weights once, into LDS, then groups of 8 threads take every 32nd piece, four channels a thread, and meet by shuffles and in LDS.
 // (A wave a row, piece after piece, spent its time on one round trip to memory after the other: 256 pieces 80 us; a workgroup
-// for all channels of a row took 5.7 us for 74 pieces of 32 rows, this 4.5.)
+// for all channels of a row took 5.7 us for 74 pieces of 32 rows, this 4.5; 114 pieces of 32 rows 4.4.)
 template <int DTYPE, int D>
 __global__ __launch_bounds__(kThreads) void merge8_kernel(const Table td, int n_q_heads, const float *__restrict__ part_o,
                                                           const float4 *__restrict__ part_ml, void *__restrict__ out, float *__restrict__ lse_out)

@@ -14,8 +14,11 @@ namespace kvs {
 namespace {
 
 constexpr int kThreads = 256;
-// Tokens of a workgroup's tile: 32 cells at least, two a lane.  V of 32768 tokens of 8 heads 18.5 us with 4, 19.3 with 8 or 16, 18.5
-// with 32; 12000 of them 9.0, 9.2 and with 32 14.9; 131072 of 4 heads 42 with 4, 34 with 8 or 16, 35 with 32.
+// Tokens of a workgroup's tile: 8, from 8 heads on 4, which are 32 cells and two a lane.  V in bf16, tiles of 4 and 8 (and 16): 131072 tokens of 1
+// head 28.4 and 16.9 us (11.2), 2 heads 31.3 and 19.9 (18.0), 3 heads 33.8 and 27.2 (25.6), 4 heads 37.0 and 31.5 (32.6); 65536 of 5
+// heads 25.2 and 22.7, 6 heads 27.3 and 25.6, 7 heads 29.4 and 30.4, 8 heads 31.8 and 32.8; 32768 of 12 heads 26.1 and 25.8, 16
+// heads 33.3 and 34.1, 32 heads 62.7 and 62.9; 12000 of 8 heads 9.2 and 9.6 (9.9, with 32 14.6); 8192 of 16 heads 11.7 and 11.4
+// (15.2).  Above 8 heads either would do, and larger tiles leave units idle in short launches.
 constexpr int kTok = 8, kTokMany = 4, kManyHeads = 8;
 
 struct DevArgs {

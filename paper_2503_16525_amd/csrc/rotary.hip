@@ -11,7 +11,8 @@
 // by multiplications, and a thread has one cell at a time: with divisions and two cells, 131072 rows of 4 heads took 74 us instead
 // of 52 to 54, which is what a copy of their bytes takes; 8192 rows of 32 + 8 heads 39 instead of 30 (5.5 TB/s; 34 with ordinary loads).
 // Both layouts need rotary_dim to be a multiple of two cells' channels (16 in bf16, 8 in fp32); other sizes go to a
-// kernel that takes one pair a thread.
+// kernel that takes one pair a thread and makes its angle for every head anew: 8192 rows of 32 + 8 heads with 100 channels turned 92 us, with 2 to 36
+// of them 117 to 125, where cells take 29 to 35.  Turned parts of such sizes are rare, and the kernel is kept short.
 #include "kvs_internal.h"
 
 #include <math.h>

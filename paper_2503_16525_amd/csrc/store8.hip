@@ -7,17 +7,18 @@
 // Rows in a row (no list): a workgroup has one block and its share of the units, a unit being one KV head of K or of V.  A wave
 // holds up to 32 rows of a unit, so a unit takes a team of 1, 2 or 4 waves (`waves`), which meet in LDS for their maximum.
 //
-// A list: its entries of one block, and skipped ones between them, are a run.  A wave has a few entries of the list, finds the runs that begin there from one
-// load of the positions, and takes 64 pieces of the rows of each, 4 heads of 256 bytes; no wave waits for another.  Skipped entries
-// end no run: the wave of the last one before a stretch of them looks through it (0.9 us for 512 entries; 1000 rows and 3096 of them 11.1 us, 10.1 where
-// they ended it), and the wave that begins behind it looks back.  Which entry a
-// row takes is settled in LDS: the highest that names it, whatever order the entries of a block come in.  A lane has the same
+// A list: its entries of one block, and skipped ones between them, are a run.  A wave has a few entries of the list, finds the runs
+// that begin there from one load of the positions, and takes 64 pieces of the rows of each, 4 heads of 256 bytes; no wave waits
+// for another.  Skipped entries end no run: the wave of the last one before a stretch of them looks through it (0.9 us for 512
+// entries; 1000 rows 8.0 us, with 3096 skipped entries behind them 10.8), and the wave that begins behind it looks back.  Which
+// entry a row takes is settled in LDS: the highest that names it, whatever order the entries of a block come in.  A lane has the same
 // piece of up to 8 rows: its maximum runs over the rows first, then over the lanes of its head (no exchange beyond 16 lanes), and the
 // scale is made in every lane that needs it.  What a wave waits for is one trip to memory for the positions, one for the rows
 // and old scales, and where a scale grows one or two for the codes that it rounds again, head by head with all lanes.  (4424 of 32768
 // rows of 8 heads, blocks of 32: a workgroup for each entry 35.6 us, a chunk of the list and one unit a workgroup 25.8, a wave a run
-// with whole heads one after the other 20, issue bound; this 12.5, with loads that do not stay in the caches 14.6; where scales grow 15.5, with
-// the rows rounded again for all heads of the wave at once 19.7.  One row in each of 64 blocks 3.7, in blocks of 128 whose scales grow 11, 31 so.)
+// with whole heads one after the other 20, issue bound; this 13.6 in a trace, 13.0 in a full queue.  The first time over a filled
+// cache, where 2 % of the scales grow, 18 to 21; where all grow 41, of which the codes' 134 MB would take 26 at a copy's rate.  One
+// row in each of 64 blocks of 32 4.0, in blocks of 128 whose scales all grow 39: 128 rows of 8 heads, one head after the other.)
 #include "cache8.h"
 
 #include <math.h>
