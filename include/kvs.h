@@ -534,11 +534,134 @@ KVS_API kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8 *c
                                      void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * A KV cache in pages.  The pool holds n_pages pages of `page` rows; row i of request b is row i % page of page
+ * table[b, i / page].  A page is laid out as the rows of the other calls are, so the pool is also a cache of n_pages * page rows
+ * that kvs_scatter_kv and the others take.  Requests may share pages (a prefix, or whatever else was reused).
+ *
+ * The page table and the lengths are read on the device, when the kernels run: a captured call can be replayed after they have
+ * changed.  max_ctx is what the host promises about them: no context is longer.  Launches are sized by it, so it should not be
+ * far above; of a longer context the first max_ctx rows are taken, and of one longer than the table is wide what the table
+ * names.  A negative length is 0.  An entry of the table outside [0, n_pages) names no page: its rows are not stored to, seen or
+ * copied.  Entries behind a context's last page are not used.
+ *
+ * Tokens of a call belong to the requests in order: those of request b are [cu_new[b], cu_new[b+1]) (device memory, at
+ * least 0, non-decreasing, at most n_new; offsets that break this give unspecified results, and no access outside the tensors).
+ * Tokens outside [cu_new[0], cu_new[batch]) belong to none: nothing of theirs is read or written, so a captured call may hold
+ * more places than tokens.  cu_new == NULL: one token a request (n_new == batch).  Token i of a request's n stands at position
+ * sel_pos[cu_new[b] + i], or, with sel_pos == NULL, at ctx_len[b] - n + i: the context's last rows.  A negative position sees
+ * nothing; one behind the context sees what its last row sees.
+ *
+ * Everything is in the shape's dtype, bf16 or fp32; head_dim 64 or 128, up to 64 KV heads and 4096 query heads.
+ */
+typedef struct {
+    void *k, *v;            /* [dev] [n_pages, page, n_kv_heads, head_dim], 16-byte aligned */
+    int64_t n_pages;
+    int32_t page;           /* 16, 32, 64, 128 or 256 rows */
+} kvs_paged_cache;
+
+typedef struct {
+    const int32_t *table;   /* [dev] [batch, width] page ids */
+    const int32_t *ctx_len; /* [dev] [batch] rows of each request, new tokens' among them */
+    int64_t max_ctx;
+    int32_t batch, width;
+} kvs_page_table;
+
+/*
+ * kvs_store_paged -- rows of K and V into the pages of their requests: a chunk of a prompt, a decode step's new rows, or
+ * recomputed rows in place of reused ones.
+ *
+ * Token s goes to its position (above); tokens whose position is negative or behind the context are skipped.  Where neighbouring
+ * tokens of a request have the same position the last one counts (an ascending list may repeat itself); the same position further
+ * apart, and one row of the pool reached through two requests, are a race.
+ *
+ * k_new, v_new [dev] [n_new, n_kv_heads, head_dim]
+ * mass         [dev] fp32 [batch, n_kv_heads, mass_stride] or NULL: set to 0 at the positions stored to (kvs_mass_paged;
+ *              mass_stride at least max_ctx)
+ */
+KVS_API kvs_status kvs_store_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages,
+                                   const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new,
+                                   const void *k_new, const void *v_new, float *mass, int64_t mass_stride, void *stream);
+
+/*
+ * kvs_attention_paged -- kvs_partial_attention over a cache in pages: a chunk of new tokens, selected ones, or a decode
+ * step's single ones, all in one call if they come together.
+ *
+ * The row of a token at position p sees row i of its request if i <= p and (window == 0 or i > p - window or i < n_first): all
+ * that is before it, or a window that ends with it beside the first n_first rows.  Rows that a window leaves out are not read.
+ *   out[s,h,:] = sum_i softmax_i( scale * q_new[s,h,:] . K[i, g(h), :] ) * V[i, g(h), :]
+ *   lse[s,h]   = log sum_i exp( scale * q . K_i )                 (natural log; optional)
+ * A token that sees nothing gets 0 and -inf.  What a row does not see does not reach it, whatever it holds (NaN and
+ * infinities too).
+ *
+ * q_new, out [dev] [n_new, n_q_heads, head_dim]      lse_out [dev] fp32[n_new, n_q_heads] or NULL
+ * scale      any finite number
+ * workspace  [dev] optional (NULL / 0 is valid), 256-byte aligned, kvs_workspace_size("attention_paged", shape, batch,
+ *            max_ctx, n_new) bytes: launches that would leave units idle cut their key ranges into pieces and merge them.  Less
+ *            means fewer pieces.  One call's until that call has ended on its stream.
+ * bf16: fp32 accumulation and softmax; the weights enter the second product as two bf16 numbers that hold 16 of their bits where
+ * there are no more than 32 rows (tokens times query heads of a KV head) a request on average, rounded to one elsewhere.  fp32
+ * throughout otherwise.  Equal calls give equal bits.
+ */
+KVS_API kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages,
+                                       const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new, const void *q_new, float scale,
+                                       int32_t window, int32_t n_first, void *out, float *lse_out,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * kvs_mass_paged -- the attention that every cached row receives, added up over calls: what Alg. 1 takes as alpha
+ * (kvs_attn_colsum), for a cache that is filled in chunks and read by decode steps.
+ *
+ *   mass_out[b,g,i] = decay * mass[b,g,i] + sum over the tokens s of request b that see row i (window and n_first as above) and the
+ *                     query heads h of KV head g of exp( scale * q_new[s,h,:] . K[i,g,:] - lse[s,h] )
+ *
+ * for every row i of the contexts; entries behind them stay as they are.  lse is what kvs_attention_paged has given for the
+ * same tokens: then every token adds 1 for each query head, spread over the rows it saw.
+ *
+ * lse            [dev] fp32[n_new, n_q_heads]
+ * decay          finite, at least 0
+ * mass, mass_out [dev] fp32 [batch, n_kv_heads, mass_stride], mass_stride at least max_ctx.  mass may be mass_out, or NULL (zeros); they
+ *                may not overlap otherwise
+ * workspace      [dev] optional, 256-byte aligned, kvs_workspace_size("mass_paged", shape, batch, max_ctx, n_new) bytes:
+ *                chunks over short contexts cut their rows into pieces and add them up
+ * fp32 sums in a fixed order (bit-reproducible for equal workspaces); bf16 products are accumulated in fp32.
+ */
+KVS_API kvs_status kvs_mass_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages,
+                                  const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new, const void *q_new, const float *lse, float scale,
+                                  int32_t window, int32_t n_first, float decay, const float *mass, float *mass_out, int64_t mass_stride,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * kvs_evict_paged -- contexts that have grown too long, cut down to the rows that received most attention.
+ *
+ * Request b keeps m = min(ctx_len[b], keep[b], max_keep) rows (none for a negative keep[b]):
+ *   the first f = min(n_first, m), the last r = min(n_recent, m - f), and of the others the m - f - r with the largest
+ *   mass[b,0,i] + mass[b,1,i] + ... (fp32, in the order of the KV heads), ties to the lower index; NaN ranks below all numbers, -0 equals 0.
+ * They are copied, in order, to the pages of new_table: row j of them to row j % page of page new_table[b, j / page].  Pages that
+ * requests share stay as they are: a request takes pages of its own for what it keeps, and gives back its old ones.  The two
+ * tables' pages in use may not overlap (rows would be overwritten before they are read).  The rest of a last page stays as it was.
+ *
+ * keep      [dev] int32[batch]
+ * max_keep  what the host promises about keep, as max_ctx
+ * mass      [dev] fp32 [batch, n_kv_heads, mass_stride], mass_stride at least max_ctx
+ * new_table [dev] int32[batch, new_width], new_width pages holding at least max_keep rows; NULL: nothing is copied.  Entries outside
+ *           [0, n_pages) take nothing
+ * kept      [dev] int32[batch, max_keep] or NULL: the kept rows' positions, ascending; entries from m on stay as they are
+ * new_len   [dev] int32[batch] or NULL: m.  May be ctx_len
+ * new_mass  [dev] fp32 [batch, n_kv_heads, max_keep] or NULL: the kept rows' mass; entries from m on stay as they are.  No overlap with mass
+ * workspace [dev] kvs_workspace_size("evict_paged", shape, batch, max_ctx, 0) bytes, 256-byte aligned, required
+ * Exact and deterministic.
+ */
+KVS_API kvs_status kvs_evict_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages,
+                                   const int32_t *keep, int64_t max_keep, int32_t n_first, int32_t n_recent, const float *mass, int64_t mass_stride,
+                                   const int32_t *new_table, int32_t new_width, int32_t *kept, int32_t *new_len, float *new_mass,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Workspace a call needs, in bytes, for the given problem.  `call` is "select_topk",
- * "partial_attention", "decode_check", "attn_colsum", "first_order_impact", "match_tokens" or "attention_kv8" (anything else
- * returns 0).  n_rows_total is the total number of score / cache rows the call will see (match_tokens: the
+ * "partial_attention", "decode_check", "attn_colsum", "first_order_impact", "match_tokens", "attention_kv8", "attention_paged", "mass_paged" or
+ * "evict_paged" (anything else returns 0).  n_rows_total is the total number of score / cache rows the call will see (match_tokens: the
  * target's tokens), n_sel_total the total number of selected tokens (partial_attention, attention_kv8) or the candidate's
- * tokens (match_tokens, which ignores shape: it may be NULL there).  The answer is an upper bound valid for any split of the
+ * tokens (match_tokens, which ignores shape: it may be NULL there).  The paged calls take max_ctx as n_rows_total and n_new as n_sel_total.  The answer is an upper bound valid for any split of the
  * totals over `batch` requests, and does not shrink as the totals grow.
  */
 KVS_API size_t kvs_workspace_size(const char *call, const kvs_shape *shape, int32_t batch,

@@ -27,7 +27,8 @@ E4M3, INT8 = 0, 1
 
 EXPORTS = ("kvs_deviation", "kvs_deviation_topk", "kvs_select_topk", "kvs_select_topk_static", "kvs_scatter_kv", "kvs_partial_attention",
            "kvs_decode_check", "kvs_attn_colsum", "kvs_first_order_impact", "kvs_match_tokens", "kvs_project_qkv",
-           "kvs_rotary", "kvs_store_kv8", "kvs_deviation_kv8", "kvs_attention_kv8", "kvs_workspace_size", "kvs_strerror", "kvs_last_error", "kvs_version")
+           "kvs_rotary", "kvs_store_kv8", "kvs_deviation_kv8", "kvs_attention_kv8", "kvs_store_paged", "kvs_attention_paged", "kvs_mass_paged",
+           "kvs_evict_paged", "kvs_workspace_size", "kvs_strerror", "kvs_last_error", "kvs_version")
 
 
 class KvsError(RuntimeError):
@@ -50,6 +51,15 @@ class RotarySpec(ctypes.Structure):
 class _Cache8(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_rows", ctypes.c_int64), ("block", ctypes.c_int32), ("code", ctypes.c_int32)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page", ctypes.c_int32)]
+
+
+class _PageTable(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("ctx_len", ctypes.c_void_p), ("max_ctx", ctypes.c_int64), ("batch", ctypes.c_int32),
+                ("width", ctypes.c_int32)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -84,10 +94,16 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.kvs_store_kv8.argtypes = [sp, cp, vp, vp, vp, i64, i64, vp, vp, vp]
     lib.kvs_deviation_kv8.argtypes = [sp, cp, i64, i64, vp, vp, vp, vp, i32, vp, vp, vp, vp]
     lib.kvs_attention_kv8.argtypes = [sp, cp, i32, vp, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]
+    pp, tp = ctypes.POINTER(_PagedCache), ctypes.POINTER(_PageTable)
+    lib.kvs_store_paged.argtypes = [sp, pp, tp, vp, vp, i64, vp, vp, vp, i64, vp]
+    lib.kvs_attention_paged.argtypes = [sp, pp, tp, vp, vp, i64, vp, f32, i32, i32, vp, vp, vp, sz, vp]
+    lib.kvs_mass_paged.argtypes = [sp, pp, tp, vp, vp, i64, vp, vp, f32, i32, i32, f32, vp, vp, i64, vp, sz, vp]
+    lib.kvs_evict_paged.argtypes = [sp, pp, tp, vp, i64, i32, i32, vp, i64, vp, i32, vp, vp, vp, vp, sz, vp]
     lib.kvs_workspace_size.argtypes = [ctypes.c_char_p, sp, i32, i64, i64]
     for n in ("kvs_deviation", "kvs_deviation_topk", "kvs_select_topk", "kvs_select_topk_static", "kvs_scatter_kv", "kvs_partial_attention",
               "kvs_decode_check", "kvs_attn_colsum", "kvs_first_order_impact", "kvs_match_tokens", "kvs_project_qkv",
-              "kvs_rotary", "kvs_store_kv8", "kvs_deviation_kv8", "kvs_attention_kv8"):
+              "kvs_rotary", "kvs_store_kv8", "kvs_deviation_kv8", "kvs_attention_kv8", "kvs_store_paged", "kvs_attention_paged",
+              "kvs_mass_paged", "kvs_evict_paged"):
         getattr(lib, n).restype = ctypes.c_int
     lib.kvs_workspace_size.restype = sz
     lib.kvs_strerror.argtypes = [ctypes.c_int]
@@ -431,6 +447,132 @@ def kvs_attention_kv8(shape: Shape, cache: Cache8, ctx_off: Sequence[int], ctx_l
                                   _at(lse_out, dev, torch.float32, heads, "lse_out"), ws, ws_bytes, _stream(stream))
     if rc:
         _check(rc, "kvs_attention_kv8")
+
+
+class PagedCache:
+    """A pool of pages: k, v [pages, rows of a page, KV heads, head_dim] (torch.bfloat16 or torch.float32)."""
+
+    def __init__(self, k, v):
+        if k.dtype not in _TYPES.values() or v.dtype is not k.dtype:
+            raise TypeError(f"k and v are torch.bfloat16 or torch.float32, not {k.dtype}, {v.dtype}")
+        if k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("k and v are [pages, rows of a page, KV heads, head_dim], of one shape")
+        self.k, self.v = k, v
+        self.n_pages, self.page, self.n_kv_heads, self.head_dim = k.shape
+        self.dtype, self.device = k.dtype, k.get_device()
+        if v.get_device() != self.device:
+            raise ValueError("the cache's tensors are on one device")
+        self.raw = _PagedCache(_ptr(k), _ptr(v), self.n_pages, self.page)
+
+    @classmethod
+    def empty(cls, shape: Shape, n_pages: int, page: int, device="cuda") -> "PagedCache":
+        """A pool whose rows hold nothing yet (zeros)."""
+        return cls(*(torch.zeros((n_pages, page, shape.n_kv_heads, shape.head_dim), dtype=_type(shape), device=device) for _ in range(2)))
+
+
+class PageTable:
+    """Where the requests' rows are: table int32 [requests, pages], ctx_len int32 [requests], both on the device and read when the
+    kernels run; max_ctx: no context is longer (None: as long as the table is wide, for pages of `page` rows)."""
+
+    def __init__(self, table, ctx_len, max_ctx: Optional[int] = None, page: int = 0):
+        if table.dim() != 2 or ctx_len.shape != (table.shape[0],):
+            raise ValueError("table is [requests, pages], ctx_len [requests]")
+        if max_ctx is None:
+            if page <= 0:
+                raise ValueError("without max_ctx the rows of a page are needed")
+            max_ctx = table.shape[1] * page
+        self.table, self.ctx_len, self.max_ctx = table, ctx_len, max_ctx
+        self.batch, self.width = table.shape
+        self.device = table.get_device()
+        if ctx_len.get_device() != self.device:
+            raise ValueError("the table and the lengths are on one device")
+        self.raw = _PageTable(_ptr(table, torch.int32), _ptr(ctx_len, torch.int32), max_ctx, self.batch, self.width)
+
+
+def _paged(cache: PagedCache, pages: PageTable, shape: Shape, dev: int):
+    if cache.n_kv_heads != shape.n_kv_heads or cache.head_dim != shape.head_dim:
+        raise ValueError(f"the cache has {cache.n_kv_heads} KV heads of {cache.head_dim}, the shape {shape.n_kv_heads} of {shape.head_dim}")
+    if cache.dtype is not _type(shape):
+        raise TypeError(f"the cache holds {cache.dtype}, the shape says {_type(shape)}")
+    if cache.device != dev or pages.device != dev:
+        raise ValueError(f"the cache is on device {cache.device}, the page table on {pages.device}, the current device is {dev}")
+    return cache.raw, pages.raw
+
+
+def _mass_at(mass, pages: PageTable, shape: Shape, dev: int, what: str, stride: Optional[int] = None):
+    """Address and stride of fp32 [requests, KV heads, stride]."""
+    if mass is None:
+        return None, 0
+    if mass.dim() != 3 or mass.shape[:2] != (pages.batch, shape.n_kv_heads) or (stride is not None and mass.shape[2] != stride):
+        raise ValueError(f"{what}: expected {(pages.batch, shape.n_kv_heads, 'rows' if stride is None else stride)}, got {tuple(mass.shape)}")
+    return _at(mass, dev, torch.float32, 0, what), mass.shape[2]
+
+
+def _bytes_at(workspace, dev: int):
+    if workspace is None:
+        return None, 0
+    return _at(workspace, dev, workspace.dtype, 0, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def kvs_store_paged(shape: Shape, cache: PagedCache, pages: PageTable, cu_new, sel_pos, k_new, v_new, mass=None, stream=None) -> None:
+    n, dev, dt = k_new.shape[0], _device(), _type(shape)
+    cells = n * shape.n_kv_heads * shape.head_dim
+    craw, praw = _paged(cache, pages, shape, dev)
+    mp, ms = _mass_at(mass, pages, shape, dev, "mass")
+    rc = load().kvs_store_paged(shape, craw, praw, _at(cu_new, dev, torch.int32, pages.batch + 1, "cu_new"), _at(sel_pos, dev, torch.int32, n, "sel_pos"), n,
+                                _at(k_new, dev, dt, cells, "k_new"), _at(v_new, dev, dt, cells, "v_new"), mp, ms, _stream(stream))
+    if rc:
+        _check(rc, "kvs_store_paged")
+
+
+def kvs_attention_paged(shape: Shape, cache: PagedCache, pages: PageTable, cu_new, sel_pos, q_new, scale: float, window: int, n_first: int, out,
+                        lse_out=None, workspace=None, stream=None) -> None:
+    n, dev, dt = q_new.shape[0], _device(), _type(shape)
+    heads = n * shape.n_q_heads
+    cells = heads * shape.head_dim
+    craw, praw = _paged(cache, pages, shape, dev)
+    ws, ws_bytes = _bytes_at(workspace, dev)
+    rc = load().kvs_attention_paged(shape, craw, praw, _at(cu_new, dev, torch.int32, pages.batch + 1, "cu_new"), _at(sel_pos, dev, torch.int32, n, "sel_pos"), n,
+                                    _at(q_new, dev, dt, cells, "q_new"), scale, window, n_first, _at(out, dev, dt, cells, "out"),
+                                    _at(lse_out, dev, torch.float32, heads, "lse_out"), ws, ws_bytes, _stream(stream))
+    if rc:
+        _check(rc, "kvs_attention_paged")
+
+
+def kvs_mass_paged(shape: Shape, cache: PagedCache, pages: PageTable, cu_new, sel_pos, q_new, lse, scale: float, window: int, n_first: int, decay: float,
+                   mass, mass_out, workspace=None, stream=None) -> None:
+    n, dev, dt = q_new.shape[0], _device(), _type(shape)
+    heads = n * shape.n_q_heads
+    craw, praw = _paged(cache, pages, shape, dev)
+    op, ms = _mass_at(mass_out, pages, shape, dev, "mass_out")
+    ip, _ = _mass_at(mass, pages, shape, dev, "mass", ms)
+    ws, ws_bytes = _bytes_at(workspace, dev)
+    rc = load().kvs_mass_paged(shape, craw, praw, _at(cu_new, dev, torch.int32, pages.batch + 1, "cu_new"), _at(sel_pos, dev, torch.int32, n, "sel_pos"), n,
+                               _at(q_new, dev, dt, heads * shape.head_dim, "q_new"), _at(lse, dev, torch.float32, heads, "lse"), scale, window, n_first, decay,
+                               ip, op, ms, ws, ws_bytes, _stream(stream))
+    if rc:
+        _check(rc, "kvs_mass_paged")
+
+
+def kvs_evict_paged(shape: Shape, cache: PagedCache, pages: PageTable, keep, n_first: int, n_recent: int, mass, new_table, kept=None, new_len=None,
+                    new_mass=None, workspace=None, max_keep: Optional[int] = None, stream=None) -> None:
+    """max_keep: what the host promises about `keep`; None: kept's or new_mass's columns, or as many rows as new_table holds."""
+    dev = _device()
+    craw, praw = _paged(cache, pages, shape, dev)
+    if max_keep is None:
+        max_keep = kept.shape[1] if kept is not None else new_mass.shape[2] if new_mass is not None else new_table.shape[1] * cache.page if new_table is not None else pages.max_ctx
+    if new_table is not None and (new_table.dim() != 2 or new_table.shape[0] != pages.batch):
+        raise ValueError(f"new_table: expected [{pages.batch}, pages], got {tuple(new_table.shape)}")
+    if kept is not None and tuple(kept.shape) != (pages.batch, max_keep):
+        raise ValueError(f"kept: expected {(pages.batch, max_keep)}, got {tuple(kept.shape)}")
+    mp, ms = _mass_at(mass, pages, shape, dev, "mass")
+    np_, _ = _mass_at(new_mass, pages, shape, dev, "new_mass", max_keep)
+    ws, ws_bytes = _bytes_at(workspace, dev)
+    rc = load().kvs_evict_paged(shape, craw, praw, _at(keep, dev, torch.int32, pages.batch, "keep"), max_keep, n_first, n_recent, mp, ms,
+                                _at(new_table, dev, torch.int32, 0, "new_table"), new_table.shape[1] if new_table is not None else 0,
+                                _at(kept, dev, torch.int32, 0, "kept"), _at(new_len, dev, torch.int32, pages.batch, "new_len"), np_, ws, ws_bytes, _stream(stream))
+    if rc:
+        _check(rc, "kvs_evict_paged")
 
 
 def shape_of(workload) -> Shape:

@@ -1,0 +1,658 @@
+// kvs_attention_paged: attention of new or selected tokens over a cache in pages, with an optional sliding window beside a few first
+// tokens that stay visible.
+//
+// Mathematics.  out = sum_i p_i v_i / sum_i p_i with p_i = exp(scale q . k_i - max) over the keys that the row sees: one pass
+// over the keys with a running maximum and sum.
+//
+// Tiles.  A wave takes 32 rows (the query heads of one KV head flattened with the tokens) against tiles of 32 keys, S^T = K Q^T and
+// O^T += V^T P^T, so that P stays in registers as the operand of the second product.  A tile is two runs of 16 rows, each in
+// one page; the wave's next 32 tiles' places are kept in its lanes, two a tile, and read from them without a trip to memory.
+// Under a window a row block's tiles are those of the first tokens and those from its lowest row's window on; the others are
+// not counted, loaded or computed.
+//
+// The four waves of a workgroup take the same 32 rows and every fourth tile, each with an LDS slot for K and one for V that its
+// loads go to directly (global to LDS, 16 bytes a lane, no registers), without a barrier: K of the next tile is asked for once
+// this tile's has been read, V likewise, so that a tile's worth of loads is under way all the time, and two workgroups share a CU.
+// At the end the waves meet in LDS.  Launches of too few workgroups cut the keys into pieces, which a second kernel merges.
+//
+// fp32 goes through the fp32 matrix instruction, whose operands need no other order than that of memory.
+#include "paged.h"
+
+#include <math.h>
+
+namespace kvs {
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
+
+constexpr int kWaves = 4, kThreads = kWaves * kWave;
+constexpr int kRows = 32;              // rows of a block
+constexpr int kKeys = 32;              // keys of a tile
+constexpr float kSlack = 8.f;          // powers of two that a score may lie above its reference
+constexpr int kMaxPieces = 512;
+constexpr int kPlaces = 512;           // workgroups that the chip holds at once
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4_t v) { return __builtin_bit_cast(bf16x8, v); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    f32x2 f = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+}
+
+__device__ __forceinline__ float max_of_halves(float x)      // of lanes i and i + 32
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// PARTS: bf16 numbers that a weight enters the second product as: one, or two that hold 16 of its bits
+template <int DTYPE, int D, int PARTS>
+__global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
+    const Paged pg, int n_q_heads, int n_kv_heads, int units, int pieces, int piece_tiles,
+    const char *__restrict__ k_pool, const char *__restrict__ v_pool, const void *__restrict__ q_new, float scale_log2,
+    void *__restrict__ out, float *__restrict__ lse_out, float *__restrict__ part_o, float4 *__restrict__ part_ml)
+{
+    constexpr bool F32 = DTYPE == KVS_F32;
+    constexpr int ES = F32 ? 4 : 2;
+    constexpr int NDB = D / 32;
+    constexpr int ROW_B = D * ES;
+    constexpr int CPR = ROW_B / 16;                          // 16-byte chunks of a row
+    constexpr int RPL = kWave / CPR;                         // rows a load moves
+    constexpr int NH = kGranule / RPL;                       // loads of half a tile
+    constexpr int NL = 2 * NH;
+    constexpr int TILE_B = kKeys * ROW_B;
+    constexpr int WAVE_B = 2 * TILE_B;                       // a slot for K, one for V
+    constexpr int MEET_B = kRows * D * 4;                    // the wave's sums at the end
+    static_assert(MEET_B <= WAVE_B, "the sums take the slots' place");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float4 ml_s[kWaves][kRows];
+    __shared__ int odd_s;
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hf = lane >> 5, ln = lane & 31;
+
+    // Workgroup = (piece, block, KV head), KV heads side by side: their rows of the cache are neighbours.  A piece's blocks come
+    // together, which share its keys in L2.
+    const int g = (int)(blockIdx.x % (uint32_t)n_kv_heads);
+    const int rest = (int)(blockIdx.x / (uint32_t)n_kv_heads);
+    const int piece = rest / units;
+    const int grp = n_q_heads / n_kv_heads;
+    int b, blk;
+    if (!find_block<kRows>(pg, grp, rest - piece * units, b, blk)) return;
+    b = __builtin_amdgcn_readfirstlane(b);
+    blk = __builtin_amdgcn_readfirstlane(blk);
+    int tok0, n_tok;
+    tokens_of(pg, b, tok0, n_tok);
+    const int len = len_of(pg, b);
+    const int rows = n_tok * grp;
+
+    // ---- this lane's row (both half-waves hold the same 32) ------------------------------------------------
+    const int rq = min(blk * kRows + ln, rows - 1);
+    const int t_own = rq / grp, hh = rq - t_own * grp;
+    const int pos = position_of(pg, tok0, n_tok, t_own, len);
+    int pmin = pos, pmax = pos, plow = pos < 0 ? 0x7fffffff : pos;        // plow: of those that see anything
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        pmin = min(pmin, __shfl_xor(pmin, o));
+        pmax = max(pmax, __shfl_xor(pmax, o));
+        plow = min(plow, __shfl_xor(plow, o));
+    }
+    pmin = __builtin_amdgcn_readfirstlane(pmin);
+    pmax = __builtin_amdgcn_readfirstlane(pmax);
+    plow = __builtin_amdgcn_readfirstlane(plow);
+    const int window = pg.window, n_first = window ? pg.n_first : 0;
+    const int below = window ? pos - window : -1;            // keys up to here are seen only if they are first ones
+
+    // ---- the block's tiles: `head` tiles from 0 on, then those from `low` on ------------------------------
+    const int low = window && pmax >= 0 ? max(plow - window + 1, 0) / kKeys : 0;
+    const int head = min(low, (int)(((int64_t)n_first + kKeys - 1) / kKeys));
+    const int total = pmax < 0 ? 0 : head + pmax / kKeys + 1 - low;
+    const int t_lo = (int)min((int64_t)piece * piece_tiles, (int64_t)total), t_hi = (int)min((int64_t)t_lo + piece_tiles, (int64_t)total);
+    const int mine = max(0, (t_hi - t_lo - wave + kWaves - 1) / kWaves);
+    auto tile_of = [&](int i) { const int t = t_lo + wave + kWaves * i; return t < head ? t : t - head + low; };
+
+    if (t_lo >= t_hi && pieces > 1) {                        // nothing for the merge
+        if (wave == 0 && hf == 0 && blk * kRows + ln < rows)
+            part_ml[((int64_t)(tok0 + t_own) * n_q_heads + g * grp + hh) * pieces + piece] = make_float4(kLowest, 0.f, 0.f, 0.f);
+        return;
+    }
+
+    // places of tiles i0 .. i0 + 31 (two a tile); -1 where the table names no page
+    int place = -1;
+    auto look_up = [&](int i0) {
+        const int i = i0 + (lane >> 1);
+        place = i < mine ? granule_of(pg, b, 2 * tile_of(i) + (lane & 1)) : -1;
+    };
+    look_up(0);
+
+    // ---- Q as the B operand; a negative scale's sign goes into it, so that the largest score is the largest product's ----
+    const bool negative = scale_log2 < 0.f;
+    const float scale_abs = fabsf(scale_log2);
+    u32x4_t qreg[D / (F32 ? 8 : 16)];
+    {
+        const char *at = (const char *)q_new + (((int64_t)(tok0 + t_own) * n_q_heads + g * grp + hh) * D) * ES;
+#pragma unroll
+        for (int ks = 0; ks < D / (F32 ? 8 : 16); ++ks) {
+            u32x4_t w = *reinterpret_cast<const u32x4_t *>(at + 32 * ks + 16 * hf);
+            if constexpr (F32) w ^= (negative ? 0x80000000u : 0u);
+            else w ^= (negative ? 0x80008000u : 0u);
+            qreg[ks] = w;
+        }
+    }
+
+    // ---- staging ------------------------------------------------------------------------------------------------
+    // A load moves RPL rows, 16 bytes a lane, to consecutive LDS.  Chunk c of row r lies at c ^ swz(r): K's for lanes that read one
+    // chunk of many rows, V's for the transposing reads of four rows.
+    char *const my_lds = lds + wave * WAVE_B;
+    char *const kt = my_lds, *const vt = my_lds + TILE_B;
+    const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)my_lds);
+    const uint32_t row_bytes = (uint32_t)n_kv_heads * ROW_B;
+    auto k_swz = [](int r) { return CPR >= 16 ? (r & 15) : (r & 7); };
+    auto v_swz = [](int r) { return F32 ? (CPR >= 16 ? (r & 15) : (r & 7)) : CPR >= 16 ? 2 * (r & 7) : 2 * (r & 3); };
+    const int st_row = lane / CPR, st_at = lane % CPR;
+    uint32_t k_off[NH], v_off[NH];
+#pragma unroll
+    for (int j = 0; j < NH; ++j) {
+        const int r = j * RPL + st_row;
+        k_off[j] = (uint32_t)r * row_bytes + (uint32_t)(st_at ^ k_swz(r)) * 16u;
+        v_off[j] = (uint32_t)r * row_bytes + (uint32_t)(st_at ^ v_swz(r)) * 16u;
+    }
+    // Written by hand: issued through the compiler's builtin, every later LDS read would wait for all loads in flight.  M0 holds
+    // the LDS address of lane 0; the nop is the wait state that a write to M0 needs before such a load.
+    auto load_1k = [&](uint32_t dst, uint32_t off, const char *base) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(base) : "memory");
+    };
+    const uint64_t granule_bytes = (uint64_t)row_bytes * kGranule;
+    auto stage = [&](int i, const char *pool, const uint32_t (&off)[NH], uint32_t dst) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = max(__builtin_amdgcn_readlane(place, 2 * (i & 31) + h), 0);       // (no page: any rows, masked below)
+            const char *base = pool + (uint64_t)(uint32_t)at * granule_bytes + (uint32_t)g * ROW_B;
+#pragma unroll
+            for (int j = 0; j < NH; ++j) load_1k(dst + (h * NH + j) * 1024, off[j], base);
+        }
+    };
+    auto stage_k = [&](int i) { stage(i, k_pool, k_off, lds_base); };
+    auto stage_v = [&](int i) { stage(i, v_pool, v_off, lds_base + TILE_B); };
+
+    // ---- running state ------------------------------------------------------------------------------------------
+    floatx16 o_acc[NDB];
+    float m_run, l_run, l_rnd;
+    // entry r of the score accumulator is key `entry(r) + (F32 ? 4 : 8) hf` of the tile: K rows are fed to the bf16 instruction with bits 2
+    // and 3 swapped, so that a lane's weights are 8 consecutive keys twice
+    const int krow = F32 ? ln : (ln & ~12) | ((ln & 4) << 1) | ((ln & 8) >> 1);
+    constexpr int HALF = F32 ? 4 : 8;
+    auto entry = [](int r) { return F32 ? 8 * (r >> 2) + (r & 3) : 16 * (r >> 3) + (r & 7); };
+    const int tr_s = lane & 15, tr_g = lane >> 4;                        // (see read_v)
+    const int tr_key = 8 * (tr_g >> 1) + (tr_s >> 2), tr_c = 2 * (tr_g & 1) + ((tr_s & 3) >> 1);
+    auto read_v = [&](int a, int db) -> u32x4_t {
+        // The A operand of the second product: channel 32 db + ln, 8 consecutive keys, out of two transposing reads: in each
+        // group of 16 lanes, lane s points at 4 channels of key s / 4 and lane i receives channel i of the four keys.
+        typedef short v4i16 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+        u32x4_t r;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int key = 16 * a + tr_key + 4 * u;
+            const char *at = vt + key * ROW_B + ((4 * db + tr_c) ^ v_swz(key)) * 16 + 8 * (tr_s & 1);
+            const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16 *)(at)));
+            r[2 * u] = w.x;
+            r[2 * u + 1] = w.y;
+        }
+        return r;
+    };
+    auto v_element = [&](int key, int c) -> float {
+        const char *at = vt + key * ROW_B + ((c * ES / 16) ^ v_swz(key)) * 16 + (c * ES) % 16;
+        if constexpr (F32) return *reinterpret_cast<const float *>(at);
+        else return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(at) << 16);
+    };
+
+    // A weight of 0 does not hide a V that is infinite or NaN.  Rows behind the context, and of no page, are cleared in LDS.  Others, in a
+    // tile that some row does not see all of, are found out at the end: an output that is no number makes the workgroup sweep once
+    // more, carefully, where such keys are multiplied with the weights of the rows that see them, and no others.
+    for (int careful = 0; careful < 2; ++careful) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o_acc[db][r] = 0.f;
+        m_run = kLowest;           // reference of the weights: a former maximum of the scores times log2 e, the same in both half-waves
+        l_run = l_rnd = 0.f;       // this half-wave's share of the sum of weights; the same of the weights as the second product sees them
+        if (careful) look_up(0);
+        if (mine > 0) { stage_k(0); stage_v(0); }
+        for (int i = 0; i < mine; ++i) {
+            const int x0 = tile_of(i) * kKeys;
+            const bool none[2] = {__builtin_amdgcn_readlane(place, 2 * (i & 31)) < 0, __builtin_amdgcn_readlane(place, 2 * (i & 31) + 1) < 0};
+            const bool more = i + 1 < mine;
+            asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NL) : "memory");           // K has landed, V may still be on its way
+            if (more && ((i + 1) & 31) == 0) look_up(i + 1);
+
+            floatx16 s = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < CPR / 2; ++c) {
+                const u32x4_t w = *reinterpret_cast<const u32x4_t *>(kt + krow * ROW_B + ((2 * c + hf) ^ k_swz(krow)) * 16);
+                if constexpr (F32) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[u]), __uint_as_float(qreg[c][u]), s, 0, 0, 0);
+                } else {
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w), as_bf16x8(qreg[c]), s, 0, 0, 0);
+                }
+            }
+            if (more) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // what lay in the slot has been read
+                stage_k(i + 1);
+            }
+            const bool masked = x0 + kKeys - 1 > pmin || none[0] || none[1] || (window && x0 <= pmax - window && x0 + kKeys > n_first);
+            float f = scale_abs;
+            if (masked) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = x0 + entry(r) + HALF * hf;
+                    const bool seen = key <= pos && (key > below || key < n_first) && !none[r >> 3];
+                    s[r] = seen ? s[r] * f : -INFINITY;
+                }
+                f = 1.f;
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+            mx = max_of_halves(mx) * f;
+            // The reference that weights are relative to moves only once a score is kSlack above it (in powers of two): weights of up
+            // to 2^kSlack lose nothing, and sums are seldom scaled behind a row's first tiles.
+            if (__builtin_amdgcn_ballot_w64(mx > m_run + kSlack) != 0) {
+                const float m_new = fmaxf(m_run, mx), corr = __builtin_amdgcn_exp2f(m_run - m_new);
+                m_run = m_new;
+                l_run *= corr;
+                l_rnd *= corr;
+#pragma unroll
+                for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o_acc[db][r] *= corr;
+            }
+            float y[16], psum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], f, -m_run));
+                psum += y[r];
+            }
+            l_run += psum;
+            u32x4_t pop[F32 ? 1 : 2][F32 ? 1 : PARTS];
+            if constexpr (!F32) {
+                typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float u = y[8 * a + 2 * j], v = y[8 * a + 2 * j + 1];
+                        const uint32_t w = pack2(u, v);
+                        pop[a][0][j] = w;
+                        if constexpr (PARTS == 2) pop[a][1][j] = pack2(u - bf16_lo(w), v - bf16_hi(w));
+                        // One part: the normaliser is made of the rounded weights.  Numerator and denominator then carry the same rounding, and a
+                        // row that one key dominates returns that key's V to within the output's own rounding.
+                        else l_rnd = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3f803f80u), l_rnd, false);
+                    }
+            }
+
+            if (more) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NL) : "memory");      // V has landed, the next K may still be on its way
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (x0 + kKeys > len || none[0] || none[1]) {
+#pragma unroll
+                for (int e = 0; e < TILE_B / 1024; ++e) {
+                    const int r = (e * kWave + lane) / CPR;
+                    if (x0 + r >= len || none[r >> 4]) reinterpret_cast<u32x4_t *>(vt)[e * kWave + lane] = u32x4_t{0u, 0u, 0u, 0u};
+                }
+            }
+            if (careful && masked) {
+                // Next K is on its way into its slot, so the weights change hands through the registers, key by key.
+                for (int key = 0; key < kKeys; ++key) {
+                    bool odd = false;
+                    for (int c = lane; c < D; c += kWave) odd = odd || !(fabsf(v_element(key, c)) < INFINITY);
+                    if (__builtin_amdgcn_ballot_w64(odd) == 0) continue;
+                    const int from = (key / HALF) & 1;                    // the half-wave that holds the key's weights, and their place in it
+                    const int at = F32 ? 4 * (key >> 3) + (key & 3) : 8 * (key >> 4) + (key & 7);
+                    float p = y[0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) p = r == at ? y[r] : p;
+                    p = __shfl(p, ln + 32 * from);
+                    const int k_at = x0 + key;
+                    const bool seen = k_at <= pos && (k_at > below || k_at < n_first) && !none[key >> 4];
+                    if (seen) {
+                        p = fmaxf(p, 1e-37f);
+#pragma unroll
+                        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) o_acc[db][r] += p * v_element(key, 32 * db + 8 * (r >> 2) + 4 * hf + (r & 3));
+                    }
+                    if (lane < CPR) *reinterpret_cast<u32x4_t *>(vt + key * ROW_B + lane * 16) = u32x4_t{0u, 0u, 0u, 0u};
+                }
+            }
+            if constexpr (F32) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db)
+                        o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_element(entry(r) + HALF * hf, 32 * db + ln), y[r], o_acc[db], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db) {
+                        const u32x4_t va = read_v(a, db);
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va), as_bf16x8(pop[a][p]), o_acc[db], 0, 0, 0);
+                    }
+            }
+            if (more) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                stage_v(i + 1);
+            }
+        }
+
+        // ---- the waves meet ----------------------------------------------------------------------------------------
+        {
+            const float l = l_run + __shfl_xor(l_run, 32), lr = l_rnd + __shfl_xor(l_rnd, 32);
+            if (hf == 0) ml_s[wave][ln] = make_float4(m_run, l, !F32 && PARTS == 1 ? lr : l, 0.f);
+            if (tid == 0) odd_s = 0;
+        }
+        __syncthreads();
+        {
+            float top = ml_s[0][ln].x;
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml_s[w][ln].x);
+            const float f = __builtin_amdgcn_exp2f(m_run - top);
+            float *mine_o = reinterpret_cast<float *>(my_lds) + ln * D;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c4 = 8 * db + 2 * q + hf;          // channels 4 c4 .. + 3: at place c4 ^ row, so that rows use different banks
+                    *reinterpret_cast<float4 *>(mine_o + 4 * (c4 ^ (ln & (D / 4 - 1)))) =
+                        make_float4(o_acc[db][4 * q] * f, o_acc[db][4 * q + 1] * f, o_acc[db][4 * q + 2] * f, o_acc[db][4 * q + 3] * f);
+                }
+        }
+        __syncthreads();
+        constexpr int CPT = D / 8;                               // channels a thread stores
+        const int row = tid >> 3, part = tid & 7;
+        const int row_q = blk * kRows + row;
+        float top = kLowest, l = 0.f, lr = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml_s[w][row].x);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float4 x = ml_s[w][row];
+            const float f = __builtin_amdgcn_exp2f(x.x - top);
+            l += x.y * f;
+            lr += x.z * f;
+        }
+        float o[CPT];
+#pragma unroll
+        for (int c = 0; c < CPT; ++c) o[c] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float *from = reinterpret_cast<const float *>(lds + w * WAVE_B) + row * D;
+#pragma unroll
+            for (int k = 0; k < CPT / 4; ++k) {
+                const float4 x = *reinterpret_cast<const float4 *>(from + 4 * ((CPT / 4 * part + k) ^ (row & (D / 4 - 1))));
+                o[4 * k] += x.x; o[4 * k + 1] += x.y; o[4 * k + 2] += x.z; o[4 * k + 3] += x.w;
+            }
+        }
+        if (!careful) {
+            float sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < CPT; ++c) sum += o[c] * 0.f;                  // 0, or NaN
+            if (!(sum == 0.f)) odd_s = 1;
+            __syncthreads();
+            if (odd_s) { __syncthreads(); continue; }
+        }
+        if (row_q >= rows) return;
+        const int t2 = row_q / grp;
+        const int64_t at = (int64_t)(tok0 + t2) * n_q_heads + g * grp + (row_q - t2 * grp);
+        if (pieces > 1) {
+            const int64_t slot = at * pieces + piece;
+            if (part == 0) part_ml[slot] = make_float4(top, l, lr, 0.f);
+            if (l != 0.f) {                                      // (the merge passes over a piece without keys)
+                float4 *dst = reinterpret_cast<float4 *>(part_o + slot * D + part * CPT);
+#pragma unroll
+                for (int c = 0; c < CPT / 4; ++c) dst[c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+            }
+            return;
+        }
+        const float inv = l != 0.f ? 1.f / lr : 0.f;
+#pragma unroll
+        for (int c = 0; c < CPT; ++c) o[c] = l != 0.f ? o[c] * inv : 0.f;
+        if constexpr (!F32) {
+            uint4 *dst = reinterpret_cast<uint4 *>((uint16_t *)out + at * D + part * CPT);
+#pragma unroll
+            for (int c = 0; c < CPT / 8; ++c)
+                dst[c] = make_uint4(pack2(o[8 * c], o[8 * c + 1]), pack2(o[8 * c + 2], o[8 * c + 3]), pack2(o[8 * c + 4], o[8 * c + 5]), pack2(o[8 * c + 6], o[8 * c + 7]));
+        } else {
+            float4 *dst = reinterpret_cast<float4 *>((float *)out + at * D + part * CPT);
+#pragma unroll
+            for (int c = 0; c < CPT / 4; ++c) dst[c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+        }
+        if (lse_out && part == 0) lse_out[at] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+        return;
+    }
+}
+
+// out = sum_p w_p O_p / sum_p w_p l_p with w_p = 2^(m_p - max m).  A workgroup takes 32 channels of one row: its threads make the
+// pieces' weights once, into LDS, then groups of 8 threads take every 32nd piece, four channels a thread, and meet by shuffles and in LDS.
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kThreads) void merge_paged_kernel(const Paged pg, int n_q_heads, int pieces, const float *__restrict__ part_o,
+                                                               const float4 *__restrict__ part_ml, void *__restrict__ out, float *__restrict__ lse_out)
+{
+    constexpr int kLanes = 8, kGroups = kThreads / kLanes;
+    __shared__ float weight[kMaxPieces];
+    __shared__ float meet[3][kWaves];
+    __shared__ float4 sum_s[kWaves][kLanes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t item = blockIdx.x;
+    if (pg.cu_new) {                                         // tokens of no request stay as they are
+        const int token = (int)(item / n_q_heads);
+        if (token < pg.cu_new[0] || token >= pg.cu_new[pg.batch]) return;
+    }
+    const int64_t slot = item * pieces;
+    static_assert(kMaxPieces == 2 * kThreads, "two records a thread");
+    float4 x[2];
+    float top = kLowest;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int p = tid + i * kThreads;
+        x[i] = p < pieces ? part_ml[slot + p] : make_float4(kLowest, 0.f, 0.f, 0.f);
+        top = fmaxf(top, x[i].x);
+    }
+    top = wave_max(top);
+    if (lane == 0) meet[0][wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, meet[0][w]);
+    float l = 0.f, lr = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float f = __builtin_amdgcn_exp2f(x[i].x - top);
+        l += x[i].y * f;
+        lr += x[i].z * f;
+        if (tid + i * kThreads < pieces) weight[tid + i * kThreads] = x[i].y != 0.f ? f : -1.f;      // (-1: a piece without keys has left no sums)
+    }
+    l = wave_sum(l);
+    lr = wave_sum(lr);
+    if (lane == 0) { meet[1][wave] = l; meet[2][wave] = lr; }
+    __syncthreads();
+    l = (meet[1][0] + meet[1][1]) + (meet[1][2] + meet[1][3]);
+    lr = (meet[2][0] + meet[2][1]) + (meet[2][2] + meet[2][3]);
+    const int c = (int)blockIdx.y * kLanes + tid % kLanes;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 *from = reinterpret_cast<const float4 *>(part_o + slot * D) + c;
+#pragma unroll 4
+    for (int p = tid / kLanes; p < pieces; p += kGroups) {
+        const float f = weight[p];
+        if (f == -1.f) continue;
+        const float4 y = from[(int64_t)p * (D / 4)];
+        o.x += f * y.x; o.y += f * y.y; o.z += f * y.z; o.w += f * y.w;
+    }
+#pragma unroll
+    for (int m = kLanes; m < kWave; m <<= 1) {
+        o.x += __shfl_xor(o.x, m); o.y += __shfl_xor(o.y, m); o.z += __shfl_xor(o.z, m); o.w += __shfl_xor(o.w, m);
+    }
+    if (lane < kLanes) sum_s[wave][lane] = o;
+    __syncthreads();
+    if (tid >= kLanes) return;
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) {
+        const float4 y = sum_s[i][lane];
+        o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+    }
+    const float inv = 1.f / lr;
+    if (l != 0.f) { o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv; }
+    else o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (DTYPE == KVS_BF16) *reinterpret_cast<uint2 *>((uint16_t *)out + item * D + 4 * c) = make_uint2(pack2(o.x, o.y), pack2(o.z, o.w));
+    else *reinterpret_cast<float4 *>((float *)out + item * D + 4 * c) = o;
+    if (lse_out && c == 0) lse_out[item] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+}
+
+inline size_t slot_bytes(int d) { return (size_t)d * sizeof(float) + sizeof(float4); }
+
+// Tiles that a block of rows may need at most.
+int64_t most_tiles(const Paged &pg, int grp)
+{
+    int64_t keys = pg.max_ctx;
+    if (pg.window && !pg.sel_pos) {                          // consecutive tokens: the window, and what 32 rows lie apart
+        const int64_t some = (int64_t)pg.window + kRows / (grp < kRows ? grp : kRows) + 2 * kKeys + pg.n_first + kKeys;
+        if (some < keys) keys = some;
+    }
+    return (keys + kKeys - 1) / kKeys + 1;
+}
+
+// How keys are cut: `pieces` pieces of `tiles` tiles.  The contexts' lengths are on the device; the host knows how long one can be.
+struct Plan { int32_t pieces, tiles; };
+
+Plan plan_pieces(const kvs_shape *shape, const Paged &pg, int64_t units, size_t workspace_bytes)
+{
+    const int64_t wgs = units * shape->n_kv_heads, most = most_tiles(pg, shape->n_q_heads / shape->n_kv_heads);
+    const int64_t slots = (int64_t)(workspace_bytes / slot_bytes(shape->head_dim)) / ((int64_t)pg.n_new * shape->n_q_heads);
+    int64_t pieces = (4 * kPlaces + wgs - 1) / wgs;
+    if (pieces > slots) pieces = slots;
+    if (pieces > kMaxPieces) pieces = kMaxPieces;
+    if (wgs >= 4 * kPlaces || pieces <= 1 || most <= 2 * kWaves) return {1, 0x7fffffff};
+    int64_t tiles = (most + pieces - 1) / pieces;
+    tiles = (tiles + kWaves - 1) / kWaves * kWaves;
+    if (tiles < 2 * kWaves) tiles = 2 * kWaves;
+    return {(int32_t)((most + tiles - 1) / tiles), (int32_t)tiles};
+}
+
+template <int DTYPE, int D, int PARTS>
+kvs_status launch(const kvs_shape *shape, const kvs_paged_cache *c, const Paged &pg, int64_t units, const Plan &plan, const void *q, float scale,
+                  void *out, float *lse_out, void *workspace, hipStream_t hs)
+{
+    static DeviceOnce once;
+    constexpr int es = DTYPE == KVS_F32 ? 4 : 2;
+    constexpr int lds = kWaves * 2 * kKeys * D * es;
+    kvs_status st = once_per_device(once, [&]() -> kvs_status {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_paged_kernel<DTYPE, D, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_attention_paged: %s", hipGetErrorString(e));
+    });
+    if (st != KVS_OK) return st;
+    const int64_t items = (int64_t)pg.n_new * shape->n_q_heads;
+    float4 *ml = reinterpret_cast<float4 *>(workspace);
+    float *po = reinterpret_cast<float *>(ml + (plan.pieces > 1 ? items * plan.pieces : 0));
+    hipLaunchKernelGGL((attention_paged_kernel<DTYPE, D, PARTS>), dim3((unsigned)(units * plan.pieces * shape->n_kv_heads)), dim3(kThreads), lds, hs, pg, shape->n_q_heads,
+                       shape->n_kv_heads, (int)units, plan.pieces, plan.tiles, (const char *)c->k, (const char *)c->v, q, scale * 1.4426950408889634f, out, lse_out, po, ml);
+    if ((st = check_launch("kvs_attention_paged")) != KVS_OK || plan.pieces <= 1) return st;
+    hipLaunchKernelGGL((merge_paged_kernel<DTYPE, D>), dim3((unsigned)items, D / 32), dim3(kThreads), 0, hs, pg, shape->n_q_heads, plan.pieces, po, ml, out, lse_out);
+    return check_launch("kvs_attention_paged(merge)");
+}
+
+} // namespace
+
+size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new)
+{
+    if (check_shape(shape) != KVS_OK || n_new <= 0 || max_ctx <= 0) return 256;
+    const int64_t items = n_new * shape->n_q_heads;
+    int64_t pieces = max_ctx / (2 * kWaves * kKeys) + 2;
+    if (pieces > kMaxPieces) pieces = kMaxPieces;
+    // a launch that is cut has at most 4 kPlaces workgroups before and twice that after it, of 32 rows each
+    const int64_t most = (int64_t)8 * kPlaces * kRows;
+    const int64_t slots = items < most && items * pieces < most ? items * pieces : most > items ? most : 0;
+    return ((size_t)slots * slot_bytes(shape->head_dim) + 255) / 256 * 256 + 256;
+}
+
+kvs_status check_paged(const char *me, const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages, Paged *out)
+{
+    kvs_status st = check_shape(shape);
+    if (st != KVS_OK) return st;
+    if (!cache || !pages) return fail(KVS_EINVAL, "%s: the cache or the page table is NULL", me);
+    if (shape->n_kv_heads > 64) return fail(KVS_EUNSUPPORTED, "%s: more than 64 kv heads", me);
+    if (shape->n_q_heads > 4096) return fail(KVS_EUNSUPPORTED, "%s: more than 4096 query heads", me);
+    if (cache->page != 16 && cache->page != 32 && cache->page != 64 && cache->page != 128 && cache->page != 256)
+        return fail(KVS_EINVAL, "%s: pages of %d rows (16, 32, 64, 128 and 256 are built)", me, cache->page);
+    if (cache->n_pages < 0 || cache->n_pages > (int64_t)0x7fffffff / (cache->page / kGranule))
+        return fail(KVS_EINVAL, "%s: %lld pages", me, (long long)cache->n_pages);
+    if (pages->batch < 0 || pages->width < 0 || pages->max_ctx < 0) return fail(KVS_EINVAL, "%s: negative size of the page table", me);
+    if (pages->max_ctx > 0x7fffff00LL) return fail(KVS_EINVAL, "%s: contexts of %lld rows", me, (long long)pages->max_ctx);
+    if (pages->batch > 0 && (!pages->ctx_len || (pages->width > 0 && !pages->table))) return fail(KVS_EINVAL, "%s: the page table or the lengths are NULL", me);
+    if (cache->n_pages > 0 && (!cache->k || !cache->v)) return fail(KVS_EINVAL, "%s: the cache's K or V is NULL", me);
+    if (!aligned16(cache->k) || !aligned16(cache->v)) return fail(KVS_EINVAL, "%s: the cache's K and V must be 16-byte aligned", me);
+    Paged pg = {};
+    pg.table = pages->table;
+    pg.ctx_len = pages->ctx_len;
+    pg.batch = pages->batch;
+    pg.width = pages->width;
+    const int64_t rows = (int64_t)pages->width * cache->page;
+    pg.max_ctx = (int32_t)(rows < pages->max_ctx ? rows : pages->max_ctx);
+    if (cache->n_pages == 0) pg.max_ctx = 0;
+    pg.n_pages = (int32_t)cache->n_pages;
+    pg.page_log2 = __builtin_ctz((unsigned)cache->page);
+    *out = pg;
+    return KVS_OK;
+}
+
+kvs_status check_new_tokens(const char *me, const kvs_shape *shape, const kvs_page_table *pages, const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new,
+                            int32_t window, int32_t n_first, Paged *out)
+{
+    if (n_new < 0) return fail(KVS_EINVAL, "%s: n_new < 0", me);
+    if (window < 0 || n_first < 0) return fail(KVS_EINVAL, "%s: a negative window or number of first tokens", me);
+    if (!cu_new && n_new != pages->batch) return fail(KVS_EINVAL, "%s: %lld tokens of %d requests without cu_new", me, (long long)n_new, pages->batch);
+    if (n_new > 0x3fffff00LL / shape->n_q_heads) return fail(KVS_EINVAL, "%s: %lld tokens in one call", me, (long long)n_new);
+    out->cu_new = cu_new;
+    out->sel_pos = sel_pos;
+    out->n_new = (int32_t)n_new;
+    out->window = window;
+    out->n_first = n_first;
+    return KVS_OK;
+}
+
+} // namespace kvs
+
+extern "C" kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages,
+                                          const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new, const void *q_new, float scale,
+                                          int32_t window, int32_t n_first, void *out, float *lse_out,
+                                          void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace kvs;
+    const char *me = "kvs_attention_paged";
+    Paged pg;
+    kvs_status st = check_paged(me, shape, cache, pages, &pg);
+    if (st != KVS_OK || (st = check_new_tokens(me, shape, pages, cu_new, sel_pos, n_new, window, n_first, &pg)) != KVS_OK) return st;
+    if (!isfinite(scale)) return fail(KVS_EINVAL, "%s: the scale is not finite", me);
+    if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return fail(KVS_EINVAL, "%s: workspace must be 256-byte aligned", me);
+    if (!workspace) workspace_bytes = 0;
+    if (n_new == 0 || pages->batch == 0) return KVS_OK;
+    if (!q_new || !out) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
+    if (!aligned16(q_new) || !aligned16(out)) return fail(KVS_EINVAL, "%s: Q/out pointers must be 16-byte aligned", me);
+    hipStream_t hs = (hipStream_t)stream;
+    const int grp = shape->n_q_heads / shape->n_kv_heads;
+    const int64_t units = most_blocks(pg, grp, kRows);
+    const Plan plan = plan_pieces(shape, pg, units, workspace_bytes);
+    if (units * plan.pieces * shape->n_kv_heads > kMostWgs || (int64_t)pg.n_new * shape->n_q_heads * (plan.pieces > 1 ? 4 : 0) > kMostWgs)
+        return fail(KVS_EINVAL, "%s: too many rows in one call", me);
+    const bool wide = shape->head_dim == 128, few = (int64_t)pg.n_new * grp <= (int64_t)kRows * pg.batch;
+#define KVS_AP(DT, DD, PP) launch<DT, DD, PP>(shape, cache, pg, units, plan, q_new, scale, out, lse_out, workspace, hs)
+    if (shape->dtype == KVS_F32) return wide ? KVS_AP(KVS_F32, 128, 1) : KVS_AP(KVS_F32, 64, 1);
+    if (few) return wide ? KVS_AP(KVS_BF16, 128, 2) : KVS_AP(KVS_BF16, 64, 2);
+    return wide ? KVS_AP(KVS_BF16, 128, 1) : KVS_AP(KVS_BF16, 64, 1);
+#undef KVS_AP
+}

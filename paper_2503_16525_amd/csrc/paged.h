@@ -1,0 +1,97 @@
+// What the kernels over a cache in pages share (not part of the ABI).
+#pragma once
+
+#include "kvs_internal.h"
+
+namespace kvs {
+
+// A call's requests as its kernels see them.  Lengths, offsets, positions and page ids come from device memory and are not
+// trusted: whatever stands there, every access stays inside the tensors that the host was told about.
+struct Paged {
+    const int32_t *table, *ctx_len, *cu_new, *sel_pos;
+    int32_t batch, width, n_new;
+    int32_t max_ctx;              // at most width pages of rows
+    int32_t n_pages, page_log2;
+    int32_t window, n_first;      // window 0: none
+};
+
+constexpr int kGranule = 16;      // rows that lie together whatever the page size: no page is shorter
+
+kvs_status check_paged(const char *me, const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages, Paged *out);
+// the same with a call's new tokens
+kvs_status check_new_tokens(const char *me, const kvs_shape *shape, const kvs_page_table *pages, const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new,
+                            int32_t window, int32_t n_first, Paged *out);
+size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new);
+size_t mass_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new);
+size_t evict_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx);
+
+__device__ __forceinline__ int len_of(const Paged &pg, int b) { return min(max(pg.ctx_len[b], 0), pg.max_ctx); }
+
+// The tokens of request b: [lo, lo + n) of the call's.
+__device__ __forceinline__ void tokens_of(const Paged &pg, int b, int &lo, int &n)
+{
+    if (!pg.cu_new) { lo = b; n = 1; return; }
+    lo = min(max(pg.cu_new[b], 0), pg.n_new);
+    n = min(max(pg.cu_new[b + 1], lo), pg.n_new) - lo;
+}
+
+// Position of token i of a request's n, -1 where it sees nothing, at most the context's last.
+__device__ __forceinline__ int position_of(const Paged &pg, int lo, int n, int i, int len)
+{
+    const int p = pg.sel_pos ? pg.sel_pos[lo + i] : len - n + i;
+    return p < 0 ? -1 : min(p, len - 1);
+}
+
+// Which 16 rows of the pool rows 16 gi .. 16 gi + 15 of request b are, -1: none.
+__device__ __forceinline__ int granule_of(const Paged &pg, int b, int gi)
+{
+    const int shift = pg.page_log2 - 4, at = gi >> shift;
+    if (gi < 0 || at >= pg.width) return -1;
+    const int id = pg.table[(int64_t)b * pg.width + at];
+    return (uint32_t)id < (uint32_t)pg.n_pages ? (id << shift) + (gi & ((1 << shift) - 1)) : -1;
+}
+
+// A call's rows (tokens times the query heads that share a KV head) in blocks of R rows, none of which holds two requests: which request
+// block u belongs to and which of its blocks it is.  All lanes of a wave ask for the same block; 64 requests a step.
+template <int R>
+__device__ __forceinline__ bool find_block(const Paged &pg, int grp, int u, int &b, int &blk)
+{
+    if (!pg.cu_new) {
+        const int per = (grp + R - 1) / R;
+        b = u / per;
+        blk = u - b * per;
+        return b < pg.batch;
+    }
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b0 = 0; b0 < pg.batch; b0 += 64) {
+        int lo, n = 0;
+        if (b0 + lane < pg.batch) tokens_of(pg, b0 + lane, lo, n);
+        const int mine = (n * grp + R - 1) / R;
+        int upto = mine;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int x = __shfl_up(upto, s);
+            upto += lane >= s ? x : 0;
+        }
+        const unsigned long long past = __ballot(base + upto > u);
+        if (past) {
+            const int at = __ffsll((long long)past) - 1;
+            b = b0 + at;
+            blk = u - base - __builtin_amdgcn_readlane(upto - mine, at);
+            return true;
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// How many such blocks there can be, whatever the offsets.
+inline int64_t most_blocks(const Paged &pg, int grp, int r)
+{
+    if (!pg.cu_new) return (int64_t)pg.batch * ((grp + r - 1) / r);
+    const int64_t rows = (int64_t)pg.n_new * grp, reqs = pg.batch < pg.n_new ? pg.batch : pg.n_new;
+    return rows / r + reqs;
+}
+
+} // namespace kvs
