@@ -1,42 +1,43 @@
 // kvs_evict_paged: a request's rows that received most attention, copied to pages of their own.
 //
-// Three launches.  keys: every row's mass, added up over the KV heads, as an order-preserving 32-bit key; protected rows get the
-// largest.  select: a workgroup a request finds the m-th largest key by four passes of eight bits, then writes the list of the kept
-// rows, ascending, ties to the lower index.  move: the rows' K, V and mass.
+// Every row has a 32-bit key, its mass added up over the KV heads, order-preserving; protected rows have the largest.  The m-th largest key
+// is found by its digits, 11, 11 and 10 bits from the top: a count of the digit's values in LDS tells which one the key has.  Rows
+// above it stay, and so many of those that equal it, from the lowest index on.
+//   Up to kSmall rows a workgroup a request holds all keys in registers.  Longer contexts take two launches for it: segments make
+//   their keys and count their first digits, then a workgroup a request adds these up, reads the keys once, sets those of the
+//   one value aside in LDS and goes on with them; a third launch counts what stays of every 256 rows.
+//   The last launch moves: a workgroup for every 256 rows ranks its own behind those before it and copies them.
+// What bounds it: the copy, at most; the keys' passes are a few dependent trips to memory each.
 #include "paged.h"
 
 namespace kvs {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kSub = kThreads;              // rows of a moving workgroup
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / kWave;
+constexpr int kKeysPerThread = 8;
+constexpr int kSmall = kSelThreads * kKeysPerThread;
+constexpr int kSeg = 2048;                  // rows whose first digits are counted together
+constexpr int kBins = 2048;                 // values of a digit
+constexpr int kAside = 2304;                // keys that LDS holds besides, for each wave
 
-struct Kept { int m, first, recent; };      // rows kept, protected ones among them
+struct Picked { uint32_t key; int32_t want, m, len; };      // the m-th largest key, how many that equal it stay
 
-__device__ __forceinline__ Kept kept_of(const Paged &pg, const int32_t *keep, int max_keep, int n_first, int n_recent, int b, int len)
+__device__ __forceinline__ uint32_t key_of(const Paged &pg, int b, int i, int len, int m, int n_first, int n_recent, int n_kv_heads, const float *__restrict__ mass, int64_t mass_stride)
 {
-    Kept k;
-    k.m = min(len, min(max(keep[b], 0), max_keep));
-    k.first = min(n_first, k.m);
-    k.recent = min(n_recent, k.m - k.first);
-    return k;
+    const int first = min(n_first, m), recent = min(n_recent, m - first);
+    const float *at = mass + (int64_t)b * n_kv_heads * mass_stride + i;
+    float sum = at[0];
+#pragma unroll 4
+    for (int g = 1; g < n_kv_heads; ++g) sum += at[g * mass_stride];
+    return i < first || i >= len - recent ? 0xffffffffu : sum == sum ? score_key(sum) : 0u;
 }
 
-__global__ __launch_bounds__(kThreads) void evict_keys_kernel(const Paged pg, int n_kv_heads, const int32_t *__restrict__ keep, int max_keep, int n_first, int n_recent,
-                                                              const float *__restrict__ mass, int64_t mass_stride, uint32_t *__restrict__ keys)
-{
-    const int b = blockIdx.y;
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int len = len_of(pg, b);
-    if (i >= len) return;
-    const Kept k = kept_of(pg, keep, max_keep, n_first, n_recent, b, len);
-    float sum = mass[(int64_t)b * n_kv_heads * mass_stride + i];
-    for (int g = 1; g < n_kv_heads; ++g) sum += mass[((int64_t)b * n_kv_heads + g) * mass_stride + i];
-    const uint32_t key = i < k.first || i >= len - k.recent ? 0xffffffffu : sum == sum ? score_key(sum) : 0u;
-    keys[(int64_t)b * pg.max_ctx + i] = key;
-}
+__device__ __forceinline__ int kept_of(const int32_t *keep, int max_keep, int b, int len) { return min(len, min(max(keep[b], 0), max_keep)); }
 
 // exclusive sum over the workgroup, and the total
+template <int WAVES>
 __device__ __forceinline__ int scan_exclusive(int x, int *sums, int &total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -52,123 +53,294 @@ __device__ __forceinline__ int scan_exclusive(int x, int *sums, int &total)
     int before = 0;
     total = 0;
 #pragma unroll
-    for (int w = 0; w < kSelWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         before += w < wave ? sums[w] : 0;
         total += sums[w];
     }
     return before + upto - x;
 }
 
-__global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const Paged pg, const int32_t *keep, int max_keep, int n_first, int n_recent, const uint32_t *__restrict__ keys,
-                                                                   int32_t *__restrict__ list, int32_t *__restrict__ counts, int32_t *__restrict__ kept, int32_t *new_len)
+// From the counts of a digit's values: the value of the want-th largest, and how many of that value are still wanted.  Two values a thread.
+__device__ __forceinline__ void find_digit(int large, int small, int *sums, int *found, uint32_t &digit, int &want)
 {
-    __shared__ int hist[256];
-    __shared__ int sums[kSelWaves];
-    __shared__ uint32_t found[2];
-    const int b = blockIdx.x, tid = threadIdx.x;
+    int total;
+    const int before = scan_exclusive<kSelWaves>(large + small, sums, total);
+    if (before < want && before + large >= want) { found[0] = kBins - 1 - 2 * (int)threadIdx.x; found[1] = want - before; }
+    else if (before + large < want && before + large + small >= want) { found[0] = kBins - 2 - 2 * (int)threadIdx.x; found[1] = want - before - large; }
+    __syncthreads();
+    digit = (uint32_t)found[0];
+    want = found[1];
+    __syncthreads();
+}
+
+// Up to kSmall rows a request: keys, the m-th of them, and what stays of every kSub rows.
+__global__ __launch_bounds__(kSelThreads) void evict_small_kernel(const Paged pg, int n_kv_heads, const int32_t *keep, int max_keep, int n_first, int n_recent,
+                                                                  const float *__restrict__ mass, int64_t mass_stride, uint32_t *__restrict__ keys, int64_t stride, Picked *__restrict__ picked,
+                                                                  int2 *__restrict__ counts, int subs, int32_t *new_len)
+{
+    __shared__ int hist[kBins];
+    __shared__ int sums[kSelWaves], found[2];
+    __shared__ int above_s[kSmall / kSub], equal_s[kSmall / kSub];
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int len = len_of(pg, b);
-    const int m = kept_of(pg, keep, max_keep, n_first, n_recent, b, len).m;
-    const uint32_t *key = keys + (int64_t)b * pg.max_ctx;
-    list += (int64_t)b * pg.max_ctx;
-    __syncthreads();                                         // new_len may be the lengths
+    const int m = kept_of(keep, max_keep, b, len);
+    uint32_t key[kKeysPerThread];
+#pragma unroll
+    for (int j = 0; j < kKeysPerThread; ++j) {
+        const int i = tid + j * kSelThreads;
+        key[j] = i < len ? key_of(pg, b, i, len, m, n_first, n_recent, n_kv_heads, mass, mass_stride) : 0u;
+        if (i < len) keys[(int64_t)b * stride + i] = key[j];
+    }
+    if (tid < kSmall / kSub) above_s[tid] = equal_s[tid] = 0;
+    uint32_t prefix = 0;
+    int want = m;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const uint32_t mask = pass == 2 ? 1023u : 2047u;
+        hist[tid] = hist[tid + kSelThreads] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kKeysPerThread; ++j)
+            if (tid + j * kSelThreads < len && (pass == 0 || key[j] >> (pass == 1 ? 21 : 10) == prefix)) atomicAdd(&hist[(key[j] >> shift) & mask], 1);
+        __syncthreads();
+        uint32_t digit = 0;
+        if (m > 0) find_digit(hist[kBins - 1 - 2 * tid], hist[kBins - 2 - 2 * tid], sums, found, digit, want);
+        prefix = (prefix << (pass == 2 ? 10 : 11)) | digit;
+    }
+    if (m == 0) { prefix = 0xffffffffu; want = 0; }
+#pragma unroll
+    for (int j = 0; j < kKeysPerThread; ++j) {
+        const int i = tid + j * kSelThreads;
+        const int above = __popcll(__ballot(i < len && key[j] > prefix)), equal = __popcll(__ballot(i < len && key[j] == prefix));
+        if (lane == 0) { atomicAdd(&above_s[i / kSub], above); atomicAdd(&equal_s[i / kSub], equal); }
+    }
+    __syncthreads();
+    for (int i = tid; i < subs; i += kSelThreads) counts[(int64_t)b * subs + i] = make_int2(above_s[i], equal_s[i]);
     if (tid == 0) {
-        counts[b] = m;
+        picked[b] = {prefix, want, m, len};
         if (new_len) new_len[b] = m;
-    }
-    if (m == 0) return;
-    uint32_t prefix = 0;                                     // the threshold's leading bits
-    int want = m;                                            // ... and how many keys that begin with them are still to be taken
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < len; i += kSelThreads) {
-            const uint32_t k = key[i];
-            if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1);
-        }
-        __syncthreads();
-        const int mine = tid < 256 ? hist[255 - tid] : 0;    // from the largest digit down
-        int total;
-        const int before = scan_exclusive(mine, sums, total);
-        if (before < want && before + mine >= want) {
-            found[0] = (prefix << 8) | (uint32_t)(255 - tid);
-            found[1] = (uint32_t)(want - before);
-        }
-        __syncthreads();
-        prefix = found[0];
-        want = (int)found[1];
-    }
-    // keys above the threshold, and the first `want` that equal it
-    int taken = 0, equal = 0;
-    for (int i0 = 0; i0 < len; i0 += kSelThreads) {
-        const int i = i0 + tid;
-        const uint32_t k = i < len ? key[i] : 0u;
-        const bool above = i < len && k > prefix, same = i < len && k == prefix;
-        int total;
-        const int before = scan_exclusive((above ? 1 : 0) | (same ? 0x10000 : 0), sums, total);
-        const int same_before = equal + (before >> 16);
-        if (above || (same && same_before < want)) {
-            const int at = taken + (before & 0xffff) + min(same_before, want);
-            list[at] = i;
-            if (kept) kept[(int64_t)b * max_keep + at] = i;
-        }
-        taken += total & 0xffff;
-        equal += total >> 16;
     }
 }
 
-// PPL: 16-byte pieces of a row a lane moves, ROWS: rows of a wave
-template <int PPL, int ROWS>
-__global__ __launch_bounds__(kThreads) void evict_move_kernel(const Paged pg, int n_kv_heads, int pieces_per_row, const int32_t *__restrict__ list, const int32_t *__restrict__ counts,
-                                                              const int32_t *__restrict__ new_table, int new_width, uint4 *k_pool, uint4 *v_pool,
-                                                              const float *__restrict__ mass, int64_t mass_stride, float *__restrict__ new_mass, int max_keep)
+__global__ __launch_bounds__(kSelThreads) void evict_keys_kernel(const Paged pg, int n_kv_heads, const int32_t *__restrict__ keep, int max_keep, int n_first, int n_recent,
+                                                              const float *__restrict__ mass, int64_t mass_stride, uint32_t *__restrict__ keys, int64_t stride, uint32_t *__restrict__ firsts)
+{
+    __shared__ int hist[kBins];
+    const int b = blockIdx.y, tid = threadIdx.x, lo = (int)blockIdx.x * kSeg;
+    const int len = len_of(pg, b);
+    if (lo >= len) return;
+    const int m = kept_of(keep, max_keep, b, len);
+#pragma unroll
+    for (int j = 0; j < kBins / kSelThreads; ++j) hist[tid + j * kSelThreads] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSeg / kSelThreads; ++j) {
+        const int64_t i = lo + tid + j * kSelThreads;
+        if (i < len) {
+            const uint32_t key = key_of(pg, b, (int)i, len, m, n_first, n_recent, n_kv_heads, mass, mass_stride);
+            keys[(int64_t)b * stride + i] = key;
+            atomicAdd(&hist[key >> 21], 1);
+        }
+    }
+    __syncthreads();
+    uint32_t *to = firsts + ((int64_t)b * gridDim.x + blockIdx.x) * (kBins / 2);       // two counts of at most kSeg a word
+    static_assert(kBins == 2 * kSelThreads, "a word a thread");
+    to[tid] = (uint32_t)hist[2 * tid] | (uint32_t)hist[2 * tid + 1] << 16;
+}
+
+__global__ __launch_bounds__(kSelThreads) void evict_pick_kernel(const Paged pg, const int32_t *keep, int max_keep, const uint32_t *__restrict__ keys, int64_t stride,
+                                                                 const uint32_t *__restrict__ firsts, int segs, Picked *__restrict__ picked, int32_t *new_len)
+{
+    extern __shared__ uint32_t aside_s[];                    // kAside keys a wave
+    __shared__ int hist[kBins];
+    __shared__ int sums[kSelWaves], found[2], too_many;
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const int len = len_of(pg, b);
+    const int m = kept_of(keep, max_keep, b, len);
+    uint32_t *const aside = aside_s + (tid >> 6) * kAside;
+    uint32_t key = 0xffffffffu;
+    int want = m;
+    if (m > 0) {
+        const int live = (len + kSeg - 1) / kSeg;
+        int large = 0, small = 0;                            // word kBins / 2 - 1 - tid
+#pragma unroll 32
+        for (int s = 0; s < live; ++s) {
+            const uint32_t w = firsts[((int64_t)b * segs + s) * (kBins / 2) + kBins / 2 - 1 - tid];
+            large += (int)(w >> 16);
+            small += (int)(w & 0xffffu);
+        }
+        hist[tid] = hist[tid + kSelThreads] = 0;
+        if (tid == 0) too_many = 0;
+        uint32_t digit;
+        find_digit(large, small, sums, found, digit, want);
+        key = digit;
+        const uint4 *from = reinterpret_cast<const uint4 *>(keys + (int64_t)b * stride);
+        int n_aside = 0;                                     // of the wave
+        auto take = [&](uint32_t k, int i) {
+            const bool mine = i < len && k >> 21 == key;
+            const unsigned long long all = __ballot(mine);
+            if (mine) {
+                atomicAdd(&hist[(k >> 10) & 2047u], 1);
+                const int at = n_aside + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u));
+                if (at < kAside) aside[at] = k;
+            }
+            n_aside += __popcll(all);
+        };
+        constexpr int U = 8;
+        for (int i0 = 0; i0 < len; i0 += 4 * U * kSelThreads) {
+            uint4 k[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + 4 * (u * kSelThreads + tid);
+                k[u] = i < len ? from[i / 4] : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + 4 * (u * kSelThreads + tid);
+                take(k[u].x, i); take(k[u].y, i + 1); take(k[u].z, i + 2); take(k[u].w, i + 3);
+            }
+        }
+        if (n_aside > kAside) too_many = 1;
+        __syncthreads();
+        find_digit(hist[kBins - 1 - 2 * tid], hist[kBins - 2 - 2 * tid], sums, found, digit, want);
+        key = key << 11 | digit;
+        hist[tid] = hist[tid + kSelThreads] = 0;
+        __syncthreads();
+        if (!too_many) {
+            for (int i = tid & 63; i < n_aside; i += kWave)
+                if (aside[i] >> 10 == key) atomicAdd(&hist[aside[i] & 1023u], 1);
+        } else {
+            for (int i = tid; i < len; i += kSelThreads) {
+                const uint32_t k = keys[(int64_t)b * stride + i];
+                if (k >> 10 == key) atomicAdd(&hist[k & 1023u], 1);
+            }
+        }
+        __syncthreads();
+        find_digit(hist[kBins - 1 - 2 * tid], hist[kBins - 2 - 2 * tid], sums, found, digit, want);
+        key = key << 10 | digit;
+    }
+    if (tid == 0) {
+        picked[b] = {key, want, m, len};
+        if (new_len) new_len[b] = m;
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void evict_count_kernel(const uint32_t *__restrict__ keys, int64_t stride, const Picked *__restrict__ picked, int2 *__restrict__ counts, int subs)
 {
     const int b = blockIdx.y, lane = threadIdx.x & 63;
-    const int64_t j0 = ((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) * ROWS;
-    const int m = counts[b];
-    if (j0 >= m) return;
-    list += (int64_t)b * pg.max_ctx;
-    Paged to = pg;
-    to.table = new_table;
-    to.width = new_width;
-    int64_t from_row[ROWS], to_row[ROWS];
+    const int sub = (int)blockIdx.x * kWaves + (threadIdx.x >> 6);          // a wave for kSub rows
+    const Picked p = picked[b];
+    if (sub >= subs || (int64_t)sub * kSub >= p.len) return;
+    int above = 0, equal = 0;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const int j = (int)j0 + r;
-        const int i = list[min(j, m - 1)];
-        const int from = granule_of(pg, b, i / kGranule), into = new_table && j < m ? granule_of(to, b, j / kGranule) : -1;
-        from_row[r] = from < 0 ? -1 : (int64_t)from * kGranule + i % kGranule;
-        to_row[r] = into < 0 ? -1 : (int64_t)into * kGranule + j % kGranule;
-        if (new_mass && j < m && lane < n_kv_heads) new_mass[((int64_t)b * n_kv_heads + lane) * max_keep + j] = mass[((int64_t)b * n_kv_heads + lane) * mass_stride + i];
+    for (int j = 0; j < kSub / kWave; ++j) {
+        const int64_t i = (int64_t)sub * kSub + j * kWave + lane;
+        const uint32_t k = i < p.len ? keys[(int64_t)b * stride + i] : 0u;
+        above += __popcll(__ballot(i < p.len && k > p.key));
+        equal += __popcll(__ballot(i < p.len && k == p.key));
     }
-    uint4 kv[ROWS][PPL], vv[ROWS][PPL];
+    if (lane == 0) counts[(int64_t)b * subs + sub] = make_int2(above, equal);
+}
+
+// PPL: 16-byte pieces of a row a lane moves, ROWS: rows of a wave at a time
+template <int PPL, int ROWS>
+__global__ __launch_bounds__(kThreads) void evict_move_kernel(const Paged pg, int n_kv_heads, int pieces_per_row, const uint32_t *__restrict__ keys, int64_t stride,
+                                                              const Picked *__restrict__ picked, const int2 *__restrict__ counts, int subs,
+                                                              const int32_t *__restrict__ new_table, int new_width, uint4 *k_pool, uint4 *v_pool, const float *__restrict__ mass,
+                                                              int64_t mass_stride, int32_t *__restrict__ kept, float *__restrict__ new_mass, int max_keep)
+{
+    __shared__ int sums[kWaves];
+    __shared__ int4 move_s[kSub];                            // 16 rows of the pool each way, and the row among them
+    const int b = blockIdx.y, sub = blockIdx.x, part = blockIdx.z, parts = gridDim.z, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Picked p = picked[b];
+    const int64_t i = (int64_t)sub * kSub + tid;
+    if ((int64_t)sub * kSub >= p.len || p.m == 0) return;
+    const uint32_t key = i < p.len ? keys[(int64_t)b * stride + i] : 0u;
+    int above = 0, equal = 0;                                // before the workgroup's rows
+    for (int s = tid; s < sub; s += kThreads) {
+        const int2 c = counts[(int64_t)b * subs + s];
+        above += c.x;
+        equal += c.y;
+    }
+    int total;
+    scan_exclusive<kWaves>(above, sums, total);
+    above = total;
+    scan_exclusive<kWaves>(equal, sums, total);
+    equal = total;
+    const bool is_above = i < p.len && key > p.key, is_equal = i < p.len && key == p.key;
+    const int before = scan_exclusive<kWaves>((is_above ? 1 : 0) | (is_equal ? 0x10000 : 0), sums, total);
+    const int equal_before = equal + (before >> 16);
+    const int first = above + min(equal, p.want);            // rank of the workgroup's first kept row
+    const int n = above + (total & 0xffff) + min(equal + (total >> 16), p.want) - first;
+    if (is_above || (is_equal && equal_before < p.want)) {
+        const int rank = above + (before & 0xffff) + min(equal_before, p.want);
+        if (kept && part == 0) kept[(int64_t)b * max_keep + rank] = (int)i;
+        for (int g = part; new_mass && g < n_kv_heads; g += parts)
+            new_mass[((int64_t)b * n_kv_heads + g) * max_keep + rank] = mass[((int64_t)b * n_kv_heads + g) * mass_stride + i];
+        if (new_table) {
+            Paged to = pg;
+            to.table = new_table;
+            to.width = new_width;
+            const int from = granule_of(pg, b, (int)i / kGranule), into = granule_of(to, b, rank / kGranule);
+            move_s[rank - first] = make_int4(max(from, 0), from < 0 ? -1 : into, (int)i % kGranule, rank % kGranule);
+        }
+    }
+    if (!new_table) return;
+    __syncthreads();
+    for (int r0 = (part * kWaves + wave) * ROWS; r0 < n; r0 += parts * kWaves * ROWS) {
+        uint4 kv[ROWS][PPL], vv[ROWS][PPL];
+        int64_t to_row[ROWS];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+        for (int r = 0; r < ROWS; ++r) {
+            const int4 mv = move_s[min(r0 + r, n - 1)];
+            const int64_t from_row = (int64_t)mv.x * kGranule + mv.z;
+            to_row[r] = r0 + r < n && mv.y >= 0 ? (int64_t)mv.y * kGranule + mv.w : -1;
 #pragma unroll
-        for (int i = 0; i < PPL; ++i) {
-            const int piece = lane + i * kWave;
-            if (from_row[r] >= 0 && to_row[r] >= 0 && piece < pieces_per_row) {
-                kv[r][i] = k_pool[from_row[r] * pieces_per_row + piece];
-                vv[r][i] = v_pool[from_row[r] * pieces_per_row + piece];
+            for (int u = 0; u < PPL; ++u) {
+                const int piece = min(lane + u * kWave, pieces_per_row - 1);
+                kv[r][u] = stream_load16(k_pool + from_row * pieces_per_row + piece);
+                vv[r][u] = stream_load16(v_pool + from_row * pieces_per_row + piece);
             }
         }
+        asm volatile("" ::: "memory");                       // all loads before the first store
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+        for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int i = 0; i < PPL; ++i) {
-            const int piece = lane + i * kWave;
-            if (from_row[r] >= 0 && to_row[r] >= 0 && piece < pieces_per_row) {
-                k_pool[to_row[r] * pieces_per_row + piece] = kv[r][i];
-                v_pool[to_row[r] * pieces_per_row + piece] = vv[r][i];
+            for (int u = 0; u < PPL; ++u) {
+                const int piece = lane + u * kWave;
+                if (to_row[r] >= 0 && piece < pieces_per_row) {
+                    k_pool[to_row[r] * pieces_per_row + piece] = kv[r][u];
+                    v_pool[to_row[r] * pieces_per_row + piece] = vv[r][u];
+                }
             }
-        }
+    }
+}
+
+struct Layout { int64_t stride, subs, segs; size_t picked, counts, keys, firsts, bytes; };
+
+Layout layout_of(int64_t batch, int64_t max_ctx)
+{
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    Layout l;
+    l.stride = (max_ctx + 63) / 64 * 64;
+    l.subs = (max_ctx + kSub - 1) / kSub;
+    l.segs = max_ctx > kSmall ? (max_ctx + kSeg - 1) / kSeg : 0;
+    l.picked = 0;
+    l.counts = up((size_t)batch * sizeof(Picked));
+    l.keys = l.counts + up((size_t)batch * (size_t)l.subs * sizeof(int2));
+    l.firsts = l.keys + up((size_t)batch * (size_t)l.stride * 4);
+    l.bytes = l.firsts + up((size_t)batch * (size_t)l.segs * (kBins / 2) * 4);
+    return l;
 }
 
 } // namespace
 
 size_t evict_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx)
 {
-    if (check_shape(shape) != KVS_OK || batch <= 0 || max_ctx <= 0) return 256;
-    return (((size_t)batch * 4 + (size_t)batch * (size_t)max_ctx * 8) + 511) / 256 * 256;
+    if (check_shape(shape) != KVS_OK || batch <= 0) return 256;
+    return layout_of(batch, max_ctx).bytes;
 }
 
 } // namespace kvs
@@ -195,25 +367,42 @@ extern "C" kvs_status kvs_evict_paged(const kvs_shape *shape, const kvs_paged_ca
     if (mass == new_mass) return fail(KVS_EINVAL, "%s: new_mass may not be mass", me);
     if (!workspace || workspace_bytes < evict_paged_workspace_bytes(shape, pages->batch, pg.max_ctx)) return fail(KVS_EWORKSPACE, "%s: workspace too small", me);
     hipStream_t hs = (hipStream_t)stream;
-    const int64_t stride = pg.max_ctx;
-    uint32_t *keys = (uint32_t *)workspace;
-    int32_t *list = (int32_t *)(keys + (int64_t)pg.batch * stride);
-    int32_t *counts = list + (int64_t)pg.batch * stride;
-    if (stride > 0) {
-        hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)((stride + kThreads - 1) / kThreads), (unsigned)pg.batch), dim3(kThreads), 0, hs, pg, shape->n_kv_heads, keep, (int)max_keep,
-                           n_first, n_recent, mass, mass_stride, keys);
+    if (pg.max_ctx == 0) max_keep = 0;
+    const Layout l = layout_of(pg.batch, pg.max_ctx);
+    char *ws = (char *)workspace;
+    Picked *picked = (Picked *)(ws + l.picked);
+    int2 *counts = (int2 *)(ws + l.counts);
+    uint32_t *keys = (uint32_t *)(ws + l.keys), *firsts = (uint32_t *)(ws + l.firsts);
+    const dim3 threads(kThreads), requests((unsigned)pg.batch);
+    if (!l.segs) {
+        hipLaunchKernelGGL(evict_small_kernel, requests, dim3(kSelThreads), 0, hs, pg, shape->n_kv_heads, keep, (int)max_keep, n_first, n_recent, mass, mass_stride, keys, l.stride, picked,
+                           counts, (int)l.subs, new_len);
+    } else {
+        static DeviceOnce once;
+        constexpr int lds = kAside * kSelWaves * 4;
+        st = once_per_device(once, [&]() -> kvs_status {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&evict_pick_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_evict_paged: %s", hipGetErrorString(e));
+        });
+        if (st != KVS_OK) return st;
+        hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)l.segs, (unsigned)pg.batch), dim3(kSelThreads), 0, hs, pg, shape->n_kv_heads, keep, (int)max_keep, n_first, n_recent, mass, mass_stride,
+                           keys, l.stride, firsts);
         if ((st = check_launch(me)) != KVS_OK) return st;
+        hipLaunchKernelGGL(evict_pick_kernel, requests, dim3(kSelThreads), lds, hs, pg, keep, (int)max_keep, keys, l.stride, firsts, (int)l.segs, picked, new_len);
+        if ((st = check_launch(me)) != KVS_OK) return st;
+        hipLaunchKernelGGL(evict_count_kernel, dim3((unsigned)((l.subs + kWaves - 1) / kWaves), (unsigned)pg.batch), threads, 0, hs, keys, l.stride, picked, counts, (int)l.subs);
     }
-    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)pg.batch), dim3(kSelThreads), 0, hs, pg, keep, (int)max_keep, n_first, n_recent, keys, list, counts, kept, new_len);
     if ((st = check_launch(me)) != KVS_OK) return st;
-    if (max_keep == 0 || stride == 0 || (!new_table && !new_mass)) return KVS_OK;
+    if (max_keep == 0 || (!new_table && !new_mass && !kept)) return KVS_OK;
     const int ppr = (int)(shape->n_kv_heads * shape->head_dim * (int64_t)elem_bytes(shape->dtype) / 16);
     const int ppl = (ppr + kWave - 1) / kWave;
-    const int64_t most = max_keep < stride ? max_keep : stride;
+    // Short contexts do not fill the chip with a workgroup for every kSub rows: several rank the same rows then, and copy a part each.
+    int64_t parts = 1024 / (l.subs * pg.batch);
+    parts = parts < 1 || !new_table ? 1 : parts > 8 ? 8 : parts;
 #define KVS_MOVE(P, R)                                                                                                                            \
-    hipLaunchKernelGGL((evict_move_kernel<P, R>), dim3((unsigned)((most + (R) * kWaves - 1) / ((R) * kWaves)), (unsigned)pg.batch), dim3(kThreads), 0, hs, pg, \
-                       shape->n_kv_heads, ppr, list, counts, new_table, new_width, (uint4 *)cache->k, (uint4 *)cache->v, mass, mass_stride, new_mass, (int)max_keep)
-    if (ppl <= 1) KVS_MOVE(1, 4);
+    hipLaunchKernelGGL((evict_move_kernel<P, R>), dim3((unsigned)l.subs, (unsigned)pg.batch, (unsigned)parts), threads, 0, hs, pg, shape->n_kv_heads, ppr, keys, l.stride, picked, counts, (int)l.subs, \
+                       new_table, new_width, (uint4 *)cache->k, (uint4 *)cache->v, mass, mass_stride, kept, new_mass, (int)max_keep)
+    if (ppl <= 1) KVS_MOVE(1, 8);
     else if (ppl <= 2) KVS_MOVE(2, 4);
     else if (ppl <= 4) KVS_MOVE(4, 2);
     else if (ppl <= 8) KVS_MOVE(8, 1);
