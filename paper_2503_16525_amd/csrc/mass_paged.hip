@@ -8,6 +8,7 @@
 #include "paged.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace kvs {
 namespace {
@@ -16,7 +17,8 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kRows = 32;
+constexpr int kRows = 32;               // rows of a tile
+constexpr int kStep = 64;               // rows between two barriers
 constexpr int kMaxPieces = 16;
 template <int DTYPE> constexpr int kBlocks = DTYPE == KVS_F32 ? 1 : 2;             // of 32 keys a wave
 template <int DTYPE> constexpr int kWgKeys = 32 * kBlocks<DTYPE> * kWaves;
@@ -33,11 +35,14 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
     constexpr int CPR = ROW_B / 16;
     constexpr int NB = kBlocks<DTYPE>;
     constexpr int NS = CPR / 2;                              // products of a tile (fp32: four each)
-    constexpr int NQ = kRows * CPR / kThreads;               // chunks of a row tile a thread moves
-    __shared__ __attribute__((aligned(16))) char q_s[2][kRows * ROW_B];
-    __shared__ __attribute__((aligned(16))) float lse_s[2][kRows];
-    __shared__ __attribute__((aligned(16))) int pos_s[2][kRows];
-    __shared__ int span_s[2][3];                             // lowest position, highest, lowest of those that see anything
+    constexpr int RPL = kWave / CPR;                         // rows a load moves
+    constexpr int NQ = kStep / RPL / kWaves;                 // loads of a wave for a step's rows
+    constexpr int NT = kStep / kRows;                        // tiles of a step
+    __shared__ __attribute__((aligned(16))) char q_s[2][kStep * ROW_B];
+    __shared__ __attribute__((aligned(16))) float lse_s[2][kThreads];       // of a workgroup's number of rows
+    __shared__ __attribute__((aligned(16))) int pos_s[2][kThreads];
+    __shared__ int span_s[2][kWaves][3];                     // of a step: lowest position, highest, lowest of those that see anything
+    static_assert(kStep == kWave, "a wave looks after a step's rows");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -55,8 +60,8 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
     tokens_of(pg, b, tok0, n_tok);
     const int grp = n_q_heads / n_kv_heads;
     const int rows = n_tok * grp;
-    const int row_blocks = (rows + kRows - 1) / kRows, per_piece = (row_blocks + pieces - 1) / pieces;
-    const int rb_lo = min(piece * per_piece, row_blocks), rb_hi = min(rb_lo + per_piece, row_blocks);
+    const int steps = (rows + kStep - 1) / kStep, per_piece = (steps + pieces - 1) / pieces;
+    const int st_lo = min(piece * per_piece, steps), st_hi = min(st_lo + per_piece, steps);
 
     // ---- keys ---------------------------------------------------------------------------------------------------
     u32x4_t kreg[NB][NS];
@@ -73,109 +78,152 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
 
     // ---- rows ---------------------------------------------------------------------------------------------------
     auto swz = [](int r) { return CPR >= 16 ? (r & 15) : (r & 7); };
+    // Rows go from memory straight into LDS, 16 bytes a lane; chunk c of row r lies at c ^ swz(r).  A step is the same number of bytes
+    // further on for every lane where the query heads of a KV head divide 64; else its lanes follow their rows by additions.
+    // (By hand: the compiler would wait for all loads in flight before every LDS read.)
+    const int dh = kStep % grp, info_dt = kThreads / grp, info_dh = kThreads % grp;
+    const int64_t stride = (int64_t)n_q_heads * ROW_B, inc = (int64_t)(kStep / grp) * stride;
+    const int wrap = (n_q_heads - grp) * ROW_B;
+    const char *q_base = q_new + ((int64_t)tok0 * n_q_heads + g * grp) * ROW_B + st_lo * inc;
+    const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&q_s[0][0]);
     struct Row { int t, h; };
     auto row_at = [&](int r) { return Row{r / grp, r % grp}; };
-    const int dt = kRows / grp, dh = kRows % grp;
-    auto advance = [&](Row &r) {
-        r.t += dt;
-        r.h += dh;
-        if (r.h >= grp) { r.h -= grp; ++r.t; }
-    };
-    Row mine[NQ], info = row_at(rb_lo * kRows + ln);
+    Row info = row_at(st_lo * kStep + tid);
+    int64_t q_off[NQ];                                       // from q_base
+    int q_head[NQ];
 #pragma unroll
-    for (int j = 0; j < NQ; ++j) mine[j] = row_at(rb_lo * kRows + (tid + j * kThreads) / CPR);
-    u32x4_t q_next[NQ];
+    for (int j = 0; j < NQ; ++j) {
+        const int r = (j * kWaves + wave) * RPL + lane / CPR;
+        const Row at = row_at(st_lo * kStep + r);
+        q_off[j] = at.t * stride - st_lo * inc + at.h * ROW_B + ((lane % CPR) ^ swz(r)) * 16;
+        q_head[j] = at.h;
+    }
     float lse_next = 0.f;
     int pos_next = -1;
-    auto fetch = [&]() {
+    auto stage = [&](int st) {
+        const uint32_t dst = lds_base + (uint32_t)(((st - st_lo) & 1) * (kStep * ROW_B) + wave * 1024);
+        if (dh == 0 && (st + 1) * kStep <= rows) {
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            q_next[j] = u32x4_t{0u, 0u, 0u, 0u};
-            if (mine[j].t < n_tok)
-                q_next[j] = *reinterpret_cast<const u32x4_t *>(q_new + ((int64_t)(tok0 + mine[j].t) * n_q_heads + g * grp + mine[j].h) * ROW_B + ((tid + j * kThreads) % CPR) * 16);
-            advance(mine[j]);
-        }
-        if (wave == 0) {
-            pos_next = -1;
-            lse_next = 0.f;
-            if (info.t < n_tok) {
-                lse_next = lse[(int64_t)(tok0 + info.t) * n_q_heads + g * grp + info.h] * 1.4426950408889634f;
-                pos_next = position_of(pg, tok0, n_tok, info.t, len);
-                if (lse_next == -INFINITY) pos_next = -1;    // saw nothing
+            for (int j = 0; j < NQ; ++j)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst + j * (kWaves * 1024)), "v"((uint32_t)q_off[j]), "s"(q_base) : "memory");
+        } else {
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) {
+                const int r = st * kStep + (j * kWaves + wave) * RPL + lane / CPR;
+                const char *from = r < rows ? q_base + q_off[j] : q_new;     // (rows behind the last: any)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(dst + j * (kWaves * 1024)), "v"(from) : "memory");
+                q_head[j] += dh;
+                const bool over = q_head[j] >= grp;
+                q_head[j] -= over ? grp : 0;
+                q_off[j] += dh * ROW_B + (over ? wrap : 0);
             }
-            advance(info);
         }
+        q_base += inc;
+    };
+    auto fetch_info = [&]() {
+        pos_next = -1;
+        lse_next = 0.f;
+        if (info.t < n_tok) {
+            lse_next = lse[(int64_t)(tok0 + info.t) * n_q_heads + g * grp + info.h] * 1.4426950408889634f;
+            pos_next = position_of(pg, tok0, n_tok, info.t, len);
+            if (lse_next == -INFINITY) pos_next = -1;        // saw nothing
+        }
+        info.t += info_dt;
+        info.h += info_dh;
+        if (info.h >= grp) { info.h -= grp; ++info.t; }
     };
     const int window = pg.window, n_first = window ? pg.n_first : 0;
     float acc[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) acc[nb] = 0.f;
-    if (rb_lo < rb_hi) fetch();
-    for (int rb = rb_lo; rb < rb_hi; ++rb) {
-        const int buf = (rb - rb_lo) & 1;
-#pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            const int r = (tid + j * kThreads) / CPR, c = (tid + j * kThreads) % CPR;
-            *reinterpret_cast<u32x4_t *>(q_s[buf] + r * ROW_B + (c ^ swz(r)) * 16) = q_next[j];
-        }
-        if (wave == 0) {
+    if (st_lo < st_hi) { fetch_info(); stage(st_lo); }
+    for (int st = st_lo; st < st_hi; ++st) {
+        const int buf = (st - st_lo) & 1, sub = (st - st_lo) % kWaves, ibuf = ((st - st_lo) / kWaves) & 1;
+        if (sub == 0) {
             int lo = pos_next, hi = pos_next, low = pos_next < 0 ? 0x7fffffff : pos_next;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
+            for (int o = 1; o < 64; o <<= 1) {
                 lo = min(lo, __shfl_xor(lo, o));
                 hi = max(hi, __shfl_xor(hi, o));
                 low = min(low, __shfl_xor(low, o));
             }
-            if (hf == 0) { lse_s[buf][ln] = lse_next; pos_s[buf][ln] = pos_next; }
-            if (lane == 0) { span_s[buf][0] = lo; span_s[buf][1] = hi; span_s[buf][2] = low; }
+            lse_s[ibuf][tid] = lse_next;
+            pos_s[ibuf][tid] = pos_next;
+            if (lane == 0) { span_s[ibuf][wave][0] = lo; span_s[ibuf][wave][1] = hi; span_s[ibuf][wave][2] = low; }
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the step's rows have landed
         __syncthreads();
-        if (rb + 1 < rb_hi) fetch();
-        const int pmin = __builtin_amdgcn_readfirstlane(span_s[buf][0]), pmax = __builtin_amdgcn_readfirstlane(span_s[buf][1]), plow = __builtin_amdgcn_readfirstlane(span_s[buf][2]);
+        if (st + 1 < st_hi) {
+            stage(st + 1);
+            if (sub == kWaves - 1) fetch_info();
+        }
+        const int pmin = __builtin_amdgcn_readfirstlane(span_s[ibuf][sub][0]), pmax = __builtin_amdgcn_readfirstlane(span_s[ibuf][sub][1]), plow = __builtin_amdgcn_readfirstlane(span_s[ibuf][sub][2]);
         if (pmax < wg_lo || (window && wg_hi <= plow - window && wg_lo >= n_first)) continue;
         const bool masked = wg_hi > pmin || (window && wg_lo <= pmax - window && wg_hi >= n_first);
-        floatx16 s[NB];
+        auto scores = [&](int t, floatx16 (&s)[NB]) {
+            const int r = t * kRows + ln;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[nb][r] = 0.f;
+                for (int i = 0; i < 16; ++i) s[nb][i] = 0.f;
 #pragma unroll
-        for (int c = 0; c < NS; ++c) {
-            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(q_s[buf] + ln * ROW_B + ((2 * c + hf) ^ swz(ln)) * 16);
+            for (int c = 0; c < NS; ++c) {
+                const u32x4_t w = *reinterpret_cast<const u32x4_t *>(q_s[buf] + r * ROW_B + ((2 * c + hf) ^ swz(r)) * 16);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                if constexpr (F32) {
+                for (int nb = 0; nb < NB; ++nb) {
+                    if constexpr (F32) {
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) s[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[u]), __uint_as_float(kreg[nb][c][u]), s[nb], 0, 0, 0);
-                } else {
-                    s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w), as_bf16x8(kreg[nb][c]), s[nb], 0, 0, 0);
+                        for (int u = 0; u < 4; ++u) s[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[u]), __uint_as_float(kreg[nb][c][u]), s[nb], 0, 0, 0);
+                    } else {
+                        s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w), as_bf16x8(kreg[nb][c]), s[nb], 0, 0, 0);
+                    }
                 }
             }
-        }
-        float sum[NB];
+        };
+        auto add_up = [&](int t, const floatx16 (&s)[NB], auto with_mask) {
+            const int r0 = sub * kStep + t * kRows + 4 * hf;
+            float sum[NB];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) sum[nb] = 0.f;
+            for (int nb = 0; nb < NB; ++nb) sum[nb] = 0.f;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {                        // entry 4 q + u is row 8 q + 4 hf + u
-            const float4 l4 = *reinterpret_cast<const float4 *>(&lse_s[buf][8 * q + 4 * hf]);
-            const float l[4] = {l4.x, l4.y, l4.z, l4.w};
-            const int4 p4 = *reinterpret_cast<const int4 *>(&pos_s[buf][8 * q + 4 * hf]);
-            const int p[4] = {p4.x, p4.y, p4.z, p4.w};
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                float e[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) e[u] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][4 * q + u], scale_log2, -l[u]));
-                if (masked) {
-                    const int key = wg_lo + (wave * NB + nb) * 32 + ln;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) e[u] = key <= p[u] && (!window || key > p[u] - window || key < n_first) ? e[u] : 0.f;
+            for (int q = 0; q < 4; ++q) {                    // entry 4 q + u is row 8 q + 4 hf + u
+                const float4 l4 = *reinterpret_cast<const float4 *>(&lse_s[ibuf][r0 + 8 * q]);
+                const float l[4] = {l4.x, l4.y, l4.z, l4.w};
+                int p[4] = {};
+                if constexpr (decltype(with_mask)::value) {
+                    const int4 p4 = *reinterpret_cast<const int4 *>(&pos_s[ibuf][r0 + 8 * q]);
+                    p[0] = p4.x; p[1] = p4.y; p[2] = p4.z; p[3] = p4.w;
                 }
-                sum[nb] += (e[0] + e[1]) + (e[2] + e[3]);
-            }
-        }
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) acc[nb] += sum[nb];
+                for (int nb = 0; nb < NB; ++nb) {
+                    float e[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) e[u] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][4 * q + u], scale_log2, -l[u]));
+                    if constexpr (decltype(with_mask)::value) {
+                        const int key = wg_lo + (wave * NB + nb) * 32 + ln;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) e[u] = key <= p[u] && (!window || key > p[u] - window || key < n_first) ? e[u] : 0.f;
+                    }
+                    sum[nb] += (e[0] + e[1]) + (e[2] + e[3]);
+                }
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) acc[nb] += sum[nb];
+        };
+        if (masked) {
+#pragma unroll 1
+            for (int t = 0; t < NT; ++t) {
+                floatx16 s[NB];
+                scores(t, s);
+                add_up(t, s, std::true_type{});
+            }
+        } else {
+            floatx16 s[NT][NB];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) scores(t, s[t]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) add_up(t, s[t], std::false_type{});
+        }
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -189,6 +237,179 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
             const int64_t at = ((int64_t)b * n_kv_heads + g) * mass_stride + key;
             mass_out[at] = mass ? __builtin_fmaf(decay, mass[at], total) : total;
         }
+    }
+}
+
+// Few rows a request, a decode step's: the cache's bytes bound it, half of what the attention itself reads.  A wave holds the rows as
+// operands and takes every fourth tile of 32 keys of the workgroup's piece, two of them on their way into LDS slots of its own
+// (global to LDS, 16 bytes a lane, no registers, no barrier).  Sums of kFlush tiles wait in LDS until they are added to the
+// mass that was: loads and stores of its own in every tile would have to be waited for in order with the keys.
+// Requests of more than 32 rows, which the host cannot see, come here too where there are few on average: block by block.
+constexpr int kFlush = 16;
+
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kThreads, 2) void mass_few_kernel(
+    const Paged pg, int n_q_heads, int n_kv_heads, int pieces, int piece_tiles, const char *__restrict__ k_pool, const char *__restrict__ q_new,
+    const float *__restrict__ lse, float scale_log2, float decay, const float *mass, float *mass_out, int64_t mass_stride)
+{
+    constexpr bool F32 = DTYPE == KVS_F32;
+    constexpr int ROW_B = D * (F32 ? 4 : 2);
+    constexpr int CPR = ROW_B / 16;
+    constexpr int NS = CPR / 2;
+    constexpr int RPL = kWave / CPR;                         // rows a load moves
+    constexpr int NH = kGranule / RPL, NL = 2 * NH;          // loads of half a tile, of a tile
+    constexpr int TILE_B = 32 * ROW_B;
+    extern __shared__ __attribute__((aligned(16))) char lds[];       // two slots a wave
+    __shared__ float sum_s[kWaves][kFlush][32];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hf = lane >> 5, ln = lane & 31;
+    const int g = (int)(blockIdx.x % (uint32_t)n_kv_heads);
+    const int rest = (int)(blockIdx.x / (uint32_t)n_kv_heads);
+    const int b = rest % pg.batch, piece = rest / pg.batch;
+    const int len = len_of(pg, b);
+    const int tiles = (len + 31) / 32;
+    const int p_lo = (int)min((int64_t)piece * piece_tiles, (int64_t)tiles), p_hi = (int)min((int64_t)p_lo + piece_tiles, (int64_t)tiles);
+    if (p_lo >= p_hi) return;
+    int tok0, n_tok;
+    tokens_of(pg, b, tok0, n_tok);
+    const int grp = n_q_heads / n_kv_heads, rows = n_tok * grp;
+    const int window = pg.window, n_first = window ? pg.n_first : 0;
+    const int64_t out_at = ((int64_t)b * n_kv_heads + g) * mass_stride;
+
+    char *const my_lds = lds + wave * (2 * TILE_B);
+    const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)my_lds);
+    const uint32_t row_bytes = (uint32_t)n_kv_heads * ROW_B;
+    auto swz = [](int r) { return CPR >= 16 ? (r & 15) : (r & 7); };
+    uint32_t k_off[NH];
+#pragma unroll
+    for (int j = 0; j < NH; ++j) {
+        const int r = j * RPL + lane / CPR;
+        k_off[j] = (uint32_t)r * row_bytes + (uint32_t)((lane % CPR) ^ swz(r)) * 16u;
+    }
+    // By hand, as in attention_paged.hip: the compiler would wait for all loads in flight before every LDS read.
+    auto load_1k = [&](uint32_t dst, uint32_t off, const char *base) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(base) : "memory");
+    };
+    const uint64_t granule_bytes = (uint64_t)row_bytes * kGranule;
+
+    const int blocks = max(1, (rows + 31) / 32);             // no rows: everything decays
+    for (int blk = 0; blk < blocks; ++blk) {
+        // ---- rows ---------------------------------------------------------------------------------------------------
+        const int rq = blk * 32 + ln;
+        const int t_own = rows ? min(rq, rows - 1) / grp : 0, h_own = rows ? min(rq, rows - 1) - t_own * grp : 0;
+        int pos = -1;
+        float lse2 = 0.f;
+        u32x4_t qreg[NS];
+#pragma unroll
+        for (int c = 0; c < NS; ++c) qreg[c] = u32x4_t{0u, 0u, 0u, 0u};
+        if (rows) {
+            const int64_t row = (int64_t)(tok0 + t_own) * n_q_heads + g * grp + h_own;
+            pos = rq < rows ? position_of(pg, tok0, n_tok, t_own, len) : -1;
+            lse2 = lse[row] * 1.4426950408889634f;
+            if (lse2 == -INFINITY) pos = -1;                 // saw nothing
+#pragma unroll
+            for (int c = 0; c < NS; ++c) qreg[c] = *reinterpret_cast<const u32x4_t *>(q_new + row * ROW_B + (2 * c + hf) * 16);
+        }
+        int pmin = pos, pmax = pos, plow = pos < 0 ? 0x7fffffff : pos;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            pmin = min(pmin, __shfl_xor(pmin, o));
+            pmax = max(pmax, __shfl_xor(pmax, o));
+            plow = min(plow, __shfl_xor(plow, o));
+        }
+        pmin = __builtin_amdgcn_readfirstlane(pmin);
+        pmax = __builtin_amdgcn_readfirstlane(pmax);
+        plow = __builtin_amdgcn_readfirstlane(plow);
+        float l_of[16];                                      // entry r of a product is row 8 (r >> 2) + 4 hf + (r & 3)
+        int p_of[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            l_of[r] = __shfl(lse2, 8 * (r >> 2) + 4 * hf + (r & 3));
+            p_of[r] = __shfl(pos, 8 * (r >> 2) + 4 * hf + (r & 3));
+        }
+        // ---- the piece's tiles that any of them sees: [p_lo, head) and [low, high) ---------------------------------
+        int low = window && pmax >= 0 ? max(plow - window + 1, 0) / 32 : 0;
+        int head = min(low, (int)(((int64_t)n_first + 31) / 32));
+        const int high = min(p_hi, pmax < 0 ? 0 : pmax / 32 + 1);
+        low = max(low, p_lo);
+        head = max(min(head, high), p_lo);
+        const int total = head - p_lo + max(high - low, 0);
+        const int mine = max(0, (total - wave + kWaves - 1) / kWaves);
+        auto tile_of = [&](int i) { const int t = p_lo + wave + kWaves * i; return t < head ? t : t - head + low; };
+        int place = -1;
+        auto look_up = [&](int i0) {
+            const int i = i0 + (lane >> 1);
+            place = i < mine ? granule_of(pg, b, 2 * tile_of(i) + (lane & 1)) : -1;
+        };
+        auto stage = [&](int i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = max(__builtin_amdgcn_readlane(place, 2 * (i & 31) + h), 0);
+                const char *base = k_pool + (uint64_t)(uint32_t)at * granule_bytes + (uint32_t)g * ROW_B;
+#pragma unroll
+                for (int j = 0; j < NH; ++j) load_1k(lds_base + (uint32_t)((i & 1) * TILE_B + (h * NH + j) * 1024), k_off[j], base);
+            }
+        };
+        // what becomes of a key: in the first block its mass decays
+        auto store = [&](int key, float sum) {
+            if (key >= len) return;
+            const float old = blk ? mass_out[out_at + key] : mass ? mass[out_at + key] : 0.f;
+            mass_out[out_at + key] = blk ? old + sum : __builtin_fmaf(decay, old, sum);
+        };
+        auto flush = [&](int i0, int n) {                    // the sums of tiles i0 .. i0 + n - 1
+            for (int e = lane; e < n * 32; e += kWave) store(tile_of(i0 + e / 32) * 32 + e % 32, sum_s[wave][e / 32][e % 32]);
+        };
+        look_up(0);
+        if (mine > 0) stage(0);
+        if (mine > 1) stage(1);
+        int none_at = place;                                 // of the tiles that are worked on
+        for (int i = 0; i < mine; ++i) {
+            const int x0 = tile_of(i) * 32;
+            if ((i & 31) == 0) none_at = place;
+            const bool none[2] = {__builtin_amdgcn_readlane(none_at, 2 * (i & 31)) < 0, __builtin_amdgcn_readlane(none_at, 2 * (i & 31) + 1) < 0};
+            if (((i + 2) & 31) == 0 && i + 2 < mine) look_up(i + 2);
+            if (i + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NL) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            const char *const kt = my_lds + (i & 1) * TILE_B;
+            floatx16 s;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NS; ++c) {
+                const u32x4_t w = *reinterpret_cast<const u32x4_t *>(kt + ln * ROW_B + ((2 * c + hf) ^ swz(ln)) * 16);
+                if constexpr (F32) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(qreg[c][u]), __uint_as_float(w[u]), s, 0, 0, 0);
+                } else {
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qreg[c]), as_bf16x8(w), s, 0, 0, 0);
+                }
+            }
+            if (i + 2 < mine) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // what lay in the slot has been read
+                stage(i + 2);
+            }
+            const int key = x0 + ln;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const bool seen = key <= p_of[r] && (!window || key > p_of[r] - window || key < n_first);
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], scale_log2, -l_of[r]));
+                sum += seen ? e : 0.f;
+            }
+            sum += __shfl_xor(sum, 32);
+            if (hf == 0) sum_s[wave][i % kFlush][ln] = none[ln >> 4] ? 0.f : sum;
+            if (i % kFlush == kFlush - 1) flush(i + 1 - kFlush, kFlush);
+        }
+        flush(mine - mine % kFlush, mine % kFlush);
+        // ---- and those that none sees -------------------------------------------------------------------------------
+        if (blk == 0 && !(mass == mass_out && decay == 1.f)) {
+            const int gap_lo = head, gap_hi = max(low, head);              // tiles of the piece between the two ranges, and behind them
+            for (int key = max(gap_lo, p_lo) * 32 + tid; key < min(gap_hi, p_hi) * 32; key += kThreads) store(key, 0.f);
+            for (int key = max(max(high, gap_hi), p_lo) * 32 + tid; key < p_hi * 32; key += kThreads) store(key, 0.f);
+        }
+        if (blk + 1 < blocks) __syncthreads();               // (the next rows' tiles may fall to other waves)
     }
 }
 
@@ -213,10 +434,10 @@ inline int64_t blocks_of(const kvs_shape *shape, int64_t max_ctx)
 int pieces_of(const kvs_shape *shape, int64_t batch, int64_t max_ctx, int64_t n_new)
 {
     const int64_t wgs = batch * shape->n_kv_heads * blocks_of(shape, max_ctx);
-    const int64_t row_blocks = n_new * (shape->n_q_heads / shape->n_kv_heads) / (batch * kRows);
+    const int64_t steps = n_new * (shape->n_q_heads / shape->n_kv_heads) / (batch * kStep);
     if (wgs <= 0 || wgs >= 1024 || batch * shape->n_kv_heads > 65535) return 1;
     int64_t p = (2048 + wgs - 1) / wgs;
-    if (p > row_blocks / 8) p = row_blocks / 8;
+    if (p > steps / 4) p = steps / 4;
     if (p > kMaxPieces) p = kMaxPieces;
     return p < 1 ? 1 : (int)p;
 }
@@ -234,11 +455,38 @@ kvs_status launch(const kvs_shape *shape, const kvs_paged_cache *c, const Paged 
     return check_launch("kvs_mass_paged(join)");
 }
 
+template <int DTYPE, int D>
+kvs_status launch_few(const kvs_shape *shape, const kvs_paged_cache *c, const Paged &pg, const void *q, const float *lse, float scale, float decay, const float *mass, float *mass_out,
+                      int64_t mass_stride, hipStream_t hs)
+{
+    static DeviceOnce once;
+    constexpr int lds = kWaves * 2 * 32 * D * (DTYPE == KVS_F32 ? 4 : 2);
+    kvs_status st = once_per_device(once, [&]() -> kvs_status {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&mass_few_kernel<DTYPE, D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_mass_paged: %s", hipGetErrorString(e));
+    });
+    if (st != KVS_OK) return st;
+    const int64_t units = (int64_t)pg.batch * shape->n_kv_heads, tiles = (pg.max_ctx + 31) / 32;
+    int64_t pieces = (2048 + units - 1) / units;
+    if (pieces < (tiles + 127) / 128) pieces = (tiles + 127) / 128;
+    int64_t piece_tiles = (tiles + pieces - 1) / pieces;
+    piece_tiles = piece_tiles < 2 * kWaves ? 2 * kWaves : (piece_tiles + kWaves - 1) / kWaves * kWaves;
+    pieces = (tiles + piece_tiles - 1) / piece_tiles;
+    if (pieces * units > kMostWgs) return fail(KVS_EINVAL, "kvs_mass_paged: too many rows in one call");
+    hipLaunchKernelGGL((mass_few_kernel<DTYPE, D>), dim3((unsigned)(pieces * units)), dim3(kThreads), lds, hs, pg, shape->n_q_heads, shape->n_kv_heads, (int)pieces, (int)piece_tiles,
+                       (const char *)c->k, (const char *)q, lse, scale * 1.4426950408889634f, decay, mass, mass_out, mass_stride);
+    return check_launch("kvs_mass_paged");
+}
+
+// Whether a call's rows are so few that the keys' bytes bound it.
+inline bool few_rows(const kvs_shape *shape, int64_t batch, int64_t n_new) { return n_new * (shape->n_q_heads / shape->n_kv_heads) <= 32 * batch; }
+
 } // namespace
 
 size_t mass_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new)
 {
     if (check_shape(shape) != KVS_OK || batch <= 0 || max_ctx <= 0 || n_new <= 0) return 256;
+    if (few_rows(shape, batch, n_new)) return 256;
     const int p = pieces_of(shape, batch, max_ctx, n_new);
     return p == 1 ? 256 : ((size_t)p * (size_t)batch * shape->n_kv_heads * (size_t)max_ctx * 4 + 255) / 256 * 256;
 }
@@ -264,13 +512,19 @@ extern "C" kvs_status kvs_mass_paged(const kvs_shape *shape, const kvs_paged_cac
     if (!mass_out) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
     if (n_new > 0 && (!q_new || !lse)) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
     if (!aligned16(q_new)) return fail(KVS_EINVAL, "%s: Q must be 16-byte aligned", me);
+    const bool wide = shape->head_dim == 128;
+    hipStream_t hs = (hipStream_t)stream;
+    if (few_rows(shape, pg.batch, n_new)) {
+#define KVS_MF(DT, DD) launch_few<DT, DD>(shape, cache, pg, q_new, lse, scale, decay, mass, mass_out, mass_stride, hs)
+        if (shape->dtype == KVS_F32) return wide ? KVS_MF(KVS_F32, 128) : KVS_MF(KVS_F32, 64);
+        return wide ? KVS_MF(KVS_BF16, 128) : KVS_MF(KVS_BF16, 64);
+#undef KVS_MF
+    }
     const int64_t key_blocks = blocks_of(shape, pg.max_ctx);
     int pieces = pieces_of(shape, pg.batch, pg.max_ctx, n_new);
     const int64_t fit = (int64_t)(workspace_bytes / 4) / ((int64_t)pg.batch * shape->n_kv_heads * pg.max_ctx);
     if (pieces > fit) pieces = fit < 1 ? 1 : (int)fit;
     if (key_blocks * pieces * pg.batch * shape->n_kv_heads > kMostWgs) return fail(KVS_EINVAL, "%s: too many rows in one call", me);
-    const bool wide = shape->head_dim == 128;
-    hipStream_t hs = (hipStream_t)stream;
 #define KVS_MP(DT, DD) launch<DT, DD>(shape, cache, pg, key_blocks, pieces, q_new, lse, scale, decay, mass, mass_out, mass_stride, (float *)workspace, hs)
     if (shape->dtype == KVS_F32) return wide ? KVS_MP(KVS_F32, 128) : KVS_MP(KVS_F32, 64);
     return wide ? KVS_MP(KVS_BF16, 128) : KVS_MP(KVS_BF16, 64);
