@@ -16,7 +16,7 @@
 // At the end the waves meet in LDS.  Launches of too few workgroups cut the keys into pieces, which a second kernel merges.
 //
 // fp32 goes through the fp32 matrix instruction, whose operands need no other order than that of memory.
-#include "paged.h"
+#include "attention_paged.h"
 
 #include <math.h>
 
@@ -30,7 +30,7 @@ constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kRows = 32;              // rows of a block
 constexpr int kKeys = 32;              // keys of a tile
 constexpr float kSlack = 8.f;          // powers of two that a score may lie above its reference
-constexpr int kMaxPieces = 512;
+constexpr int kMaxPieces = kPagedMaxPieces;
 constexpr int kPlaces = 512;           // workgroups that the chip holds at once
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4_t v) { return __builtin_bit_cast(bf16x8, v); }
@@ -50,9 +50,10 @@ __device__ __forceinline__ float max_of_halves(float x)      // of lanes i and i
 }
 
 // PARTS: bf16 numbers that a weight enters the second product as: one, or two that hold 16 of its bits
-template <int DTYPE, int D, int PARTS>
+// AGAIN: the rows of row tiles of 256 whose kernel asks for it (`odd`, a word a workgroup of its), eight blocks each.
+template <int DTYPE, int D, int PARTS, bool AGAIN>
 __global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
-    const Paged pg, int n_q_heads, int n_kv_heads, int units, int pieces, int piece_tiles,
+    const Paged pg, int n_q_heads, int n_kv_heads, int units, int pieces, int piece_tiles, const int32_t *__restrict__ odd,
     const char *__restrict__ k_pool, const char *__restrict__ v_pool, const void *__restrict__ q_new, float scale_log2,
     void *__restrict__ out, float *__restrict__ lse_out, float *__restrict__ part_o, float4 *__restrict__ part_ml)
 {
@@ -80,19 +81,32 @@ __global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
     // together, which share its keys in L2.
     const int g = (int)(blockIdx.x % (uint32_t)n_kv_heads);
     const int rest = (int)(blockIdx.x / (uint32_t)n_kv_heads);
-    const int piece = rest / units;
+    const int piece = AGAIN ? 0 : rest / units;
     const int grp = n_q_heads / n_kv_heads;
     int b, blk;
-    if (!find_block<kRows>(pg, grp, rest - piece * units, b, blk)) return;
+    if constexpr (AGAIN) {
+        constexpr int per = kPagedLargeRows / kRows;
+        const int unit = rest / per;
+        int any = 0;
+        for (int p = 0; p < pieces; ++p) any |= odd[(p * units + unit) * n_kv_heads + g];
+        if (!any || !find_block<kPagedLargeRows>(pg, grp, units - 1 - unit, b, blk)) return;
+        blk = blk * per + rest % per;
+    } else if (!find_block<kRows>(pg, grp, rest - piece * units, b, blk)) {
+        return;
+    }
     b = __builtin_amdgcn_readfirstlane(b);
     blk = __builtin_amdgcn_readfirstlane(blk);
     int tok0, n_tok;
     tokens_of(pg, b, tok0, n_tok);
     const int len = len_of(pg, b);
     const int rows = n_tok * grp;
+    // (row tiles of 256 end with their request's rows)
+    const int row0 = blk * kRows - (AGAIN ? (rows + kPagedLargeRows - 1) / kPagedLargeRows * kPagedLargeRows - rows : 0);
+    if (AGAIN && row0 + kRows <= 0) return;
+    if (AGAIN) { pieces = 1; piece_tiles = 0x7fffffff; }
 
     // ---- this lane's row (both half-waves hold the same 32) ------------------------------------------------
-    const int rq = min(blk * kRows + ln, rows - 1);
+    const int rq = min(max(row0 + ln, 0), rows - 1);
     const int t_own = rq / grp, hh = rq - t_own * grp;
     const int pos = position_of(pg, tok0, n_tok, t_own, len);
     int pmin = pos, pmax = pos, plow = pos < 0 ? 0x7fffffff : pos;        // plow: of those that see anything
@@ -117,7 +131,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
     auto tile_of = [&](int i) { const int t = t_lo + wave + kWaves * i; return t < head ? t : t - head + low; };
 
     if (t_lo >= t_hi && pieces > 1) {                        // nothing for the merge
-        if (wave == 0 && hf == 0 && blk * kRows + ln < rows)
+        if (wave == 0 && hf == 0 && row0 + ln < rows)
             part_ml[((int64_t)(tok0 + t_own) * n_q_heads + g * grp + hh) * pieces + piece] = make_float4(kLowest, 0.f, 0.f, 0.f);
         return;
     }
@@ -377,7 +391,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
         __syncthreads();
         constexpr int CPT = D / 8;                               // channels a thread stores
         const int row = tid >> 3, part = tid & 7;
-        const int row_q = blk * kRows + row;
+        const int row_q = row0 + row;
         float top = kLowest, l = 0.f, lr = 0.f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml_s[w][row].x);
@@ -408,7 +422,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
             __syncthreads();
             if (odd_s) { __syncthreads(); continue; }
         }
-        if (row_q >= rows) return;
+        if (row_q >= rows || row_q < 0) return;
         const int t2 = row_q / grp;
         const int64_t at = (int64_t)(tok0 + t2) * n_q_heads + g * grp + (row_q - t2 * grp);
         if (pieces > 1) {
@@ -514,8 +528,6 @@ __global__ __launch_bounds__(kThreads) void merge_paged_kernel(const Paged pg, i
     if (lse_out && c == 0) lse_out[item] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
-inline size_t slot_bytes(int d) { return (size_t)d * sizeof(float) + sizeof(float4); }
-
 // Tiles that a block of rows may need at most.
 int64_t most_tiles(const Paged &pg, int grp)
 {
@@ -533,7 +545,7 @@ struct Plan { int32_t pieces, tiles; };
 Plan plan_pieces(const kvs_shape *shape, const Paged &pg, int64_t units, size_t workspace_bytes)
 {
     const int64_t wgs = units * shape->n_kv_heads, most = most_tiles(pg, shape->n_q_heads / shape->n_kv_heads);
-    const int64_t slots = (int64_t)(workspace_bytes / slot_bytes(shape->head_dim)) / ((int64_t)pg.n_new * shape->n_q_heads);
+    const int64_t slots = (int64_t)(workspace_bytes / paged_slot_bytes(shape->head_dim)) / ((int64_t)pg.n_new * shape->n_q_heads);
     int64_t pieces = (4 * kPlaces + wgs - 1) / wgs;
     if (pieces > slots) pieces = slots;
     if (pieces > kMaxPieces) pieces = kMaxPieces;
@@ -552,21 +564,46 @@ kvs_status launch(const kvs_shape *shape, const kvs_paged_cache *c, const Paged 
     constexpr int es = DTYPE == KVS_F32 ? 4 : 2;
     constexpr int lds = kWaves * 2 * kKeys * D * es;
     kvs_status st = once_per_device(once, [&]() -> kvs_status {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_paged_kernel<DTYPE, D, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_paged_kernel<DTYPE, D, PARTS, false>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_attention_paged: %s", hipGetErrorString(e));
     });
     if (st != KVS_OK) return st;
     const int64_t items = (int64_t)pg.n_new * shape->n_q_heads;
-    float4 *ml = reinterpret_cast<float4 *>(workspace);
-    float *po = reinterpret_cast<float *>(ml + (plan.pieces > 1 ? items * plan.pieces : 0));
-    hipLaunchKernelGGL((attention_paged_kernel<DTYPE, D, PARTS>), dim3((unsigned)(units * plan.pieces * shape->n_kv_heads)), dim3(kThreads), lds, hs, pg, shape->n_q_heads,
-                       shape->n_kv_heads, (int)units, plan.pieces, plan.tiles, (const char *)c->k, (const char *)c->v, q, scale * 1.4426950408889634f, out, lse_out, po, ml);
+    const PagedParts parts = paged_parts(workspace, plan.pieces > 1 ? items * plan.pieces : 0);
+    hipLaunchKernelGGL((attention_paged_kernel<DTYPE, D, PARTS, false>), dim3((unsigned)(units * plan.pieces * shape->n_kv_heads)), dim3(kThreads), lds, hs, pg, shape->n_q_heads,
+                       shape->n_kv_heads, (int)units, plan.pieces, plan.tiles, (const int32_t *)nullptr, (const char *)c->k, (const char *)c->v, q, scale * 1.4426950408889634f, out, lse_out, parts.o, parts.ml);
     if ((st = check_launch("kvs_attention_paged")) != KVS_OK || plan.pieces <= 1) return st;
-    hipLaunchKernelGGL((merge_paged_kernel<DTYPE, D>), dim3((unsigned)items, D / 32), dim3(kThreads), 0, hs, pg, shape->n_q_heads, plan.pieces, po, ml, out, lse_out);
-    return check_launch("kvs_attention_paged(merge)");
+    return launch_merge_paged(shape, pg, plan.pieces, parts, out, lse_out, hs);
 }
 
 } // namespace
+
+kvs_status launch_merge_paged(const kvs_shape *shape, const Paged &pg, int pieces, const PagedParts &parts, void *out, float *lse_out, hipStream_t hs)
+{
+    const int64_t items = (int64_t)pg.n_new * shape->n_q_heads;
+#define KVS_MERGE(DT, DD) hipLaunchKernelGGL((merge_paged_kernel<DT, DD>), dim3((unsigned)items, DD / 32), dim3(kThreads), 0, hs, pg, shape->n_q_heads, pieces, parts.o, parts.ml, out, lse_out)
+    const bool wide = shape->head_dim == 128;
+    if (shape->dtype == KVS_F32) { if (wide) KVS_MERGE(KVS_F32, 128); else KVS_MERGE(KVS_F32, 64); }
+    else { if (wide) KVS_MERGE(KVS_BF16, 128); else KVS_MERGE(KVS_BF16, 64); }
+#undef KVS_MERGE
+    return check_launch("kvs_attention_paged(merge)");
+}
+
+kvs_status launch_again_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const Paged &pg, const PagedLargePlan &plan, const int32_t *odd, const void *q, float scale,
+                              void *out, float *lse_out, hipStream_t hs)
+{
+    static DeviceOnce once;
+    constexpr int D = 128, lds = kWaves * 2 * kKeys * D * 2;
+    const kvs_status st = once_per_device(once, [&]() -> kvs_status {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_paged_kernel<KVS_BF16, D, 1, true>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_attention_paged: %s", hipGetErrorString(e));
+    });
+    if (st != KVS_OK) return st;
+    hipLaunchKernelGGL((attention_paged_kernel<KVS_BF16, D, 1, true>), dim3((unsigned)(plan.units * (kPagedLargeRows / kRows) * shape->n_kv_heads)), dim3(kThreads), lds, hs, pg,
+                       shape->n_q_heads, shape->n_kv_heads, (int)plan.units, plan.pieces, plan.tiles, odd, (const char *)cache->k, (const char *)cache->v, q, scale * 1.4426950408889634f, out,
+                       lse_out, (float *)nullptr, (float4 *)nullptr);
+    return check_launch("kvs_attention_paged(again)");
+}
 
 size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new)
 {
@@ -577,7 +614,10 @@ size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, in
     // a launch that is cut has at most 4 kPlaces workgroups before and twice that after it, of 32 rows each
     const int64_t most = (int64_t)8 * kPlaces * kRows;
     const int64_t slots = items < most && items * pieces < most ? items * pieces : most > items ? most : 0;
-    return ((size_t)slots * slot_bytes(shape->head_dim) + 255) / 256 * 256 + 256;
+    size_t bytes = (size_t)slots * paged_slot_bytes(shape->head_dim);
+    const size_t large = attention_paged_large_workspace_bytes(shape, batch, n_new);
+    if (large > bytes) bytes = large;
+    return (bytes + 255) / 256 * 256 + 256;
 }
 
 kvs_status check_paged(const char *me, const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages, Paged *out)
@@ -645,6 +685,8 @@ extern "C" kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_page
     if (!aligned16(q_new) || !aligned16(out)) return fail(KVS_EINVAL, "%s: Q/out pointers must be 16-byte aligned", me);
     hipStream_t hs = (hipStream_t)stream;
     const int grp = shape->n_q_heads / shape->n_kv_heads;
+    PagedLargePlan large;
+    if (attention_paged_takes_large(shape, pg, scale, workspace_bytes, &large)) return launch_attention_paged_large(shape, cache, pg, large, q_new, scale, out, lse_out, workspace, hs);
     const int64_t units = most_blocks(pg, grp, kRows);
     const Plan plan = plan_pieces(shape, pg, units, workspace_bytes);
     if (units * plan.pieces * shape->n_kv_heads > kMostWgs || (int64_t)pg.n_new * shape->n_q_heads * (plan.pieces > 1 ? 4 : 0) > kMostWgs)
