@@ -31,6 +31,7 @@ constexpr int kRows = 32;              // rows of a block
 constexpr int kKeys = 32;              // keys of a tile
 constexpr float kSlack = 8.f;          // powers of two that a score may lie above its reference
 constexpr int kMaxPieces = kPagedMaxPieces;
+constexpr int kUncut = 0x7fffffff;     // tiles of the one piece of keys that are not cut
 constexpr int kPlaces = 512;           // workgroups that the chip holds at once
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4_t v) { return __builtin_bit_cast(bf16x8, v); }
@@ -52,7 +53,7 @@ __device__ __forceinline__ float max_of_halves(float x)      // of lanes i and i
 // PARTS: bf16 numbers that a weight enters the second product as: one, or two that hold 16 of its bits
 // AGAIN: the rows of row tiles of 256 whose kernel asks for it (`odd`, a word a workgroup of its), eight blocks each.
 template <int DTYPE, int D, int PARTS, bool AGAIN>
-__global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
+__global__ __launch_bounds__(kThreads, DTYPE == KVS_F32 && D == 128 ? 1 : 2) void attention_paged_kernel(
     const Paged pg, int n_q_heads, int n_kv_heads, int units, int pieces, int piece_tiles, const int32_t *__restrict__ odd,
     const char *__restrict__ k_pool, const char *__restrict__ v_pool, const void *__restrict__ q_new, float scale_log2,
     void *__restrict__ out, float *__restrict__ lse_out, float *__restrict__ part_o, float4 *__restrict__ part_ml)
@@ -83,28 +84,24 @@ __global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
     const int rest = (int)(blockIdx.x / (uint32_t)n_kv_heads);
     const int piece = AGAIN ? 0 : rest / units;
     const int grp = n_q_heads / n_kv_heads;
-    int b, blk;
+    Block found;
     if constexpr (AGAIN) {
-        constexpr int per = kPagedLargeRows / kRows;
-        const int unit = rest / per;
+        const int unit = rest;
         int any = 0;
         for (int p = 0; p < pieces; ++p) any |= odd[(p * units + unit) * n_kv_heads + g];
-        if (!any || !find_block<kPagedLargeRows>(pg, grp, units - 1 - unit, b, blk)) return;
-        blk = blk * per + rest % per;
-    } else if (!find_block<kRows>(pg, grp, rest - piece * units, b, blk)) {
-        return;
+        if (!any || !find_block<kPagedLargeRows>(pg, grp, units - 1 - unit, found)) return;
+        pieces = 1;
+        piece_tiles = kUncut;
+    } else {
+        if (!find_block<kRows>(pg, grp, rest - piece * units, found)) return;
     }
-    b = __builtin_amdgcn_readfirstlane(b);
-    blk = __builtin_amdgcn_readfirstlane(blk);
-    int tok0, n_tok;
-    tokens_of(pg, b, tok0, n_tok);
-    const int len = len_of(pg, b);
+    const int b = __builtin_amdgcn_readfirstlane(found.b), blk = __builtin_amdgcn_readfirstlane(found.blk), tok0 = __builtin_amdgcn_readfirstlane(found.tok0);
+    const int n_tok = __builtin_amdgcn_readfirstlane(found.n_tok), len = __builtin_amdgcn_readfirstlane(found.len);
     const int rows = n_tok * grp;
-    // (row tiles of 256 end with their request's rows)
-    const int row0 = blk * kRows - (AGAIN ? (rows + kPagedLargeRows - 1) / kPagedLargeRows * kPagedLargeRows - rows : 0);
-    if (AGAIN && row0 + kRows <= 0) return;
-    if (AGAIN) { pieces = 1; piece_tiles = 0x7fffffff; }
 
+    // Without a window the tiles that the workgroup may have do not depend on the length, and their places are asked for beside it.
+    const int early = !AGAIN && !pg.window ? granule_of(pg, b, 2 * (piece * (piece_tiles == kUncut ? 0 : piece_tiles) + wave + kWaves * (lane >> 1)) + (lane & 1)) : -1;
+    auto block_from = [&](const int row0) __attribute__((always_inline)) {
     // ---- this lane's row (both half-waves hold the same 32) ------------------------------------------------
     const int rq = min(max(row0 + ln, 0), rows - 1);
     const int t_own = rq / grp, hh = rq - t_own * grp;
@@ -142,7 +139,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
         const int i = i0 + (lane >> 1);
         place = i < mine ? granule_of(pg, b, 2 * tile_of(i) + (lane & 1)) : -1;
     };
-    look_up(0);
+    if (AGAIN || window) look_up(0);
+    else place = (lane >> 1) < mine ? early : -1;
 
     // ---- Q as the B operand; a negative scale's sign goes into it, so that the largest score is the largest product's ----
     const bool negative = scale_log2 < 0.f;
@@ -451,6 +449,18 @@ __global__ __launch_bounds__(kThreads, 2) void attention_paged_kernel(
         if (lse_out && part == 0) lse_out[at] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
         return;
     }
+    };
+    // (row tiles of 256 end with their request's rows)
+    if constexpr (AGAIN) {
+        const int first = blk * kPagedLargeRows - ((rows + kPagedLargeRows - 1) / kPagedLargeRows * kPagedLargeRows - rows);
+        for (int r = 0; r < kPagedLargeRows; r += kRows) {
+            if (first + r + kRows <= 0) continue;
+            block_from(first + r);
+            __syncthreads();
+        }
+    } else {
+        block_from(blk * kRows);
+    }
 }
 
 // out = sum_p w_p O_p / sum_p w_p l_p with w_p = 2^(m_p - max m).  A workgroup takes 32 channels of one row: its threads make the
@@ -539,20 +549,26 @@ int64_t most_tiles(const Paged &pg, int grp)
     return (keys + kKeys - 1) / kKeys + 1;
 }
 
-// How keys are cut: `pieces` pieces of `tiles` tiles.  The contexts' lengths are on the device; the host knows how long one can be.
+// How keys are cut: `pieces` pieces of `tiles` tiles, a multiple of the waves.  The contexts' lengths are on the device; the host knows how
+// long one can be.
 struct Plan { int32_t pieces, tiles; };
 
+// As many workgroups as the chip holds at once where each has little to do, a few times as many where the longest would keep the
+// others waiting.  (One workgroup a place, two, four, us: one row of 131072 keys of 4 heads 59, 63, 66; 8 contexts of 2000 to 8000 of 8 heads
+// 38.9, 38.3, 41.7; 4 of 10000 to 40000 of 4 57.8, 59.5, 65.0; 64 of 100 to 400 18.4, 33.7, 33.5; but 30 of 1000 to 4000 74.1, 73.0, 71.9,
+// 64 of 4096 to 16384 526, 511, 490.)  Pieces of one tile a wave: 77 fp32 rows of 512 keys 15.7, of two 16.1, of four 21.
 Plan plan_pieces(const kvs_shape *shape, const Paged &pg, int64_t units, size_t workspace_bytes)
 {
     const int64_t wgs = units * shape->n_kv_heads, most = most_tiles(pg, shape->n_q_heads / shape->n_kv_heads);
     const int64_t slots = (int64_t)(workspace_bytes / paged_slot_bytes(shape->head_dim)) / ((int64_t)pg.n_new * shape->n_q_heads);
-    int64_t pieces = (4 * kPlaces + wgs - 1) / wgs;
+    const int64_t load = wgs * most / kPlaces;               // tiles for each place on the chip
+    const int64_t target = load < 48 ? kPlaces : load < 200 ? 2 * kPlaces : 4 * kPlaces;
+    int64_t pieces = (target + wgs - 1) / wgs;
     if (pieces > slots) pieces = slots;
     if (pieces > kMaxPieces) pieces = kMaxPieces;
-    if (wgs >= 4 * kPlaces || pieces <= 1 || most <= 2 * kWaves) return {1, 0x7fffffff};
+    if (wgs >= target || pieces <= 1 || most <= kWaves) return {1, kUncut};
     int64_t tiles = (most + pieces - 1) / pieces;
     tiles = (tiles + kWaves - 1) / kWaves * kWaves;
-    if (tiles < 2 * kWaves) tiles = 2 * kWaves;
     return {(int32_t)((most + tiles - 1) / tiles), (int32_t)tiles};
 }
 
@@ -599,7 +615,7 @@ kvs_status launch_again_paged(const kvs_shape *shape, const kvs_paged_cache *cac
         return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_attention_paged: %s", hipGetErrorString(e));
     });
     if (st != KVS_OK) return st;
-    hipLaunchKernelGGL((attention_paged_kernel<KVS_BF16, D, 1, true>), dim3((unsigned)(plan.units * (kPagedLargeRows / kRows) * shape->n_kv_heads)), dim3(kThreads), lds, hs, pg,
+    hipLaunchKernelGGL((attention_paged_kernel<KVS_BF16, D, 1, true>), dim3((unsigned)(plan.units * shape->n_kv_heads)), dim3(kThreads), lds, hs, pg,
                        shape->n_q_heads, shape->n_kv_heads, (int)plan.units, plan.pieces, plan.tiles, odd, (const char *)cache->k, (const char *)cache->v, q, scale * 1.4426950408889634f, out,
                        lse_out, (float *)nullptr, (float4 *)nullptr);
     return check_launch("kvs_attention_paged(again)");
@@ -609,7 +625,7 @@ size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, in
 {
     if (check_shape(shape) != KVS_OK || n_new <= 0 || max_ctx <= 0) return 256;
     const int64_t items = n_new * shape->n_q_heads;
-    int64_t pieces = max_ctx / (2 * kWaves * kKeys) + 2;
+    int64_t pieces = max_ctx / (kWaves * kKeys) + 2;
     if (pieces > kMaxPieces) pieces = kMaxPieces;
     // a launch that is cut has at most 4 kPlaces workgroups before and twice that after it, of 32 rows each
     const int64_t most = (int64_t)8 * kPlaces * kRows;

@@ -52,21 +52,26 @@ __device__ __forceinline__ int granule_of(const Paged &pg, int b, int gi)
 }
 
 // A call's rows (tokens times the query heads that share a KV head) in blocks of R rows, none of which holds two requests: which request
-// block u belongs to and which of its blocks it is.  All lanes of a wave ask for the same block; 64 requests a step.
+// block u belongs to, which of its blocks it is, the request's tokens [tok0, tok0 + n_tok) and context length.  All lanes of a wave ask
+// for the same block; 64 requests a step, whose offsets and lengths come in one trip to memory.
+struct Block { int b, blk, tok0, n_tok, len; };
 template <int R>
-__device__ __forceinline__ bool find_block(const Paged &pg, int grp, int u, int &b, int &blk)
+__device__ __forceinline__ bool find_block(const Paged &pg, int grp, int u, Block &out)
 {
     if (!pg.cu_new) {
-        const int per = (grp + R - 1) / R;
-        b = u / per;
-        blk = u - b * per;
-        return b < pg.batch;
+        const int per = (grp + R - 1) / R, b = u / per;
+        if (b >= pg.batch) return false;
+        out = {b, u - b * per, b, 1, len_of(pg, b)};
+        return true;
     }
     const int lane = threadIdx.x & 63;
     int base = 0;
     for (int b0 = 0; b0 < pg.batch; b0 += 64) {
-        int lo, n = 0;
-        if (b0 + lane < pg.batch) tokens_of(pg, b0 + lane, lo, n);
+        int lo = 0, n = 0, len = 0;
+        if (b0 + lane < pg.batch) {
+            len = len_of(pg, b0 + lane);
+            tokens_of(pg, b0 + lane, lo, n);
+        }
         const int mine = (n * grp + R - 1) / R;
         int upto = mine;
 #pragma unroll
@@ -77,8 +82,7 @@ __device__ __forceinline__ bool find_block(const Paged &pg, int grp, int u, int 
         const unsigned long long past = __ballot(base + upto > u);
         if (past) {
             const int at = __ffsll((long long)past) - 1;
-            b = b0 + at;
-            blk = u - base - __builtin_amdgcn_readlane(upto - mine, at);
+            out = {b0 + at, u - base - __builtin_amdgcn_readlane(upto - mine, at), __builtin_amdgcn_readlane(lo, at), __builtin_amdgcn_readlane(n, at), __builtin_amdgcn_readlane(len, at)};
             return true;
         }
         base += __builtin_amdgcn_readlane(upto, 63);
