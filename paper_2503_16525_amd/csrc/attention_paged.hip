@@ -31,7 +31,6 @@ constexpr int kRows = 32;              // rows of a block
 constexpr int kKeys = 32;              // keys of a tile
 constexpr float kSlack = 8.f;          // powers of two that a score may lie above its reference
 constexpr int kMaxPieces = kPagedMaxPieces;
-constexpr int kUncut = 0x7fffffff;     // tiles of the one piece of keys that are not cut
 constexpr int kPlaces = 512;           // workgroups that the chip holds at once
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4_t v) { return __builtin_bit_cast(bf16x8, v); }
@@ -54,7 +53,7 @@ __device__ __forceinline__ float max_of_halves(float x)      // of lanes i and i
 // AGAIN: the rows of row tiles of 256 whose kernel asks for it (`odd`, a word a workgroup of its), eight blocks each.
 template <int DTYPE, int D, int PARTS, bool AGAIN>
 __global__ __launch_bounds__(kThreads, DTYPE == KVS_F32 && D == 128 ? 1 : 2) void attention_paged_kernel(
-    const Paged pg, int n_q_heads, int n_kv_heads, int units, int pieces, int piece_tiles, const int32_t *__restrict__ odd,
+    const Paged pg, int n_q_heads, int n_kv_heads, int units, int pieces, int least_tiles, const int32_t *__restrict__ odd,
     const char *__restrict__ k_pool, const char *__restrict__ v_pool, const void *__restrict__ q_new, float scale_log2,
     void *__restrict__ out, float *__restrict__ lse_out, float *__restrict__ part_o, float4 *__restrict__ part_ml)
 {
@@ -78,29 +77,25 @@ __global__ __launch_bounds__(kThreads, DTYPE == KVS_F32 && D == 128 ? 1 : 2) voi
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hf = lane >> 5, ln = lane & 31;
 
-    // Workgroup = (piece, block, KV head), KV heads side by side: their rows of the cache are neighbours.  A piece's blocks come
-    // together, which share its keys in L2.
-    const int g = (int)(blockIdx.x % (uint32_t)n_kv_heads);
-    const int rest = (int)(blockIdx.x / (uint32_t)n_kv_heads);
-    const int piece = AGAIN ? 0 : rest / units;
+    const PagedPlace at = place_of(blockIdx.x, units, AGAIN ? 1 : pieces, n_kv_heads);
+    const int g = __builtin_amdgcn_readfirstlane(at.g), piece = __builtin_amdgcn_readfirstlane(at.piece), unit = __builtin_amdgcn_readfirstlane(at.unit);
     const int grp = n_q_heads / n_kv_heads;
     Block found;
     if constexpr (AGAIN) {
-        const int unit = rest;
         int any = 0;
         for (int p = 0; p < pieces; ++p) any |= odd[(p * units + unit) * n_kv_heads + g];
         if (!any || !find_block<kPagedLargeRows>(pg, grp, units - 1 - unit, found)) return;
         pieces = 1;
-        piece_tiles = kUncut;
     } else {
-        if (!find_block<kRows>(pg, grp, rest - piece * units, found)) return;
+        if (!find_block<kRows>(pg, grp, unit, found)) return;
     }
     const int b = __builtin_amdgcn_readfirstlane(found.b), blk = __builtin_amdgcn_readfirstlane(found.blk), tok0 = __builtin_amdgcn_readfirstlane(found.tok0);
     const int n_tok = __builtin_amdgcn_readfirstlane(found.n_tok), len = __builtin_amdgcn_readfirstlane(found.len);
     const int rows = n_tok * grp;
 
-    // Without a window the tiles that the workgroup may have do not depend on the length, and their places are asked for beside it.
-    const int early = !AGAIN && !pg.window ? granule_of(pg, b, 2 * (piece * (piece_tiles == kUncut ? 0 : piece_tiles) + wave + kWaves * (lane >> 1)) + (lane & 1)) : -1;
+    // Without a window the first piece's tiles do not depend on the length, and their places are asked for beside it.
+    const bool known = !AGAIN && !pg.window && piece == 0;
+    const int early = known ? granule_of(pg, b, 2 * (wave + kWaves * (lane >> 1)) + (lane & 1)) : -1;
     auto block_from = [&](const int row0) __attribute__((always_inline)) {
     // ---- this lane's row (both half-waves hold the same 32) ------------------------------------------------
     const int rq = min(max(row0 + ln, 0), rows - 1);
@@ -123,6 +118,8 @@ __global__ __launch_bounds__(kThreads, DTYPE == KVS_F32 && D == 128 ? 1 : 2) voi
     const int low = window && pmax >= 0 ? max(plow - window + 1, 0) / kKeys : 0;
     const int head = min(low, (int)(((int64_t)n_first + kKeys - 1) / kKeys));
     const int total = pmax < 0 ? 0 : head + pmax / kKeys + 1 - low;
+    // equal pieces of what there is, none below least_tiles
+    const int piece_tiles = max(((total + pieces - 1) / pieces + kWaves - 1) / kWaves * kWaves, least_tiles);
     const int t_lo = (int)min((int64_t)piece * piece_tiles, (int64_t)total), t_hi = (int)min((int64_t)t_lo + piece_tiles, (int64_t)total);
     const int mine = max(0, (t_hi - t_lo - wave + kWaves - 1) / kWaves);
     auto tile_of = [&](int i) { const int t = t_lo + wave + kWaves * i; return t < head ? t : t - head + low; };
@@ -139,7 +136,7 @@ __global__ __launch_bounds__(kThreads, DTYPE == KVS_F32 && D == 128 ? 1 : 2) voi
         const int i = i0 + (lane >> 1);
         place = i < mine ? granule_of(pg, b, 2 * tile_of(i) + (lane & 1)) : -1;
     };
-    if (AGAIN || window) look_up(0);
+    if (!known) look_up(0);
     else place = (lane >> 1) < mine ? early : -1;
 
     // ---- Q as the B operand; a negative scale's sign goes into it, so that the largest score is the largest product's ----
@@ -538,6 +535,53 @@ __global__ __launch_bounds__(kThreads) void merge_paged_kernel(const Paged pg, i
     if (lse_out && c == 0) lse_out[item] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
+// The same with D / 4 threads a row, four channels a thread, and MOST pieces asked for at once.  (By the kernel above, 12800 rows of two
+// pieces took 60 us: a workgroup for 32 channels of a row each.)
+template <int DTYPE, int D, int MOST>
+__global__ __launch_bounds__(kThreads) void merge_paged_rows_kernel(const Paged pg, int64_t n_items, int n_q_heads, int pieces, const float *__restrict__ part_o,
+                                                                    const float4 *__restrict__ part_ml, void *__restrict__ out, float *__restrict__ lse_out)
+{
+    constexpr int kLanes = D / 4;
+    const int c = threadIdx.x % kLanes;
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
+    if (item >= n_items) return;
+    if (pg.cu_new) {                                         // tokens of no request stay as they are
+        const int token = (int)(item / n_q_heads);
+        if (token < pg.cu_new[0] || token >= pg.cu_new[pg.batch]) return;
+    }
+    const int64_t slot = item * pieces;
+    const float4 *from = reinterpret_cast<const float4 *>(part_o + slot * D) + c;
+    float top = kLowest, l = 0.f, lr = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 < pieces; p0 += MOST) {
+        float4 x[MOST], y[MOST];
+        float to = top;
+#pragma unroll
+        for (int p = 0; p < MOST; ++p) {
+            x[p] = p0 + p < pieces ? part_ml[slot + p0 + p] : make_float4(kLowest, 0.f, 0.f, 0.f);
+            y[p] = p0 + p < pieces ? from[(int64_t)(p0 + p) * kLanes] : make_float4(0.f, 0.f, 0.f, 0.f);
+            to = fmaxf(to, x[p].x);
+        }
+        const float down = __builtin_amdgcn_exp2f(top - to);
+        top = to;
+        l *= down; lr *= down;
+        o.x *= down; o.y *= down; o.z *= down; o.w *= down;
+#pragma unroll
+        for (int p = 0; p < MOST; ++p) {
+            const float f = __builtin_amdgcn_exp2f(x[p].x - top);
+            l += x[p].y * f;
+            lr += x[p].z * f;
+            if (x[p].y != 0.f) { o.x += f * y[p].x; o.y += f * y[p].y; o.z += f * y[p].z; o.w += f * y[p].w; }   // (a piece without keys has left no sums)
+        }
+    }
+    const float inv = 1.f / lr;
+    if (l != 0.f) { o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv; }
+    else o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (DTYPE == KVS_BF16) *reinterpret_cast<uint2 *>((uint16_t *)out + item * D + 4 * c) = make_uint2(pack2(o.x, o.y), pack2(o.z, o.w));
+    else *reinterpret_cast<float4 *>((float *)out + item * D + 4 * c) = o;
+    if (lse_out && c == 0) lse_out[item] = l != 0.f ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+}
+
 // Tiles that a block of rows may need at most.
 int64_t most_tiles(const Paged &pg, int grp)
 {
@@ -549,27 +593,39 @@ int64_t most_tiles(const Paged &pg, int grp)
     return (keys + kKeys - 1) / kKeys + 1;
 }
 
-// How keys are cut: `pieces` pieces of `tiles` tiles, a multiple of the waves.  The contexts' lengths are on the device; the host knows how
-// long one can be.
-struct Plan { int32_t pieces, tiles; };
+// How many pieces the keys are cut into, and about how long that takes.  The contexts' lengths are on the device, where every block of rows
+// takes equal pieces of what it sees; the host knows how long a context can be.
+struct Plan { int32_t pieces; double us; };
+constexpr int kLeastTiles = kWaves;    // of a piece: one for each wave
+constexpr int64_t kMostCutWgs = 4 * kPlaces;
 
-// As many workgroups as the chip holds at once where each has little to do, a few times as many where the longest would keep the
-// others waiting.  (One workgroup a place, two, four, us: one row of 131072 keys of 4 heads 59, 63, 66; 8 contexts of 2000 to 8000 of 8 heads
-// 38.9, 38.3, 41.7; 4 of 10000 to 40000 of 4 57.8, 59.5, 65.0; 64 of 100 to 400 18.4, 33.7, 33.5; but 30 of 1000 to 4000 74.1, 73.0, 71.9,
-// 64 of 4096 to 16384 526, 511, 490.)  Pieces of one tile a wave: 77 fp32 rows of 512 keys 15.7, of two 16.1, of four 21.
-Plan plan_pieces(const kvs_shape *shape, const Paged &pg, int64_t units, size_t workspace_bytes)
+// In microseconds, as measured: a step of four tiles, one a wave, takes 1.0, 1.5 beside a second workgroup on the compute unit, and the rounds of
+// more follow at 0.78 a workgroup and unit; the cache comes at 5.1 TB/s; where it bounds the call or there are rounds, contexts of a batch that are
+// longer than others hold the end up by a third of a piece, and the average one is shorter than the longest; 6 for the launch and a workgroup's
+// beginning and end, 4 for a merge's.  (Estimate and measured: 16 rows of 4096 keys of 8 heads in one piece 39, 37; 64 in eight 19, 22; 200 tokens of
+// 32 heads over 4096 keys 38, 39; 700 over 16384 281, 293; one row of 8192 keys of 4 heads in 64 pieces 12, 12; 64 contexts of 4096 to 16384 in
+// four pieces 7 % less than in one.)
+Plan plan_pieces(const kvs_shape *shape, const Paged &pg, const PagedCall &call, size_t workspace_bytes)
 {
-    const int64_t wgs = units * shape->n_kv_heads, most = most_tiles(pg, shape->n_q_heads / shape->n_kv_heads);
-    const int64_t slots = (int64_t)(workspace_bytes / paged_slot_bytes(shape->head_dim)) / ((int64_t)pg.n_new * shape->n_q_heads);
-    const int64_t load = wgs * most / kPlaces;               // tiles for each place on the chip
-    const int64_t target = load < 48 ? kPlaces : load < 200 ? 2 * kPlaces : 4 * kPlaces;
-    int64_t pieces = (target + wgs - 1) / wgs;
-    if (pieces > slots) pieces = slots;
-    if (pieces > kMaxPieces) pieces = kMaxPieces;
-    if (wgs >= target || pieces <= 1 || most <= kWaves) return {1, kUncut};
-    int64_t tiles = (most + pieces - 1) / pieces;
-    tiles = (tiles + kWaves - 1) / kWaves * kWaves;
-    return {(int32_t)((most + tiles - 1) / tiles), (int32_t)tiles};
+    const int64_t wgs = (int64_t)pg.batch * call.row_blocks * shape->n_kv_heads, most = most_tiles(pg, call.grp);
+    const int64_t slots = (int64_t)(workspace_bytes / paged_slot_bytes(shape->head_dim)) / call.items;
+    const double several = pg.batch > 1 ? 1.0 : 0.0;
+    const double tile_bytes = 2.0 * kKeys * shape->head_dim * (shape->dtype == KVS_F32 ? 4 : 2);
+    const double step = shape->dtype == KVS_F32 ? 2.5 : 1.0;              // (fp32's matrix instructions)
+    const double reading = (double)pg.batch * shape->n_kv_heads * (double)most * tile_bytes * (1.0 - 0.25 * several) / 5.1e6;
+    const int64_t even = shape->n_kv_heads % 8 == 0 ? 1 : shape->n_kv_heads % 4 == 0 ? 2 : shape->n_kv_heads % 2 == 0 ? 4 : 8;
+    Plan best = {1, 1e30};
+    for (int64_t p = 1; p <= kMaxPieces; p += (p + 3) / 4) {
+        int64_t n = p >= even ? (p + even - 1) / even * even : p;        // (see place_of)
+        if (n > 1 && (n > slots || n > kMaxPieces || wgs * n > kMostCutWgs || (n - 1) * kLeastTiles >= most)) break;
+        const double steps = (double)((most + kWaves * n - 1) / (kWaves * n)), a_unit = (double)(wgs * n) / 256.0;
+        double computing = step * steps * (a_unit <= 0.9 ? 1.0 : a_unit <= 2.0 ? 1.5 : 0.78 * a_unit);
+        const bool waits = a_unit > 2.0 || reading > computing;
+        if (a_unit > 2.0) computing *= 1.0 - 0.15 * several;
+        const double us = (computing > reading ? computing : reading) + (waits ? 0.35 * several * steps : 0.0) + 6.0 + (n > 1 ? 4.0 + call.merge_us * (double)n : 0.0);
+        if (us < best.us) best = {(int32_t)n, us};
+    }
+    return best;
 }
 
 template <int DTYPE, int D, int PARTS>
@@ -587,7 +643,7 @@ kvs_status launch(const kvs_shape *shape, const kvs_paged_cache *c, const Paged 
     const int64_t items = (int64_t)pg.n_new * shape->n_q_heads;
     const PagedParts parts = paged_parts(workspace, plan.pieces > 1 ? items * plan.pieces : 0);
     hipLaunchKernelGGL((attention_paged_kernel<DTYPE, D, PARTS, false>), dim3((unsigned)(units * plan.pieces * shape->n_kv_heads)), dim3(kThreads), lds, hs, pg, shape->n_q_heads,
-                       shape->n_kv_heads, (int)units, plan.pieces, plan.tiles, (const int32_t *)nullptr, (const char *)c->k, (const char *)c->v, q, scale * 1.4426950408889634f, out, lse_out, parts.o, parts.ml);
+                       shape->n_kv_heads, (int)units, plan.pieces, kLeastTiles, (const int32_t *)nullptr, (const char *)c->k, (const char *)c->v, q, scale * 1.4426950408889634f, out, lse_out, parts.o, parts.ml);
     if ((st = check_launch("kvs_attention_paged")) != KVS_OK || plan.pieces <= 1) return st;
     return launch_merge_paged(shape, pg, plan.pieces, parts, out, lse_out, hs);
 }
@@ -597,11 +653,21 @@ kvs_status launch(const kvs_shape *shape, const kvs_paged_cache *c, const Paged 
 kvs_status launch_merge_paged(const kvs_shape *shape, const Paged &pg, int pieces, const PagedParts &parts, void *out, float *lse_out, hipStream_t hs)
 {
     const int64_t items = (int64_t)pg.n_new * shape->n_q_heads;
-#define KVS_MERGE(DT, DD) hipLaunchKernelGGL((merge_paged_kernel<DT, DD>), dim3((unsigned)items, DD / 32), dim3(kThreads), 0, hs, pg, shape->n_q_heads, pieces, parts.o, parts.ml, out, lse_out)
+#define KVS_MERGE_ROWS(DT, DD, M)                                                                                                                              \
+    hipLaunchKernelGGL((merge_paged_rows_kernel<DT, DD, M>), dim3((unsigned)((items + 4 * kThreads / DD - 1) / (4 * kThreads / DD))), dim3(kThreads), 0, hs, pg, items, \
+                       shape->n_q_heads, pieces, parts.o, parts.ml, out, lse_out)
+#define KVS_MERGE(DT, DD)                                                                                                                                      \
+    do {                                                                                                                                                       \
+        if (pieces <= 4) KVS_MERGE_ROWS(DT, DD, 4);                                                                                                            \
+        else if (pieces <= 16 || items >= 1024) KVS_MERGE_ROWS(DT, DD, 16);                                                                                     \
+        else hipLaunchKernelGGL((merge_paged_kernel<DT, DD>), dim3((unsigned)items, DD / 32), dim3(kThreads), 0, hs, pg, shape->n_q_heads, pieces, parts.o,    \
+                                parts.ml, out, lse_out);                                                                                                       \
+    } while (0)
     const bool wide = shape->head_dim == 128;
     if (shape->dtype == KVS_F32) { if (wide) KVS_MERGE(KVS_F32, 128); else KVS_MERGE(KVS_F32, 64); }
     else { if (wide) KVS_MERGE(KVS_BF16, 128); else KVS_MERGE(KVS_BF16, 64); }
 #undef KVS_MERGE
+#undef KVS_MERGE_ROWS
     return check_launch("kvs_attention_paged(merge)");
 }
 
@@ -616,7 +682,7 @@ kvs_status launch_again_paged(const kvs_shape *shape, const kvs_paged_cache *cac
     });
     if (st != KVS_OK) return st;
     hipLaunchKernelGGL((attention_paged_kernel<KVS_BF16, D, 1, true>), dim3((unsigned)(plan.units * shape->n_kv_heads)), dim3(kThreads), lds, hs, pg,
-                       shape->n_q_heads, shape->n_kv_heads, (int)plan.units, plan.pieces, plan.tiles, odd, (const char *)cache->k, (const char *)cache->v, q, scale * 1.4426950408889634f, out,
+                       shape->n_q_heads, shape->n_kv_heads, (int)plan.units, plan.pieces, kLeastTiles, odd, (const char *)cache->k, (const char *)cache->v, q, scale * 1.4426950408889634f, out,
                        lse_out, (float *)nullptr, (float4 *)nullptr);
     return check_launch("kvs_attention_paged(again)");
 }
@@ -627,9 +693,8 @@ size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, in
     const int64_t items = n_new * shape->n_q_heads;
     int64_t pieces = max_ctx / (kWaves * kKeys) + 2;
     if (pieces > kMaxPieces) pieces = kMaxPieces;
-    // a launch that is cut has at most 4 kPlaces workgroups before and twice that after it, of 32 rows each
-    const int64_t most = (int64_t)8 * kPlaces * kRows;
-    const int64_t slots = items < most && items * pieces < most ? items * pieces : most > items ? most : 0;
+    const int64_t most = kMostCutWgs * kRows;                // rows of a cut launch's workgroups
+    const int64_t slots = items < most && items * pieces < most ? items * pieces : most;
     size_t bytes = (size_t)slots * paged_slot_bytes(shape->head_dim);
     const size_t large = attention_paged_large_workspace_bytes(shape, batch, n_new);
     if (large > bytes) bytes = large;
@@ -701,10 +766,12 @@ extern "C" kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_page
     if (!aligned16(q_new) || !aligned16(out)) return fail(KVS_EINVAL, "%s: Q/out pointers must be 16-byte aligned", me);
     hipStream_t hs = (hipStream_t)stream;
     const int grp = shape->n_q_heads / shape->n_kv_heads;
+    const PagedCall call = describe(shape, pg);
+    const Plan plan = plan_pieces(shape, pg, call, workspace_bytes);
     PagedLargePlan large;
-    if (attention_paged_takes_large(shape, pg, scale, workspace_bytes, &large)) return launch_attention_paged_large(shape, cache, pg, large, q_new, scale, out, lse_out, workspace, hs);
+    if (attention_paged_takes_large(shape, pg, call, scale, workspace_bytes, &large) && large.us < plan.us)
+        return launch_attention_paged_large(shape, cache, pg, large, q_new, scale, out, lse_out, workspace, hs);
     const int64_t units = most_blocks(pg, grp, kRows);
-    const Plan plan = plan_pieces(shape, pg, units, workspace_bytes);
     if (units * plan.pieces * shape->n_kv_heads > kMostWgs || (int64_t)pg.n_new * shape->n_q_heads * (plan.pieces > 1 ? 4 : 0) > kMostWgs)
         return fail(KVS_EINVAL, "%s: too many rows in one call", me);
     const bool wide = shape->head_dim == 128, few = (int64_t)pg.n_new * grp <= (int64_t)kRows * pg.batch;
