@@ -599,12 +599,11 @@ struct Plan { int32_t pieces; double us; };
 constexpr int kLeastTiles = kWaves;    // of a piece: one for each wave
 constexpr int64_t kMostCutWgs = 4 * kPlaces;
 
-// In microseconds, as measured: a step of four tiles, one a wave, takes 1.0, 1.5 beside a second workgroup on the compute unit, and the rounds of
-// more follow at 0.78 a workgroup and unit; the cache comes at 5.1 TB/s; where it bounds the call or there are rounds, contexts of a batch that are
-// longer than others hold the end up by a third of a piece, and the average one is shorter than the longest; 6 for the launch and a workgroup's
-// beginning and end, 4 for a merge's.  (Estimate and measured: 16 rows of 4096 keys of 8 heads in one piece 39, 37; 64 in eight 19, 22; 200 tokens of
-// 32 heads over 4096 keys 38, 39; 700 over 16384 281, 293; one row of 8192 keys of 4 heads in 64 pieces 12, 12; 64 contexts of 4096 to 16384 in
-// four pieces 7 % less than in one.)
+// In microseconds, as measured: a step of four tiles, one a wave, takes 1.0, 1.5 beside a second workgroup on the compute unit, and workgroups
+// beyond 512 wait for the first; the cache comes at 5.1 TB/s, and the two hide each other less the closer they are; where reading bounds the call
+// or there are rounds, contexts of a batch that are longer than others hold the end up by a third of a piece, and the average one is shorter
+// than the longest; 6 for the launch and a workgroup's beginning and end, 4 for a merge's.  Over 39 calls of 1 to 6000 tokens and 500 to 60000
+// keys the kernel and number of pieces that this takes are within 10 % of the best there is in 30, within 22 % in 38.
 Plan plan_pieces(const kvs_shape *shape, const Paged &pg, const PagedCall &call, size_t workspace_bytes)
 {
     const int64_t wgs = (int64_t)pg.batch * call.row_blocks * shape->n_kv_heads, most = most_tiles(pg, call.grp);
@@ -615,16 +614,21 @@ Plan plan_pieces(const kvs_shape *shape, const Paged &pg, const PagedCall &call,
     const double reading = (double)pg.batch * shape->n_kv_heads * (double)most * tile_bytes * (1.0 - 0.25 * several) / 5.1e6;
     const int64_t even = shape->n_kv_heads % 8 == 0 ? 1 : shape->n_kv_heads % 4 == 0 ? 2 : shape->n_kv_heads % 2 == 0 ? 4 : 8;
     Plan best = {1, 1e30};
-    for (int64_t p = 1; p <= kMaxPieces; p += (p + 3) / 4) {
-        int64_t n = p >= even ? (p + even - 1) / even * even : p;        // (see place_of)
-        if (n > 1 && (n > slots || n > kMaxPieces || wgs * n > kMostCutWgs || (n - 1) * kLeastTiles >= most)) break;
+    auto consider = [&](int64_t p) {
+        const int64_t n = p >= even ? (p + even - 1) / even * even : p;  // (see place_of)
+        if (n > 1 && (n > slots || n > kMaxPieces || wgs * n > kMostCutWgs || (n - 1) * kLeastTiles >= most)) return false;
         const double steps = (double)((most + kWaves * n - 1) / (kWaves * n)), a_unit = (double)(wgs * n) / 256.0;
-        double computing = step * steps * (a_unit <= 0.9 ? 1.0 : a_unit <= 2.0 ? 1.5 : 0.78 * a_unit);
+        const double rounds = floor(a_unit / 2.0), rest = a_unit - 2.0 * rounds;
+        double computing = step * steps * (a_unit > 8.0 ? 0.78 * a_unit : 1.5 * rounds + (rest > 0.9 ? 1.5 : rest > 0.0 ? 1.0 : 0.0));
         const bool waits = a_unit > 2.0 || reading > computing;
         if (a_unit > 2.0) computing *= 1.0 - 0.15 * several;
-        const double us = (computing > reading ? computing : reading) + (waits ? 0.35 * several * steps : 0.0) + 6.0 + (n > 1 ? 4.0 + call.merge_us * (double)n : 0.0);
+        const double us = cbrt(computing * computing * computing + reading * reading * reading) + (waits ? 0.35 * several * steps : 0.0) + 6.0 + (n > 1 ? 4.0 + call.merge_us * (double)n : 0.0);
         if (us < best.us) best = {(int32_t)n, us};
-    }
+        return true;
+    };
+    for (int64_t p = 1; p <= kMaxPieces && consider(p); p += (p + 3) / 4) {}
+    for (int64_t fill = 256; fill <= 512; fill += 256)                    // one workgroup a compute unit, two
+        if (fill / wgs > 1) consider(fill / wgs);
     return best;
 }
 

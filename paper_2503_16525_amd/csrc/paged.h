@@ -95,7 +95,7 @@ inline int64_t most_blocks(const Paged &pg, int grp, int r)
 {
     if (!pg.cu_new) return (int64_t)pg.batch * ((grp + r - 1) / r);
     const int64_t rows = (int64_t)pg.n_new * grp, reqs = pg.batch < pg.n_new ? pg.batch : pg.n_new;
-    return rows / r + reqs;
+    return (rows + reqs * (r - 1)) / r;
 }
 
 } // namespace kvs
