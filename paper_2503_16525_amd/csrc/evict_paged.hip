@@ -3,9 +3,9 @@
 // Every row has a 32-bit key, its mass added up over the KV heads, order-preserving; protected rows have the largest.  The m-th largest key
 // is found by its digits, 11, 11 and 10 bits from the top: a count of the digit's values in LDS tells which one the key has.  Rows
 // above it stay, and so many of those that equal it, from the lowest index on.
-//   Up to kSmall rows a workgroup a request holds all keys in registers.  Longer contexts take two launches for it: segments make
-//   their keys and count their first digits, then a workgroup a request adds these up, reads the keys once, sets those of the
-//   one value aside in LDS and goes on with them; a third launch counts what stays of every 256 rows.
+//   Up to kSmall rows a workgroup a request holds all keys in registers.  Longer contexts take three launches for it: segments make
+//   their keys and count their first digits; parts add these up, set their keys of the one value aside and count the second
+//   digits; a workgroup a request finds the rest among those; a fourth counts what stays of every 256 rows.
 //   The last launch moves: a workgroup for every 256 rows ranks its own behind those before it and copies them.
 // What bounds it: the copy, at most; the keys' passes are a few dependent trips to memory each.
 #include "paged.h"
@@ -20,7 +20,7 @@ constexpr int kKeysPerThread = 8;
 constexpr int kSmall = kSelThreads * kKeysPerThread;
 constexpr int kSeg = 2048;                  // rows whose first digits are counted together
 constexpr int kBins = 2048;                 // values of a digit
-constexpr int kAside = 2304;                // keys that LDS holds besides, for each wave
+constexpr int kPart = 8192;                 // keys that a workgroup looks through
 
 struct Picked { uint32_t key; int32_t want, m, len; };      // the m-th largest key, how many that equal it stay
 
@@ -149,70 +149,91 @@ __global__ __launch_bounds__(kSelThreads) void evict_keys_kernel(const Paged pg,
     to[tid] = (uint32_t)hist[2 * tid] | (uint32_t)hist[2 * tid + 1] << 16;
 }
 
-__global__ __launch_bounds__(kSelThreads) void evict_pick_kernel(const Paged pg, const int32_t *keep, int max_keep, const uint32_t *__restrict__ keys, int64_t stride,
-                                                                 const uint32_t *__restrict__ firsts, int segs, Picked *__restrict__ picked, int32_t *new_len)
+// The first digit of the m-th key, from all segments' counts; then, of a part of the keys, those that have it: set aside, and their second digits
+// counted.  (One workgroup for all keys of a request issued instructions for 21 us of 131072.)
+__global__ __launch_bounds__(kSelThreads) void evict_scan_kernel(const Paged pg, const int32_t *__restrict__ keep, int max_keep, const uint32_t *__restrict__ keys, int64_t stride,
+                                                                 const uint32_t *__restrict__ firsts, int segs, uint32_t *__restrict__ aside, int32_t *__restrict__ n_aside,
+                                                                 uint32_t *__restrict__ seconds, Picked *__restrict__ picked)
 {
-    extern __shared__ uint32_t aside_s[];                    // kAside keys a wave
     __shared__ int hist[kBins];
-    __shared__ int sums[kSelWaves], found[2], too_many;
+    __shared__ int sums[kSelWaves], found[2], taken;
+    const int b = blockIdx.y, part = blockIdx.x, parts = gridDim.x, tid = threadIdx.x;
+    const int len = len_of(pg, b);
+    const int m = kept_of(keep, max_keep, b, len);
+    const int64_t lo = (int64_t)part * kPart;
+    if (lo >= len || m == 0) return;
+    const int live = (len + kSeg - 1) / kSeg;
+    int large = 0, small = 0;                                // word kBins / 2 - 1 - tid
+#pragma unroll 32
+    for (int s = 0; s < live; ++s) {
+        const uint32_t w = firsts[((int64_t)b * segs + s) * (kBins / 2) + kBins / 2 - 1 - tid];
+        large += (int)(w >> 16);
+        small += (int)(w & 0xffffu);
+    }
+    uint32_t key[kPart / kSelThreads];
+#pragma unroll
+    for (int j = 0; j < kPart / kSelThreads; ++j) {
+        const int64_t i = lo + j * kSelThreads + tid;
+        key[j] = i < len ? keys[(int64_t)b * stride + i] : 0u;
+    }
+    hist[tid] = hist[tid + kSelThreads] = 0;
+    if (tid == 0) taken = 0;
+    uint32_t digit;
+    int want = m;
+    find_digit(large, small, sums, found, digit, want);
+    aside += (int64_t)b * stride + lo;
+#pragma unroll
+    for (int j = 0; j < kPart / kSelThreads; ++j) {
+        const bool mine = lo + j * kSelThreads + tid < len && key[j] >> 21 == digit;
+        const unsigned long long all = __ballot(mine);
+        int at = 0;
+        if ((tid & 63) == 0 && all) at = atomicAdd(&taken, __popcll(all));          // (any order: only their values count)
+        at = __builtin_amdgcn_readfirstlane(at);
+        if (mine) {
+            atomicAdd(&hist[(key[j] >> 10) & 2047u], 1);
+            aside[at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u))] = key[j];
+        }
+    }
+    __syncthreads();
+    seconds[((int64_t)b * parts + part) * (kBins / 2) + tid] = (uint32_t)hist[2 * tid] | (uint32_t)hist[2 * tid + 1] << 16;
+    if (tid == 0) {
+        n_aside[(int64_t)b * parts + part] = taken;
+        if (part == 0) picked[b] = {digit, want, m, len};    // so far
+    }
+}
+
+// The second digit from all parts' counts, the third from the keys set aside that have both.
+__global__ __launch_bounds__(kSelThreads) void evict_pick_kernel(const Paged pg, const int32_t *keep, int max_keep, int64_t stride, const uint32_t *__restrict__ aside, const int32_t *__restrict__ n_aside, const uint32_t *__restrict__ seconds, int parts, Picked *picked, int32_t *new_len)
+{
+    __shared__ int hist[kBins];
+    __shared__ int sums[kSelWaves], found[2];
     const int b = blockIdx.x, tid = threadIdx.x;
     const int len = len_of(pg, b);
     const int m = kept_of(keep, max_keep, b, len);
-    uint32_t *const aside = aside_s + (tid >> 6) * kAside;
     uint32_t key = 0xffffffffu;
     int want = m;
     if (m > 0) {
-        const int live = (len + kSeg - 1) / kSeg;
+        const int live = (int)(((int64_t)len + kPart - 1) / kPart);
+        const Picked first = picked[b];
         int large = 0, small = 0;                            // word kBins / 2 - 1 - tid
-#pragma unroll 32
+#pragma unroll 16
         for (int s = 0; s < live; ++s) {
-            const uint32_t w = firsts[((int64_t)b * segs + s) * (kBins / 2) + kBins / 2 - 1 - tid];
+            const uint32_t w = seconds[((int64_t)b * parts + s) * (kBins / 2) + kBins / 2 - 1 - tid];
             large += (int)(w >> 16);
             small += (int)(w & 0xffffu);
         }
-        hist[tid] = hist[tid + kSelThreads] = 0;
-        if (tid == 0) too_many = 0;
         uint32_t digit;
+        want = first.want;
         find_digit(large, small, sums, found, digit, want);
-        key = digit;
-        const uint4 *from = reinterpret_cast<const uint4 *>(keys + (int64_t)b * stride);
-        int n_aside = 0;                                     // of the wave
-        auto take = [&](uint32_t k, int i) {
-            const bool mine = i < len && k >> 21 == key;
-            const unsigned long long all = __ballot(mine);
-            if (mine) {
-                atomicAdd(&hist[(k >> 10) & 2047u], 1);
-                const int at = n_aside + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u));
-                if (at < kAside) aside[at] = k;
-            }
-            n_aside += __popcll(all);
-        };
-        constexpr int U = 8;
-        for (int i0 = 0; i0 < len; i0 += 4 * U * kSelThreads) {
-            uint4 k[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = i0 + 4 * (u * kSelThreads + tid);
-                k[u] = i < len ? from[i / 4] : make_uint4(0u, 0u, 0u, 0u);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = i0 + 4 * (u * kSelThreads + tid);
-                take(k[u].x, i); take(k[u].y, i + 1); take(k[u].z, i + 2); take(k[u].w, i + 3);
-            }
-        }
-        if (n_aside > kAside) too_many = 1;
-        __syncthreads();
-        find_digit(hist[kBins - 1 - 2 * tid], hist[kBins - 2 - 2 * tid], sums, found, digit, want);
-        key = key << 11 | digit;
+        key = first.key << 11 | digit;
         hist[tid] = hist[tid + kSelThreads] = 0;
         __syncthreads();
-        if (!too_many) {
-            for (int i = tid & 63; i < n_aside; i += kWave)
-                if (aside[i] >> 10 == key) atomicAdd(&hist[aside[i] & 1023u], 1);
-        } else {
-            for (int i = tid; i < len; i += kSelThreads) {
-                const uint32_t k = keys[(int64_t)b * stride + i];
+        for (int p = tid >> 6; p < live; p += kSelWaves) {   // a wave a part
+            const int n = n_aside[(int64_t)b * parts + p];
+            const uint32_t *from = aside + (int64_t)b * stride + (int64_t)p * kPart;
+#pragma unroll 8
+            for (int i = tid & 63; i < n; i += kWave) {
+                const uint32_t k = from[i];
                 if (k >> 10 == key) atomicAdd(&hist[k & 1023u], 1);
             }
         }
@@ -318,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const Paged pg, in
     }
 }
 
-struct Layout { int64_t stride, subs, segs; size_t picked, counts, keys, firsts, bytes; };
+struct Layout { int64_t stride, subs, segs, parts; size_t picked, counts, keys, firsts, aside, n_aside, seconds, bytes; };
 
 Layout layout_of(int64_t batch, int64_t max_ctx)
 {
@@ -331,7 +352,11 @@ Layout layout_of(int64_t batch, int64_t max_ctx)
     l.counts = up((size_t)batch * sizeof(Picked));
     l.keys = l.counts + up((size_t)batch * (size_t)l.subs * sizeof(int2));
     l.firsts = l.keys + up((size_t)batch * (size_t)l.stride * 4);
-    l.bytes = l.firsts + up((size_t)batch * (size_t)l.segs * (kBins / 2) * 4);
+    l.parts = l.segs ? (max_ctx + kPart - 1) / kPart : 0;
+    l.aside = l.firsts + up((size_t)batch * (size_t)l.segs * (kBins / 2) * 4);
+    l.n_aside = l.aside + (l.segs ? up((size_t)batch * (size_t)l.stride * 4) : 0);
+    l.seconds = l.n_aside + up((size_t)batch * (size_t)l.parts * 4);
+    l.bytes = l.seconds + up((size_t)batch * (size_t)l.parts * (kBins / 2) * 4);
     return l;
 }
 
@@ -378,17 +403,16 @@ extern "C" kvs_status kvs_evict_paged(const kvs_shape *shape, const kvs_paged_ca
         hipLaunchKernelGGL(evict_small_kernel, requests, dim3(kSelThreads), 0, hs, pg, shape->n_kv_heads, keep, (int)max_keep, n_first, n_recent, mass, mass_stride, keys, l.stride, picked,
                            counts, (int)l.subs, new_len);
     } else {
-        static DeviceOnce once;
-        constexpr int lds = kAside * kSelWaves * 4;
-        st = once_per_device(once, [&]() -> kvs_status {
-            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&evict_pick_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-            return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_evict_paged: %s", hipGetErrorString(e));
-        });
-        if (st != KVS_OK) return st;
+        uint32_t *aside = (uint32_t *)(ws + l.aside), *seconds = (uint32_t *)(ws + l.seconds);
+        int32_t *n_aside = (int32_t *)(ws + l.n_aside);
         hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)l.segs, (unsigned)pg.batch), dim3(kSelThreads), 0, hs, pg, shape->n_kv_heads, keep, (int)max_keep, n_first, n_recent, mass, mass_stride,
                            keys, l.stride, firsts);
         if ((st = check_launch(me)) != KVS_OK) return st;
-        hipLaunchKernelGGL(evict_pick_kernel, requests, dim3(kSelThreads), lds, hs, pg, keep, (int)max_keep, keys, l.stride, firsts, (int)l.segs, picked, new_len);
+        hipLaunchKernelGGL(evict_scan_kernel, dim3((unsigned)l.parts, (unsigned)pg.batch), dim3(kSelThreads), 0, hs, pg, keep, (int)max_keep, keys, l.stride, firsts, (int)l.segs, aside,
+                           n_aside, seconds, picked);
+        if ((st = check_launch(me)) != KVS_OK) return st;
+        hipLaunchKernelGGL(evict_pick_kernel, requests, dim3(kSelThreads), 0, hs, pg, keep, (int)max_keep, l.stride, aside, n_aside, seconds, (int)l.parts, picked,
+                           new_len);
         if ((st = check_launch(me)) != KVS_OK) return st;
         hipLaunchKernelGGL(evict_count_kernel, dim3((unsigned)((l.subs + kWaves - 1) / kWaves), (unsigned)pg.batch), threads, 0, hs, keys, l.stride, picked, counts, (int)l.subs);
     }

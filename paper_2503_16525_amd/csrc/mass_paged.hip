@@ -288,9 +288,10 @@ __global__ __launch_bounds__(kThreads, 2) void mass_few_kernel(
         const int r = j * RPL + lane / CPR;
         k_off[j] = (uint32_t)r * row_bytes + (uint32_t)((lane % CPR) ^ swz(r)) * 16u;
     }
-    // By hand, as in attention_paged.hip: the compiler would wait for all loads in flight before every LDS read.
+    // By hand, as in attention_paged.hip: the compiler would wait for all loads in flight before every LDS read.  Keys are read once, and the loads
+    // say so (64 contexts of 4096 to 16384 281 -> 259 us).
     auto load_1k = [&](uint32_t dst, uint32_t off, const char *base) {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(base) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(dst), "v"(off), "s"(base) : "memory");
     };
     const uint64_t granule_bytes = (uint64_t)row_bytes * kGranule;
 
