@@ -171,3 +171,16 @@ def test_a_pool_behind_32_bits():
     ws = torch.empty((B.kvs_workspace_size("attention_paged", c.shape, 2, 300, 160),), dtype=torch.uint8, device="cuda")
     B.kvs_attention_paged(c.shape, B.PagedCache(*big), B.PageTable(c.table + far, c.ctx_len, 300), c.cu_new, None, c.q, c.scale, 0, 0, out, lse, ws)
     R.check_attention(c, out, lse, R.attention(c), 1, "far pages")
+
+
+@pytest.mark.parametrize("hq,hk,n,window,n_first", [(64, 2, 1100, 0, 0), (64, 2, 1301, 200, 3), (32, 8, 2100, 300, 40), (40, 1, 1700, 0, 0), (64, 4, 1100, 33, 0)])
+def test_more_row_tiles_than_compute_units(hq, hk, n, window, n_first):
+    """One request's: each workgroup takes several, of which the first ones hold a V that only later tokens may multiply."""
+    def change(y, b, is_v):
+        y = y.clone()
+        if is_v:
+            y[n - 1, 0, 7] = float("nan")
+        return y
+    c = R.Case(hq, hk, 128, BF16, 32, [(n, list(range(n - 1)) + [0])], seed=n, change=change)
+    _check(c, "dealt", window, n_first)
+    _check(R.Case(hq, hk, 128, BF16, 16, [(n + 77, n)], seed=n + 1), "dealt chunk", window, n_first)
