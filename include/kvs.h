@@ -593,14 +593,15 @@ KVS_API kvs_status kvs_store_paged(const kvs_shape *shape, const kvs_paged_cache
  * A token that sees nothing gets 0 and -inf.  What a row does not see does not reach it, whatever it holds (NaN and
  * infinities too).
  *
- * q_new, out [dev] [n_new, n_q_heads, head_dim]      lse_out [dev] fp32[n_new, n_q_heads] or NULL
- * scale      any finite number
+ * q_new, out [dev] [n_new, n_q_heads, head_dim], no overlap      lse_out [dev] fp32[n_new, n_q_heads] or NULL
+ * scale      any number up to 2^127 in magnitude
  * workspace  [dev] optional (NULL / 0 is valid), 256-byte aligned, kvs_workspace_size("attention_paged", shape, batch,
- *            max_ctx, n_new) bytes: launches that would leave units idle cut their key ranges into pieces and merge them.  Less
- *            means fewer pieces.  One call's until that call has ended on its stream.
+ *            max_ctx, n_new) bytes: launches that would leave units idle cut their key ranges into pieces and merge them, and those
+ *            of many tokens go to a kernel of larger tiles.  Less means fewer pieces and smaller tiles.  One call's until that
+ *            call has ended on its stream.
  * bf16: fp32 accumulation and softmax; the weights enter the second product as two bf16 numbers that hold 16 of their bits where
  * there are no more than 32 rows (tokens times query heads of a KV head) a request on average, rounded to one elsewhere.  fp32
- * throughout otherwise.  Equal calls give equal bits.
+ * throughout otherwise.  Sums of values beyond 2^110 may become infinite.  Equal calls give equal bits.
  */
 KVS_API kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages,
                                        const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new, const void *q_new, float scale,

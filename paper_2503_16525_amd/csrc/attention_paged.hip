@@ -765,12 +765,14 @@ extern "C" kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_page
     Paged pg;
     kvs_status st = check_paged(me, shape, cache, pages, &pg);
     if (st != KVS_OK || (st = check_new_tokens(me, shape, pages, cu_new, sel_pos, n_new, window, n_first, &pg)) != KVS_OK) return st;
-    if (!isfinite(scale)) return fail(KVS_EINVAL, "%s: the scale is not finite", me);
+    if (!isfinite(scale * 1.4426950408889634f)) return fail(KVS_EINVAL, "%s: a scale of %g", me, (double)scale);
     if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return fail(KVS_EINVAL, "%s: workspace must be 256-byte aligned", me);
     if (!workspace) workspace_bytes = 0;
     if (n_new == 0 || pages->batch == 0) return KVS_OK;
     if (!q_new || !out) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
     if (!aligned16(q_new) || !aligned16(out)) return fail(KVS_EINVAL, "%s: Q/out pointers must be 16-byte aligned", me);
+    const uintptr_t q_at = (uintptr_t)q_new, out_at = (uintptr_t)out, bytes = (uintptr_t)n_new * shape->n_q_heads * shape->head_dim * elem_bytes(shape->dtype);
+    if (q_at < out_at + bytes && out_at < q_at + bytes) return fail(KVS_EINVAL, "%s: out overlaps q_new", me);
     hipStream_t hs = (hipStream_t)stream;
     const int grp = shape->n_q_heads / shape->n_kv_heads;
     const PagedCall call = describe(shape, pg);

@@ -20,6 +20,7 @@ constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kRows = 32;               // rows of a tile
 constexpr int kStep = 64;               // rows between two barriers
 constexpr int kMaxPieces = 16;
+constexpr int64_t kCutBelow = 1024;     // launches of fewer workgroups cut their rows, into twice as many
 template <int DTYPE> constexpr int kBlocks = DTYPE == KVS_F32 ? 1 : 2;             // of 32 keys a wave
 template <int DTYPE> constexpr int kWgKeys = 32 * kBlocks<DTYPE> * kWaves;
 
@@ -436,8 +437,8 @@ int pieces_of(const kvs_shape *shape, int64_t batch, int64_t max_ctx, int64_t n_
 {
     const int64_t wgs = batch * shape->n_kv_heads * blocks_of(shape, max_ctx);
     const int64_t steps = n_new * (shape->n_q_heads / shape->n_kv_heads) / (batch * kStep);
-    if (wgs <= 0 || wgs >= 1024 || batch * shape->n_kv_heads > 65535) return 1;
-    int64_t p = (2048 + wgs - 1) / wgs;
+    if (wgs <= 0 || wgs >= kCutBelow || batch * shape->n_kv_heads > 65535) return 1;
+    int64_t p = (2 * kCutBelow + wgs - 1) / wgs;
     if (p > steps / 4) p = steps / 4;
     if (p > kMaxPieces) p = kMaxPieces;
     return p < 1 ? 1 : (int)p;
@@ -491,8 +492,9 @@ size_t mass_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t
 {
     if (check_shape(shape) != KVS_OK || batch <= 0 || max_ctx <= 0 || n_new <= 0) return 256;
     if (few_rows(shape, batch, n_new)) return 256;
-    const int p = pieces_of(shape, batch, max_ctx, n_new);
-    return p == 1 ? 256 : ((size_t)p * (size_t)batch * shape->n_kv_heads * (size_t)max_ctx * 4 + 255) / 256 * 256;
+    // no more than kMaxPieces pieces, and of kWgKeys keys fewer than 2 kCutBelow and what one more piece makes
+    const int64_t all = (int64_t)batch * shape->n_kv_heads * max_ctx, most = (int64_t)3 * kCutBelow * kWgKeys<KVS_BF16>;
+    return ((size_t)(all < most / kMaxPieces ? all * kMaxPieces : most) * 4 + 255) / 256 * 256;
 }
 
 } // namespace kvs
@@ -507,7 +509,7 @@ extern "C" kvs_status kvs_mass_paged(const kvs_shape *shape, const kvs_paged_cac
     Paged pg;
     kvs_status st = check_paged(me, shape, cache, pages, &pg);
     if (st != KVS_OK || (st = check_new_tokens(me, shape, pages, cu_new, sel_pos, n_new, window, n_first, &pg)) != KVS_OK) return st;
-    if (!isfinite(scale)) return fail(KVS_EINVAL, "%s: the scale is not finite", me);
+    if (!isfinite(scale * 1.4426950408889634f)) return fail(KVS_EINVAL, "%s: a scale of %g", me, (double)scale);
     if (!isfinite(decay) || decay < 0.f) return fail(KVS_EINVAL, "%s: a decay of %g", me, (double)decay);
     if (mass_stride < pages->max_ctx) return fail(KVS_EINVAL, "%s: a mass stride of %lld for contexts of up to %lld", me, (long long)mass_stride, (long long)pages->max_ctx);
     if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return fail(KVS_EINVAL, "%s: workspace must be 256-byte aligned", me);

@@ -266,3 +266,28 @@ def test_equal_calls_give_equal_bits():
     for _ in range(3):
         for a, b in zip(first, _attend(c)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hq,hk,d", [(8, 2, 128), (28, 4, 128), (6, 6, 64)])
+def test_one_request_of_many_tokens_among_many_of_one(hq, hk, d, dtype):
+    """Few rows a request on average, but not in all: some come in several blocks."""
+    many = 32 * 40 * hk // hq - 40
+    reqs = [(30 + 7 * i, 1) for i in range(39)]
+    reqs.insert(20, (many + 100, many))
+    _check(R.Case(hq, hk, d, dtype, 16, reqs, seed=31), "skewed")
+    _check(R.Case(hq, hk, d, dtype, 16, reqs, seed=32), "skewed", 50, 5)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,tokens", [(64, 40), (128, 40), (128, 300)])
+def test_a_query_that_is_no_number_reaches_its_row_only(d, tokens, dtype):
+    c = R.Case(4, 2, d, dtype, 16, [(400, tokens), (50, 1)], seed=33)
+    ref = R.attention(c)
+    c.q[7, 2, 5], c.q[tokens, 0, 0] = float("nan"), float("inf")
+    out, lse = _attend(c)
+    broken = torch.zeros((c.n, 4), dtype=torch.bool, device="cuda")
+    broken[7, 2] = broken[tokens, 0] = True
+    assert torch.isnan(out[broken]).all() and torch.isnan(lse[broken]).all()
+    out[broken], lse[broken] = ref[0][broken].to(dtype), ref[1][broken].float()
+    R.check_attention(c, out, lse, ref, _parts(c), "broken queries")

@@ -139,3 +139,14 @@ def test_replays_from_a_graph():
         c.q.mul_(-1.1)
     assert (mass[0][0, :, :400] > 0).all() and (mass[0][:, :, 600:] == 0).all()
     assert (mass[0][2] == 0).all()                              # its table names no page
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hq,hk,d", [(8, 2, 128), (28, 4, 128), (6, 6, 64)])
+def test_one_request_of_many_tokens_among_many_of_one(hq, hk, d, dtype):
+    """Few rows a request on average, but not in all: some come in several blocks."""
+    many = 32 * 40 * hk // hq - 40
+    reqs = [(30 + 7 * i, 1) for i in range(39)]
+    reqs.insert(20, (many + 100, many))
+    _check(R.Case(hq, hk, d, dtype, 16, reqs, seed=31), "skewed")
+    _check(R.Case(hq, hk, d, dtype, 16, reqs, seed=32), "skewed", 50, 5)

@@ -67,13 +67,15 @@ def test_refusals_of_tokens(lib, name):
         assert call(n=0) == B.OK
     if name != "store":
         assert call(window=-1) == B.EINVAL and call(n_first=-1) == B.EINVAL
-        for scale in (float("nan"), float("inf")):
+        for scale in (float("nan"), float("inf"), -3e38):
             assert call(scale=scale) == B.EINVAL
         assert call(ws=FAKE + 16, ws_bytes=1000) == B.EINVAL
 
 
 def test_refusals_of_one_call(lib):
     assert _call(lib, "store", stride=999) == B.EINVAL
+    for q, out in ((FAKE, FAKE), (FAKE, FAKE + 10 * 32 * 256 - 16), (FAKE + 16, FAKE)):
+        assert _call(lib, "attention", q=q, out=out) == B.EINVAL and b"overlaps" in lib.kvs_last_error()
     assert _call(lib, "attention", out=None) == B.EINVAL and _call(lib, "attention", out=FAKE + 2) == B.EINVAL
     assert _call(lib, "mass", stride=999) == B.EINVAL
     assert _call(lib, "mass", lse=None) == B.EINVAL and _call(lib, "mass", mass_out=None) == B.EINVAL
@@ -95,7 +97,9 @@ def test_workspace_sizes(lib):
     for call in ("attention_paged", "mass_paged", "evict_paged"):
         sizes = [B.kvs_workspace_size(call, sh, 4, n, 8) for n in (1, 100, 5000, 100000)]
         assert all(x > 0 and x % 256 == 0 for x in sizes)
-        assert sizes == sorted(sizes) or call == "mass_paged"
+        assert sizes == sorted(sizes)
+        sizes = [B.kvs_workspace_size(call, sh, 4, 5000, n) for n in (1, 8, 100, 5000, 100000, 3000000)]
+        assert sizes == sorted(sizes)
         assert B.kvs_workspace_size(call, None, 4, 100, 8) == 0
     assert B.kvs_workspace_size("evict_paged", sh, 4, 100000) >= 4 * 100000 * 8
 
