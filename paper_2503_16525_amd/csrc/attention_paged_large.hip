@@ -39,6 +39,7 @@ constexpr int ROW_B = D * 2, TILE_B = BN * ROW_B;
 constexpr int AHEAD = 4;               // steps between a tile's request and its weights
 constexpr int K_RING = 4, V_RING = 8;
 constexpr int RING_B = (K_RING + V_RING) * TILE_B;
+constexpr int PLACES_AT = RING_B + 48;
 constexpr int kMostTiles = 6144;       // of a piece: 48 KB of places
 constexpr int kLeastTiles = 8;         // of a piece
 constexpr int kMostPieces = 32, kMostCutWgs = 512;
@@ -67,9 +68,9 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
     const Paged pg, int n_q_heads, int n_kv_heads, int units, int pieces, int least_tiles, const char *__restrict__ k_pool, const char *__restrict__ v_pool,
     const uint16_t *__restrict__ q_new, float scale_log2, uint16_t *__restrict__ out, float *__restrict__ lse_out, float *__restrict__ part_o, float4 *__restrict__ part_ml, int32_t *__restrict__ odd_out)
 {
-    extern __shared__ __attribute__((aligned(16))) char lds_b[];         // rings of K and V, places
-    __shared__ int meet_s[NWAVES][2];
-    __shared__ int odd_s;
+    extern __shared__ __attribute__((aligned(16))) char lds_b[];         // rings of K and V; meet_s, odd_s; places
+    int (*const meet_s)[2] = reinterpret_cast<int (*)[2]>(lds_b + RING_B);
+    int &odd_s = *reinterpret_cast<int *>(lds_b + RING_B + sizeof(int[NWAVES][2]));
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
     }
 
     // ---- places of the piece's tiles, two runs of 16 rows each; behind the context its last run --------------------------
-    int *const place_s = reinterpret_cast<int *>(lds_b + RING_B);
+    int *const place_s = reinterpret_cast<int *>(lds_b + PLACES_AT);
     const int last_run = (len - 1) / kGranule;
     bool odd = false;                                        // a run of no page
     for (int e = tid; e < 2 * (t_hi - t_lo); e += NT) {
@@ -178,37 +179,38 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
     if (odd) odd_s = 1;
 
     // ---- staging ------------------------------------------------------------------------------------------------------
-    // One instruction moves 64 x 16 bytes, four rows, to 1 KiB of LDS; a wave stages rows 4w .. 4w+3 of each half of a tile, K and V.
-    // Piece p of row r lies at p ^ f(r): f = r & 15 for K (8 lanes read one piece of 8 rows), 2 (r & 7) for V (a transposing read
-    // covers 4 rows x 2 pieces).
+    // One instruction moves 64 x 16 bytes, four rows, to 1 KiB of LDS.  Waves 0 and 1 stage the first and the second run of a tile's K, waves 2
+    // and 3 those of V: a wave has one address a step.  Piece p of row r lies at p ^ f(r): f = r & 15 for K (8 lanes read one piece of 8 rows),
+    // 2 (r & 7) for V (a transposing read covers 4 rows x 2 pieces).
     const uint32_t row_bytes = (uint32_t)n_kv_heads * ROW_B;
     const uint64_t run_bytes = (uint64_t)row_bytes * kGranule;
-    const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds_b);
-    const int st_row = 4 * wave + (lane >> 4), st_at = lane & 15;
-    const uint32_t k_off = (uint32_t)st_row * row_bytes + (uint32_t)(st_at ^ st_row) * 16u, v_off = (uint32_t)st_row * row_bytes + (uint32_t)(st_at ^ (2 * (st_row & 7))) * 16u;
-    const char *const k_head = k_pool + (uint32_t)g * ROW_B, *const v_head = v_pool + (uint32_t)g * ROW_B;
+    const bool of_k = wave < 2;
+    // (the select is one of scalars, which the compiler has to be told)
+    const uint64_t st_pool = (uint64_t)(of_k ? k_pool : v_pool) + (uint32_t)g * ROW_B;
+    const char *const st_head = (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)st_pool) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(st_pool >> 32)) << 32);
+    const int st_mask = of_k ? K_RING - 1 : V_RING - 1;
+    const uint32_t st_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds_b) +
+                             (uint32_t)((of_k ? 0 : K_RING) * TILE_B + (wave & 1) * kGranule * ROW_B);
+    uint32_t st_off[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 4 * i + (lane >> 4);
+        st_off[i] = (uint32_t)r * row_bytes + (uint32_t)((lane & 15) ^ (of_k ? r : 2 * (r & 7))) * 16u;
+    }
     auto load_1k = [&](uint32_t dst, uint32_t off, const char *base) {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(base) : "memory");
     };
     // Tile t goes to K slot t % K_RING and V slot t % V_RING, in the second half of step t - AHEAD, behind that step's barrier: the
     // slots' former tiles were last read a step before it at the latest.  Tiles behind the piece's last are loads of
     // that one, which nothing reads: the number of loads in flight is the same in every step.
-    struct Runs { int at[2]; };
-    auto runs_of = [&](int t) -> Runs {
-        const int2 p = *reinterpret_cast<const int2 *>(place_s + 2 * (min(max(t, t_lo), t_hi - 1) - t_lo));
-        return {{__builtin_amdgcn_readfirstlane(p.x), __builtin_amdgcn_readfirstlane(p.y)}};
-    };
-    auto stage_part = [&](int t, int part, const Runs &runs) {           // part 0, 1: rows 0-15 / 16-31 of K; 2, 3: of V
-        const int q = part & 1;
-        const uint64_t offset = (uint64_t)(uint32_t)runs.at[q] * run_bytes;
-        const bool of_k = part < 2;
-        const int slot = of_k ? (t & (K_RING - 1)) : K_RING + (t & (V_RING - 1));
-        load_1k(lds_base + (uint32_t)(slot * TILE_B + (16 * q + 4 * wave) * ROW_B), of_k ? k_off : v_off, (of_k ? k_head : v_head) + offset);
+    auto run_of = [&](int t) -> int { return __builtin_amdgcn_readfirstlane(place_s[2 * (min(max(t, t_lo), t_hi - 1) - t_lo) + (wave & 1)]); };
+    auto stage_part = [&](int t, int part, int run) {
+        load_1k(st_base + (uint32_t)((t & st_mask) * TILE_B + part * 4 * ROW_B), st_off[part], st_head + (uint64_t)(uint32_t)run * run_bytes);
     };
     auto stage_tile = [&](int t) {
-        const Runs runs = runs_of(t);
+        const int run = run_of(t);
 #pragma unroll
-        for (int part = 0; part < 4; ++part) stage_part(t, part, runs);
+        for (int part = 0; part < 4; ++part) stage_part(t, part, run);
     };
 #define KVS_PAGED_BARRIER(in_flight) asm volatile("s_waitcnt vmcnt(" #in_flight ")\n\ts_barrier" ::: "memory")
 
@@ -221,13 +223,15 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
     const int tr_key = 8 * (tr_g >> 1) + (tr_s >> 2), tr_c = 2 * (tr_g & 1) + ((tr_s & 3) >> 1);
     const uint32_t v_read_lo = (uint32_t)(tr_key * ROW_B + ((tr_c ^ (2 * (tr_key & 7))) * 16) + 8 * (tr_s & 1));
     const uint32_t v_read_hi = (uint32_t)((tr_key + 4) * ROW_B + ((tr_c ^ (2 * ((tr_key + 4) & 7))) * 16) + 8 * (tr_s & 1));
-    auto read_k = [&](uint32_t slot, int ks) -> u32x4_t { return *reinterpret_cast<const u32x4_t *>(lds_b + ((k_read ^ (uint32_t)(32 * ks)) + slot)); };
+    // (Addresses in LDS are numbers: the rings begin at 0, the kernel has no other LDS, and every offset that is not the lane's is in bits that the
+    // lane's part leaves 0, so that one instruction makes an address of both.)
+    typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
+    auto read_k = [&](uint32_t slot, int ks) -> u32x4_t { return *(const lds_u32x4 *)(uintptr_t)(k_read ^ ((uint32_t)(32 * ks) | slot)); };
     auto read_vt = [&](uint32_t slot, int a, int db) -> u32x4_t {
         typedef short v4i16 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
-        const uint32_t base = slot + (uint32_t)(16 * a * ROW_B);
-        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16 *)(lds_b + ((v_read_lo ^ (uint32_t)(64 * db)) + base))));
-        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16 *)(lds_b + ((v_read_hi ^ (uint32_t)(64 * db)) + base))));
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16 *)(uintptr_t)((v_read_lo ^ ((uint32_t)(64 * db) | slot)) + 16 * a * ROW_B)));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16 *)(uintptr_t)((v_read_hi ^ ((uint32_t)(64 * db) | slot)) + 16 * a * ROW_B)));
         return u32x4_t{lo.x, lo.y, hi.x, hi.y};
     };
     auto k_slot = [&](int t) -> uint32_t { return (uint32_t)((t & (K_RING - 1)) * TILE_B); };
@@ -333,7 +337,7 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
     // One step: scores of tile jt + 1, weights of tile jt, product of tile jt - 1.  On entry the tiles jt - 1 .. jt + 1 are in the rings
     // and jt + 2, jt + 3 on their way; s_in holds tile jt's scores, p_in tile jt - 1's weights, ka and va slice 0's operands.
     auto step = [&](auto masked, int jt, floatx16 (&s_in)[NB], floatx16 (&s_out)[NB], const u32x4_t (&p_in)[NB][2], u32x4_t (&p_out)[NB][2], u32x4_t &ka, u32x4_t &va,
-                    Runs &runs) __attribute__((always_inline)) {
+                    int &run) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked)::value;
         keep_sums();
         const uint32_t ks = k_slot(jt + 1), vs = v_slot(jt - 1), ks_next = k_slot(jt + 2), vs_next = v_slot(jt);
@@ -342,8 +346,8 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) bits[nb] = seen_bits(nb, tile_of(jt) * BN);
         }
-        const Runs now = runs;
-        runs = runs_of(jt + AHEAD + 1);
+        const int now = run;
+        run = run_of(jt + AHEAD + 1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             u32x4_t ka_n, va_n;
@@ -373,11 +377,13 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
             for (int u = 0; u < 4; u += 2) l_run[nbs] = add_rounded_pair(p_out[nbs][r0 >> 3][((r0 & 7) + u) >> 1], l_run[nbs]);
             l_exact[nbs] += (e[0] + e[1]) + (e[2] + e[3]);
             o_acc[db][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va), as_bf16x8(p_in[1][a]), o_acc[db][1], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);               // a slice's vector work stays beside its products (without: all products first, 1073 -> 991 us)
             ka = ka_n;
             va = va_n;
             if (i == 3) KVS_PAGED_BARRIER(4);                // tile jt + 2 has landed; jt + 3 may be in flight
             if (i >= 4) stage_part(jt + AHEAD, i - 4, now);
         }
+        asm volatile("" : "+v"(l_exact[0]), "+v"(l_exact[1]));       // (not put off to the branch below)
         if (outgrown()) recentre(jt, s_in, p_out);
     };
     auto product = [&](int t, const u32x4_t (&pop)[NB][2]) {
@@ -425,13 +431,13 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");          // (K of the first tile has been read)
         stage_tile(begin + AHEAD);
         u32x4_t ka = read_k(k_slot(begin + 2), 0), va = read_vt(v_slot(begin), 0, 0);
-        Runs runs = runs_of(begin + 1 + AHEAD);
+        int run = run_of(begin + 1 + AHEAD);
         int jt = begin + 1;
         // two steps a trip, so that scores and weights swap roles without copies
         auto sweep = [&](auto masked, int stop) __attribute__((always_inline)) {
             for (; jt < stop && jt + 1 < t_hi; jt += 2) {
-                step(masked, jt, s_nxt, s_cur, p_a, p_b, ka, va, runs);
-                step(masked, jt + 1, s_cur, s_nxt, p_b, p_a, ka, va, runs);
+                step(masked, jt, s_nxt, s_cur, p_a, p_b, ka, va, run);
+                step(masked, jt + 1, s_cur, s_nxt, p_b, p_a, ka, va, run);
             }
         };
         sweep(std::true_type{}, clear_lo);
@@ -546,7 +552,7 @@ kvs_status launch_attention_paged_large(const kvs_shape *shape, const kvs_paged_
                                         void *out, float *lse_out, void *workspace, hipStream_t hs)
 {
     static DeviceOnce once;
-    constexpr int most_lds = RING_B + 8 * kMostTiles;
+    constexpr int most_lds = PLACES_AT + 8 * kMostTiles;
     kvs_status st = once_per_device(once, [&]() -> kvs_status {
         hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_paged_large_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, most_lds);
         if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_paged_large_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, most_lds);
@@ -556,7 +562,7 @@ kvs_status launch_attention_paged_large(const kvs_shape *shape, const kvs_paged_
     const int64_t wgs = plan.units * plan.pieces * shape->n_kv_heads;
     int32_t *const odd = (int32_t *)workspace;
     const PagedParts parts = paged_parts((char *)workspace + odd_bytes(wgs), (int64_t)pg.n_new * shape->n_q_heads * plan.pieces);
-    const int lds = RING_B + (8 * plan.tiles + 15) / 16 * 16;
+    const int lds = PLACES_AT + (8 * plan.tiles + 15) / 16 * 16;
     // (The rows of one request: of several, whose contexts differ, every tile finds its place as one becomes free.)
     const bool dealt = plan.pieces == 1 && pg.batch == 1 && wgs > 256 && 256 % shape->n_kv_heads == 0;
 #define KVS_LARGE(DEAL, N)                                                                                                                                      \
