@@ -15,6 +15,11 @@
 // this tile's has been read, V likewise, so that a tile's worth of loads is under way all the time, and two workgroups share a CU.
 // At the end the waves meet in LDS.  Launches of too few workgroups cut the keys into pieces, which a second kernel merges.
 //
+// Measured (bf16, 128 channels, one token a request, 28 or 32 query heads).  Memory bounds the long ones: 131072 keys of 4 KV heads, 268 MB, 44.5 us and
+// 4.8 for the merge, 6.0 TB/s; 64 contexts of 4096 to 16384 of 8 KV heads, 2.6 GB, 435 us, 6.0 TB/s.  The short ones are a chain of trips: launch and
+// length 2, Q and the first keys, the meeting, 6.0 us up to 128 keys, and 1.0 more for every further tile of a wave, since only one is under way: 601
+// keys 10.7.  (Eight waves a workgroup instead: 601 keys 10.0, but 1000 11.4 for 10.7 and 128 7.1 for 6.2.)
+//
 // fp32 goes through the fp32 matrix instruction, whose operands need no other order than that of memory.
 #include "attention_paged.h"
 
@@ -606,7 +611,7 @@ constexpr int64_t kMostCutWgs = 4 * kPlaces;
 // beyond 512 wait for the first; the cache comes at 5.1 TB/s, and the two hide each other less the closer they are; where reading bounds the call
 // or there are rounds, contexts of a batch that are longer than others hold the end up by a third of a piece, and the average one is shorter
 // than the longest; 6 for the launch and a workgroup's beginning and end, 4 for a merge's.  Over 39 calls of 1 to 6000 tokens and 500 to 60000
-// keys the kernel and number of pieces that this takes are within 10 % of the best there is in 30, within 22 % in 38.
+// keys the kernel and number of pieces that this takes are within 10 % of the best there is in 35, within 22 % in all.
 Plan plan_pieces(const kvs_shape *shape, const Paged &pg, const PagedCall &call, size_t workspace_bytes)
 {
     const int64_t wgs = (int64_t)pg.batch * call.row_blocks * shape->n_kv_heads, most = most_tiles(pg, call.grp);
@@ -625,7 +630,9 @@ Plan plan_pieces(const kvs_shape *shape, const Paged &pg, const PagedCall &call,
         double computing = step * steps * (a_unit > 8.0 ? 0.78 * a_unit : 1.5 * rounds + (rest > 0.9 ? 1.5 : rest > 0.0 ? 1.0 : 0.0));
         const bool waits = a_unit > 2.0 || reading > computing;
         if (a_unit > 2.0) computing *= 1.0 - 0.15 * several;
-        const double us = cbrt(computing * computing * computing + reading * reading * reading) + (waits ? 0.35 * several * steps : 0.0) + 6.0 + (n > 1 ? 4.0 + call.merge_us * (double)n : 0.0);
+        double us = cbrt(computing * computing * computing + reading * reading * reading) + (waits ? 0.35 * several * steps : 0.0) + 6.0 + (n > 1 ? 4.0 + call.merge_us * (double)n : 0.0);
+        // (more than the places hold, where fewer would fill them: 4 contexts of up to 9000 keys 28.4, in a third of the pieces 24.2; of 30000 41.9, 36.7)
+        if (a_unit > 2.0 && wgs < 256) us *= 1.0 + 0.05 * several;
         if (us < best.us) best = {(int32_t)n, us};
         return true;
     };

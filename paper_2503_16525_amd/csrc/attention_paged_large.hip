@@ -18,7 +18,13 @@
 //
 // A weight of 0 does not hide a V that is infinite or NaN.  A workgroup whose sums are no numbers, or that met an entry of the table
 // that names no page, says so, and a last launch does its rows once more with the kernel of attention_paged.hip, which
-// multiplies such keys with the weights of the rows that see them.  (Almost always nothing is to do: 2 us.)
+// multiplies such keys with the weights of the rows that see them.  (Almost always nothing is to do: 4 us.)
+//
+// What bounds it: vector instructions and matrix instructions, of which a step has 32 and about 200 others, that hide each other by half, at a clock that comes
+// down as they do (2.08 GHz at 41 % of the matrix pipes' cycles, 1.98 at 47 %).  2048 tokens of 32 heads over 32768 keys 975 to 1000 us by box, 1.06 to
+// 1.09 PFLOP/s; 8192 under a window of 4096 435, 0.95.  On the first: all but the scores' products left out 897, no exponentials 857, nothing read or
+// loaded 841.  v_dot2 shares the matrix pipes: shifts and additions in its place 997, no sum of the rounded weights at all 937, which would cost a row that
+// one key dominates its exactness.  Operands asked for two slices ahead, weights in seven slices of eight, and a check every other step gained nothing.
 #include "attention_paged.h"
 
 #include <type_traits>
@@ -534,9 +540,9 @@ bool attention_paged_takes_large(const kvs_shape *shape, const Paged &pg, const 
         const int64_t each = (tiles + p - 1) / p;
         if (each > kMostTiles) continue;
         if (p > 1 && each < kLeastTiles) break;
-        // Rounds of one workgroup a compute unit: 0.97 us a tile and 6 to begin and end; 3 for the last launch; a merge.  (us, estimate and
-        // measured: 256 tokens of 32 heads over 16384 keys in one piece 506, 506; eight 95, 97; ten 143, 140; 500 of 28 heads over 12000 in four 121, 122.)
-        const double us = (double)((wgs * p + 255) / 256) * (0.97 * (double)each + 6.0) + 3.0 + (p > 1 ? 4.0 + call.merge_us * (double)p : 0.0);
+        // Rounds of one workgroup a compute unit: 0.90 us a tile and 6 to begin and end; 3 for the last launch; a merge.  (us, estimate and
+        // measured: 256 tokens of 32 heads over 16384 keys in one piece 471, 437; eight 91, 93; ten 139, 134; 500 of 28 heads over 12000 in four 115, 113.)
+        const double us = (double)((wgs * p + 255) / 256) * (0.90 * (double)each + 6.0) + 3.0 + (p > 1 ? 4.0 + call.merge_us * (double)p : 0.0);
         if (us < plan->us) {
             plan->us = us;
             plan->pieces = (int32_t)p;

@@ -7,7 +7,8 @@
 //   their keys and count their first digits; parts add these up, set their keys of the one value aside and count the second
 //   digits; a workgroup a request finds the rest among those; a fourth counts what stays of every 256 rows.
 //   The last launch moves: a workgroup for every 256 rows ranks its own behind those before it and copies them.
-// What bounds it: the copy, at most; the keys' passes are a few dependent trips to memory each.
+// What bounds it: the copy, at most; the keys' passes are a few dependent trips to memory each.  (131072 rows of 4 heads to 65536: keys 5.6 us, first
+// digits 7.9, the rest 9.5, counts 4.7, the copy of 268 MB 56, 4.8 TB/s, 95 with the launches' gaps; 4097 rows to 3584 8.8 and 7.0.)
 #include "paged.h"
 
 namespace kvs {

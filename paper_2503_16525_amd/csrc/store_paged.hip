@@ -2,7 +2,7 @@
 //
 // A copy whose bytes bound it where it is large, and a chain of dependent trips to memory where it is small: the token's request,
 // its position, its page.  A wave takes 4 KiB or so of rows and asks for their data first, so that only the stores wait for the
-// chain.  (8192 rows of 8 heads: ... us.)
+// chain.  (8192 rows of 8 heads of bf16, 128 channels, K and V: 67 MB in 11.9 us, 5.6 TB/s; one row of 4 heads 2.1 us, a launch and the chain.)
 #include "paged.h"
 
 namespace kvs {
