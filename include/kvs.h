@@ -593,7 +593,7 @@ KVS_API kvs_status kvs_store_paged(const kvs_shape *shape, const kvs_paged_cache
  * A token that sees nothing gets 0 and -inf.  What a row does not see does not reach it, whatever it holds (NaN and
  * infinities too).
  *
- * q_new, out [dev] [n_new, n_q_heads, head_dim], no overlap      lse_out [dev] fp32[n_new, n_q_heads] or NULL
+ * q_new, out [dev] [n_new, n_q_heads, head_dim]      lse_out [dev] fp32[n_new, n_q_heads] or NULL      no overlap
  * scale      any number up to 2^127 in magnitude
  * workspace  [dev] optional (NULL / 0 is valid), 256-byte aligned, kvs_workspace_size("attention_paged", shape, batch,
  *            max_ctx, n_new) bytes: launches that would leave units idle cut their key ranges into pieces and merge them, and those

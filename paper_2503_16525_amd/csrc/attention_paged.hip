@@ -778,8 +778,10 @@ extern "C" kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_page
     if (n_new == 0 || pages->batch == 0) return KVS_OK;
     if (!q_new || !out) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
     if (!aligned16(q_new) || !aligned16(out)) return fail(KVS_EINVAL, "%s: Q/out pointers must be 16-byte aligned", me);
-    const uintptr_t q_at = (uintptr_t)q_new, out_at = (uintptr_t)out, bytes = (uintptr_t)n_new * shape->n_q_heads * shape->head_dim * elem_bytes(shape->dtype);
-    if (q_at < out_at + bytes && out_at < q_at + bytes) return fail(KVS_EINVAL, "%s: out overlaps q_new", me);
+    const size_t heads = (size_t)n_new * shape->n_q_heads, bytes = heads * shape->head_dim * elem_bytes(shape->dtype);
+    if (overlap(q_new, bytes, out, bytes)) return fail(KVS_EINVAL, "%s: out overlaps q_new", me);
+    if (lse_out && (overlap(lse_out, heads * sizeof(float), q_new, bytes) || overlap(lse_out, heads * sizeof(float), out, bytes)))
+        return fail(KVS_EINVAL, "%s: lse_out overlaps q_new or out", me);
     hipStream_t hs = (hipStream_t)stream;
     const int grp = shape->n_q_heads / shape->n_kv_heads;
     const PagedCall call = describe(shape, pg);

@@ -562,6 +562,10 @@ kvs_status launch_attention_paged_large(const kvs_shape *shape, const kvs_paged_
     kvs_status st = once_per_device(once, [&]() -> kvs_status {
         hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_paged_large_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, most_lds);
         if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_paged_large_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, most_lds);
+        hipFuncAttributes one = {}, other = {};
+        if (e == hipSuccess) e = hipFuncGetAttributes(&one, reinterpret_cast<const void *>(&attention_paged_large_kernel<false>));
+        if (e == hipSuccess) e = hipFuncGetAttributes(&other, reinterpret_cast<const void *>(&attention_paged_large_kernel<true>));
+        if (e == hipSuccess && one.sharedSizeBytes + other.sharedSizeBytes != 0) return fail(KVS_EHIP, "kvs_attention_paged: its rings do not begin at address 0");
         return e == hipSuccess ? KVS_OK : fail(KVS_EHIP, "kvs_attention_paged: %s", hipGetErrorString(e));
     });
     if (st != KVS_OK) return st;

@@ -390,7 +390,8 @@ extern "C" kvs_status kvs_evict_paged(const kvs_shape *shape, const kvs_paged_ca
     if (pages->batch == 0) return KVS_OK;
     if (!keep || !mass) return fail(KVS_EINVAL, "%s: keep or mass is NULL", me);
     if (pages->batch > 65535) return fail(KVS_EINVAL, "%s: %d requests in one call", me, pages->batch);
-    if (mass == new_mass) return fail(KVS_EINVAL, "%s: new_mass may not be mass", me);
+    const size_t lines = (size_t)pages->batch * shape->n_kv_heads * sizeof(float);
+    if (new_mass && overlap(mass, lines * mass_stride, new_mass, lines * max_keep)) return fail(KVS_EINVAL, "%s: new_mass overlaps mass", me);
     if (!workspace || workspace_bytes < evict_paged_workspace_bytes(shape, pages->batch, pg.max_ctx)) return fail(KVS_EWORKSPACE, "%s: workspace too small", me);
     hipStream_t hs = (hipStream_t)stream;
     if (pg.max_ctx == 0) max_keep = 0;

@@ -521,6 +521,8 @@ extern "C" kvs_status kvs_mass_paged(const kvs_shape *shape, const kvs_paged_cac
     if (!workspace) workspace_bytes = 0;
     if (pages->batch == 0 || pg.max_ctx == 0) return KVS_OK;
     if (!mass_out) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
+    const size_t mass_bytes = (size_t)pages->batch * shape->n_kv_heads * mass_stride * sizeof(float);
+    if (mass && mass != mass_out && overlap(mass, mass_bytes, mass_out, mass_bytes)) return fail(KVS_EINVAL, "%s: mass_out overlaps mass without being it", me);
     if (n_new > 0 && (!q_new || !lse)) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
     if (!aligned16(q_new)) return fail(KVS_EINVAL, "%s: Q must be 16-byte aligned", me);
     const bool wide = shape->head_dim == 128;

@@ -21,6 +21,10 @@ kvs_status check_paged(const char *me, const kvs_shape *shape, const kvs_paged_c
 // the same with a call's new tokens
 kvs_status check_new_tokens(const char *me, const kvs_shape *shape, const kvs_page_table *pages, const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new,
                             int32_t window, int32_t n_first, Paged *out);
+inline bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
 size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new);
 size_t mass_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new);
 size_t evict_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx);

@@ -92,6 +92,19 @@ def test_refusals_of_one_call(lib):
     assert evict(batch=70000) == B.EINVAL
 
 
+def test_refusals_of_outputs_over_inputs(lib):
+    q, rows = 0x100000, 10 * 32                              # ten tokens of 32 heads
+    attention = lambda **kw: _call(lib, "attention", q=q, **kw)
+    assert attention(out=q + rows * 256 - 16, lse=None) == B.EINVAL and b"out overlaps" in lib.kvs_last_error()
+    assert attention(out=q + rows * 256, lse=q + rows * 256 - 4) == B.EINVAL and b"lse_out overlaps" in lib.kvs_last_error()
+    assert attention(out=q + rows * 256, lse=q + 2 * rows * 256 - 4) == B.EINVAL and b"lse_out overlaps" in lib.kvs_last_error()
+    assert _call(lib, "mass", mass=FAKE, mass_out=FAKE + 4) == B.EINVAL and b"mass_out overlaps" in lib.kvs_last_error()
+    assert _call(lib, "mass", mass=FAKE + 4 * 8 * 1000 * 4 - 4, mass_out=FAKE) == B.EINVAL and b"mass_out overlaps" in lib.kvs_last_error()
+    assert _call(lib, "evict", new_mass=FAKE + 4 * 8 * 1000 * 4 - 4) == B.EINVAL and b"new_mass overlaps" in lib.kvs_last_error()
+    assert _call(lib, "evict", mass=FAKE + 4 * 8 * 500 * 4 - 4, new_mass=FAKE) == B.EINVAL and b"new_mass overlaps" in lib.kvs_last_error()
+    assert _call(lib, "evict", new_mass=FAKE + 4 * 8 * 1000 * 4) == B.EWORKSPACE         # behind it
+
+
 def test_workspace_sizes(lib):
     sh = B.make_shape(32, 8, 128, B.BF16)
     for call in ("attention_paged", "mass_paged", "evict_paged"):
