@@ -6,10 +6,10 @@
 //
 // A wave keeps its keys as operands in registers for the whole call and the rows come by, 32 at a time, through LDS.
 //
-// What bounds it: a step's vector instructions (an fma, an exponential and an addition a score) and its products take 520 and 510 of 1180 thousand cycles,
-// and with the reads from LDS beside either 407 and 415 of 560 us (2048 tokens of 32 heads over 32768 keys, 0.96 PFLOP/s).  Fenced beside
-// each other as in attention_paged_large.hip they take 545 to 590, whether within a step or across; with a row a lane, so that a tile has one lse a lane, 575;
-// 128 keys and one wave a SIMD 895.
+// What bounds it: the vector instructions (an fma, an exponential and an addition a score), the products and the reads of their operands from LDS, which
+// hide each other in part: 2048 tokens of 32 heads over 32768 keys take 537 to 553 us by box, 0.97 to 1.0 PFLOP/s, without the vector work 407, without loads of
+// rows as well 382, the products alone as a probe has them 279.  Without a tile's exponentials beside the next one's products 560; a tile that
+// waits for the next step's 589; a row a lane, so that a tile has one lse a lane, 575; eight waves a workgroup 558; 128 keys and one wave a SIMD 895.
 #include "paged.h"
 
 #include <math.h>
@@ -23,9 +23,12 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kRows = 32;               // rows of a tile
-constexpr int kStep = 64;               // rows between two barriers
+template <int ROW_B> constexpr int kStepRows = ROW_B <= 256 ? 128 : 64;           // rows between two barriers
+constexpr int kPieceRows = 64;          // rows that pieces are counted in
 constexpr int kMaxPieces = 16;
-constexpr int64_t kCutBelow = 1024;     // launches of fewer workgroups cut their rows, into twice as many
+// Launches of fewer workgroups than fill the chip cut their rows, into four times as many.  (Of fewer than 1024, 8 contexts of 4000 with 48 tokens of 28 heads
+// each 33 -> 45 us; into twice as many, 6000 tokens of 6000 264 -> 272.)
+constexpr int64_t kCutBelow = 512;
 template <int DTYPE> constexpr int kBlocks = DTYPE == KVS_F32 ? 1 : 2;             // of 32 keys a wave
 template <int DTYPE> constexpr int kWgKeys = 32 * kBlocks<DTYPE> * kWaves;
 
@@ -42,13 +45,13 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
     constexpr int NB = kBlocks<DTYPE>;
     constexpr int NS = CPR / 2;                              // products of a tile (fp32: four each)
     constexpr int RPL = kWave / CPR;                         // rows a load moves
+    constexpr int kStep = kStepRows<ROW_B>, kStepsInfo = kThreads / kStep;
     constexpr int NQ = kStep / RPL / kWaves;                 // loads of a wave for a step's rows
     constexpr int NT = kStep / kRows;                        // tiles of a step
     __shared__ __attribute__((aligned(16))) char q_s[2][kStep * ROW_B];
     __shared__ __attribute__((aligned(16))) float lse_s[2][kThreads];       // of a workgroup's number of rows
     __shared__ __attribute__((aligned(16))) int pos_s[2][kThreads];
-    __shared__ int span_s[2][kWaves][3];                     // of a step: lowest position, highest, lowest of those that see anything
-    static_assert(kStep == kWave, "a wave looks after a step's rows");
+    __shared__ int span_s[2][kWaves][3];                     // of 64 rows: lowest position, highest, lowest of those that see anything
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -61,7 +64,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
     const int len = len_of(pg, b);
     const int wg_lo = kb * kWgKeys<DTYPE>;
     if (wg_lo >= len) return;
-    const int wg_hi = min(wg_lo + kWgKeys<DTYPE>, len) - 1;
+    const int my_lo = wg_lo + wave * NB * 32, my_hi = min(my_lo + NB * 32, len) - 1;   // the wave's keys
     int tok0, n_tok;
     tokens_of(pg, b, tok0, n_tok);
     const int grp = n_q_heads / n_kv_heads;
@@ -74,7 +77,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
     bool there[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const int key = wg_lo + (wave * NB + nb) * 32 + ln;
+        const int key = my_lo + nb * 32 + ln;
         const int at = granule_of(pg, b, key / kGranule);
         there[nb] = at >= 0 && key < len;
         const char *from = k_pool + (((int64_t)max(at, 0) * kGranule + key % kGranule) * n_kv_heads + g) * ROW_B;
@@ -144,7 +147,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
     for (int nb = 0; nb < NB; ++nb) acc[nb] = 0.f;
     if (st_lo < st_hi) { fetch_info(); stage(st_lo); }
     for (int st = st_lo; st < st_hi; ++st) {
-        const int buf = (st - st_lo) & 1, sub = (st - st_lo) % kWaves, ibuf = ((st - st_lo) / kWaves) & 1;
+        const int buf = (st - st_lo) & 1, sub = (st - st_lo) % kStepsInfo, ibuf = ((st - st_lo) / kStepsInfo) & 1;
         if (sub == 0) {
             int lo = pos_next, hi = pos_next, low = pos_next < 0 ? 0x7fffffff : pos_next;
 #pragma unroll
@@ -161,11 +164,21 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
         __syncthreads();
         if (st + 1 < st_hi) {
             stage(st + 1);
-            if (sub == kWaves - 1) fetch_info();
+            if (sub == kStepsInfo - 1) fetch_info();
         }
-        const int pmin = __builtin_amdgcn_readfirstlane(span_s[ibuf][sub][0]), pmax = __builtin_amdgcn_readfirstlane(span_s[ibuf][sub][1]), plow = __builtin_amdgcn_readfirstlane(span_s[ibuf][sub][2]);
-        if (pmax < wg_lo || (window && wg_hi <= plow - window && wg_lo >= n_first)) continue;
-        const bool masked = wg_hi > pmin || (window && wg_lo <= pmax - window && wg_hi >= n_first);
+        constexpr int WPS = kStep / kWave;                   // waves that looked at a step's rows
+        int pmin = 0x7fffffff, pmax = -1, plow = 0x7fffffff;
+#pragma unroll
+        for (int i = 0; i < WPS; ++i) {
+            pmin = min(pmin, span_s[ibuf][sub * WPS + i][0]);
+            pmax = max(pmax, span_s[ibuf][sub * WPS + i][1]);
+            plow = min(plow, span_s[ibuf][sub * WPS + i][2]);
+        }
+        pmin = __builtin_amdgcn_readfirstlane(pmin);
+        pmax = __builtin_amdgcn_readfirstlane(pmax);
+        plow = __builtin_amdgcn_readfirstlane(plow);
+        if (pmax < my_lo || (window && my_hi <= plow - window && my_lo >= n_first)) continue;
+        const bool masked = my_hi > pmin || (window && my_lo <= pmax - window && my_hi >= n_first);
         auto scores = [&](int t, floatx16 (&s)[NB]) {
             const int r = t * kRows + ln;
 #pragma unroll
@@ -206,7 +219,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
 #pragma unroll
                     for (int u = 0; u < 4; ++u) e[u] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][4 * q + u], scale_log2, -l[u]));
                     if constexpr (decltype(with_mask)::value) {
-                        const int key = wg_lo + (wave * NB + nb) * 32 + ln;
+                        const int key = my_lo + nb * 32 + ln;
 #pragma unroll
                         for (int u = 0; u < 4; ++u) e[u] = key <= p[u] && (!window || key > p[u] - window || key < n_first) ? e[u] : 0.f;
                     }
@@ -216,25 +229,83 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) acc[nb] += sum[nb];
         };
-        if (masked) {
+        // Products of tile t beside the exponentials of the tile before, whose rows' lse begin at l_at.  A slice is the products of 32 (fp32: 8) of a
+        // row's channels and as large a part of the exponentials; the fences keep it together, and operands are read two slices ahead.
+        // (2048 tokens of 32 heads over 32768 keys 560 -> 537 us; one slice ahead 550; four 537.)
+        constexpr int AH = 2;
+        auto read_q = [&](int at) { return *reinterpret_cast<const u32x4_t *>(q_s[buf] + (at / NS * kRows + ln) * ROW_B + ((2 * (at % NS) + hf) ^ swz(ln)) * 16); };
+        auto both = [&](int t, floatx16 (&s)[NB], const floatx16 (&before)[NB], const float *l_at, u32x4_t (&w)[AH], auto exps) __attribute__((always_inline)) {
+            constexpr bool EXPS = decltype(exps)::value;
+            constexpr int EACH = 16 * NB / NS, SLICES = 4 * NB / EACH > 0 ? 4 * NB / EACH : 1;
+            const floatx16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            float4 l4 = {}, l4_n = {};
+            if (EXPS) l4 = *reinterpret_cast<const float4 *>(l_at);
+            float sum[NB];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) sum[nb] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NS; ++c) {
+                const u32x4_t w_n = read_q(min(t * NS + c + AH, NT * NS - 1));
+                if (EXPS && c % SLICES == 0 && c / SLICES < 3) l4_n = *reinterpret_cast<const float4 *>(l_at + 8 * (c / SLICES + 1));
+                const float l[4] = {l4.x, l4.y, l4.z, l4.w};
+                float e[EACH];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) s[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[(t * NS + c) % AH][u]), __uint_as_float(kreg[nb][c][u]), c + u == 0 ? zero : s[nb], 0, 0, 0);
+                    } else {
+                        s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w[(t * NS + c) % AH]), as_bf16x8(kreg[nb][c]), c == 0 ? zero : s[nb], 0, 0, 0);
+                    }
+                    if (EXPS && nb == 0) {
+#pragma unroll
+                        for (int u = 0; u < EACH; ++u) {
+                            const int at = c * EACH + u;
+                            e[u] = __builtin_amdgcn_exp2f(__builtin_fmaf(before[at / 4 % NB][at / (4 * NB) * 4 + at % 4], scale_log2, -l[at % 4]));
+                        }
+                    }
+                }
+                if (EXPS) {
+#pragma unroll
+                    for (int u = 0; u < EACH; ++u) sum[(c * EACH + u) / 4 % NB] += e[u];
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) asm volatile("" : "+v"(sum[nb]));
+                }
+                w[(t * NS + c) % AH] = w_n;
+                if (EXPS && c % SLICES == SLICES - 1) l4 = l4_n;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (EXPS) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) acc[nb] += sum[nb];
+            }
+        };
+        if (masked || (st + 1) * kStep > rows) {
 #pragma unroll 1
-            for (int t = 0; t < NT; ++t) {
+            for (int t = 0; t < NT && st * kStep + t * kRows < rows; ++t) {
+                const int *const span = span_s[ibuf][sub * WPS + t * kRows / kWave];
+                if (__builtin_amdgcn_readfirstlane(span[1]) < my_lo) continue;
                 floatx16 s[NB];
                 scores(t, s);
-                add_up(t, s, std::true_type{});
+                if (window || my_hi > __builtin_amdgcn_readfirstlane(span[0])) add_up(t, s, std::true_type{});
+                else add_up(t, s, std::false_type{});
             }
         } else {
-            floatx16 s[NT][NB];
+            const float *const l_at = &lse_s[ibuf][sub * kStep + 4 * hf];
+            floatx16 s[2][NB];
+            u32x4_t w[AH];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) scores(t, s[t]);
+            for (int i = 0; i < AH; ++i) w[i] = read_q(i);
+            both(0, s[0], s[1], l_at, w, std::false_type{});
 #pragma unroll
-            for (int t = 0; t < NT; ++t) add_up(t, s[t], std::false_type{});
+            for (int t = 1; t < NT; ++t) both(t, s[t & 1], s[(t - 1) & 1], l_at + (t - 1) * kRows, w, std::true_type{});
+            add_up(NT - 1, s[(NT - 1) & 1], std::false_type{});
         }
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         float total = acc[nb] + __shfl_xor(acc[nb], 32);
-        const int key = wg_lo + (wave * NB + nb) * 32 + ln;
+        const int key = my_lo + nb * 32 + ln;
         if (hf != 0 || key >= len) continue;
         if (!there[nb]) total = 0.f;
         if (pieces > 1) {
@@ -441,10 +512,10 @@ inline int64_t blocks_of(const kvs_shape *shape, int64_t max_ctx)
 int pieces_of(const kvs_shape *shape, int64_t batch, int64_t max_ctx, int64_t n_new)
 {
     const int64_t wgs = batch * shape->n_kv_heads * blocks_of(shape, max_ctx);
-    const int64_t steps = n_new * (shape->n_q_heads / shape->n_kv_heads) / (batch * kStep);
+    const int64_t steps = n_new * (shape->n_q_heads / shape->n_kv_heads) / (batch * kPieceRows);
     if (wgs <= 0 || wgs >= kCutBelow || batch * shape->n_kv_heads > 65535) return 1;
-    int64_t p = (2 * kCutBelow + wgs - 1) / wgs;
-    if (p > steps / 4) p = steps / 4;
+    int64_t p = (4 * kCutBelow + wgs - 1) / wgs;
+    if (p > (steps + 3) / 4) p = (steps + 3) / 4;
     if (p > kMaxPieces) p = kMaxPieces;
     return p < 1 ? 1 : (int)p;
 }
@@ -497,8 +568,8 @@ size_t mass_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t
 {
     if (check_shape(shape) != KVS_OK || batch <= 0 || max_ctx <= 0 || n_new <= 0) return 256;
     if (few_rows(shape, batch, n_new)) return 256;
-    // no more than kMaxPieces pieces, and of kWgKeys keys fewer than 2 kCutBelow and what one more piece makes
-    const int64_t all = (int64_t)batch * shape->n_kv_heads * max_ctx, most = (int64_t)3 * kCutBelow * kWgKeys<KVS_BF16>;
+    // no more than kMaxPieces pieces, and of kWgKeys keys fewer than 4 kCutBelow and what one more piece makes
+    const int64_t all = (int64_t)batch * shape->n_kv_heads * max_ctx, most = (int64_t)5 * kCutBelow * kWgKeys<KVS_BF16>;
     return ((size_t)(all < most / kMaxPieces ? all * kMaxPieces : most) * 4 + 255) / 256 * 256;
 }
 
