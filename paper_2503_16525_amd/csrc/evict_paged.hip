@@ -7,8 +7,8 @@
 //   their keys and count their first digits; parts add these up, set their keys of the one value aside and count the second
 //   digits; a workgroup a request finds the rest among those; a fourth counts what stays of every 256 rows.
 //   The last launch moves: a workgroup for every 256 rows ranks its own behind those before it and copies them.
-// What bounds it: the copy, at most; the keys' passes are a few dependent trips to memory each.  (131072 rows of 4 heads to 65536: keys 5.6 us, first
-// digits 7.9, the rest 9.5, counts 4.7, the copy of 268 MB 56, 4.8 TB/s, 95 with the launches' gaps; 4097 rows to 3584 8.8 and 7.0.)
+// What bounds it: the copy, at most; the keys' passes are a few dependent trips to memory each.  (131072 rows of 4 heads to 65536: keys 4.8 us, first
+// digits 7.5, the rest 6.2, counts 4.7, the copy of 268 MB 56, 4.8 TB/s, 90 with the launches' gaps; 4097 rows to 3584 8.6 and 7.0.)
 #include "paged.h"
 
 namespace kvs {
@@ -17,22 +17,38 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kSub = kThreads;              // rows of a moving workgroup
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / kWave;
-constexpr int kKeysPerThread = 8;
-constexpr int kSmall = kSelThreads * kKeysPerThread;
+constexpr int kMostKeys = 16;                // of a thread
+constexpr int kSmall = kSelThreads * kMostKeys;
 constexpr int kSeg = 2048;                  // rows whose first digits are counted together
 constexpr int kBins = 2048;                 // values of a digit
 constexpr int kPart = 8192;                 // keys that a workgroup looks through
 
 struct Picked { uint32_t key; int32_t want, m, len; };      // the m-th largest key, how many that equal it stay
 
-__device__ __forceinline__ uint32_t key_of(const Paged &pg, int b, int i, int len, int m, int n_first, int n_recent, int n_kv_heads, const float *__restrict__ mass, int64_t mass_stride)
+// Keys of rows i0, i0 + kSelThreads, ..: all rows' masses of a few heads are asked for together, and added in the heads' order.
+template <int N>
+__device__ __forceinline__ void keys_of(uint32_t (&key)[N], const Paged &pg, int b, int i0, int len, int m, int n_first, int n_recent, int n_kv_heads, const float *__restrict__ mass, int64_t mass_stride)
 {
+    constexpr int HEADS = N <= 8 ? 4 : 2;
     const int first = min(n_first, m), recent = min(n_recent, m - first);
-    const float *at = mass + (int64_t)b * n_kv_heads * mass_stride + i;
-    float sum = at[0];
-#pragma unroll 4
-    for (int g = 1; g < n_kv_heads; ++g) sum += at[g * mass_stride];
-    return i < first || i >= len - recent ? 0xffffffffu : sum == sum ? score_key(sum) : 0u;
+    const float *const from = mass + (int64_t)b * n_kv_heads * mass_stride;
+    float sum[N];
+    for (int g0 = 0; g0 < n_kv_heads; g0 += HEADS) {
+        float x[HEADS][N];
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[h][j] = from[min(g0 + h, n_kv_heads - 1) * mass_stride + min((int64_t)i0 + j * kSelThreads, (int64_t)len - 1)];
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum[j] = g0 + h == 0 ? x[h][j] : g0 + h < n_kv_heads ? sum[j] + x[h][j] : sum[j];
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int64_t i = (int64_t)i0 + j * kSelThreads;
+        key[j] = i >= len ? 0u : i < first || i >= len - recent ? 0xffffffffu : sum[j] == sum[j] ? score_key(sum[j]) : 0u;
+    }
 }
 
 __device__ __forceinline__ int kept_of(const int32_t *keep, int max_keep, int b, int len) { return min(len, min(max(keep[b], 0), max_keep)); }
@@ -74,25 +90,28 @@ __device__ __forceinline__ void find_digit(int large, int small, int *sums, int 
     __syncthreads();
 }
 
-// Up to kSmall rows a request: keys, the m-th of them, and what stays of every kSub rows.
+// Up to kSmall rows a request: keys, the m-th of them, and what stays of every kSub rows.  (One load after another a thread and eight keys at the most: 8192 rows
+// 20.7 us with the copy, now 17.8; 16384 rows by four launches 34.8, now 28.6.)
+// KPT: keys of a thread
+template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void evict_small_kernel(const Paged pg, int n_kv_heads, const int32_t *keep, int max_keep, int n_first, int n_recent,
                                                                   const float *__restrict__ mass, int64_t mass_stride, uint32_t *__restrict__ keys, int64_t stride, Picked *__restrict__ picked,
                                                                   int2 *__restrict__ counts, int subs, int32_t *new_len)
 {
     __shared__ int hist[kBins];
     __shared__ int sums[kSelWaves], found[2];
-    __shared__ int above_s[kSmall / kSub], equal_s[kSmall / kSub];
+    __shared__ int above_s[(KPT * kSelThreads) / kSub], equal_s[(KPT * kSelThreads) / kSub];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int len = len_of(pg, b);
     const int m = kept_of(keep, max_keep, b, len);
-    uint32_t key[kKeysPerThread];
+    uint32_t key[KPT] = {};
+    if (len > 0) keys_of(key, pg, b, tid, len, m, n_first, n_recent, n_kv_heads, mass, mass_stride);
 #pragma unroll
-    for (int j = 0; j < kKeysPerThread; ++j) {
+    for (int j = 0; j < KPT; ++j) {
         const int i = tid + j * kSelThreads;
-        key[j] = i < len ? key_of(pg, b, i, len, m, n_first, n_recent, n_kv_heads, mass, mass_stride) : 0u;
         if (i < len) keys[(int64_t)b * stride + i] = key[j];
     }
-    if (tid < kSmall / kSub) above_s[tid] = equal_s[tid] = 0;
+    if (tid < (KPT * kSelThreads) / kSub) above_s[tid] = equal_s[tid] = 0;
     uint32_t prefix = 0;
     int want = m;
 #pragma unroll
@@ -102,7 +121,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_small_kernel(const Paged pg
         hist[tid] = hist[tid + kSelThreads] = 0;
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kKeysPerThread; ++j)
+        for (int j = 0; j < KPT; ++j)
             if (tid + j * kSelThreads < len && (pass == 0 || key[j] >> (pass == 1 ? 21 : 10) == prefix)) atomicAdd(&hist[(key[j] >> shift) & mask], 1);
         __syncthreads();
         uint32_t digit = 0;
@@ -111,7 +130,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_small_kernel(const Paged pg
     }
     if (m == 0) { prefix = 0xffffffffu; want = 0; }
 #pragma unroll
-    for (int j = 0; j < kKeysPerThread; ++j) {
+    for (int j = 0; j < KPT; ++j) {
         const int i = tid + j * kSelThreads;
         const int above = __popcll(__ballot(i < len && key[j] > prefix)), equal = __popcll(__ballot(i < len && key[j] == prefix));
         if (lane == 0) { atomicAdd(&above_s[i / kSub], above); atomicAdd(&equal_s[i / kSub], equal); }
@@ -135,13 +154,14 @@ __global__ __launch_bounds__(kSelThreads) void evict_keys_kernel(const Paged pg,
 #pragma unroll
     for (int j = 0; j < kBins / kSelThreads; ++j) hist[tid + j * kSelThreads] = 0;
     __syncthreads();
+    uint32_t key[kSeg / kSelThreads];
+    keys_of(key, pg, b, lo + tid, len, m, n_first, n_recent, n_kv_heads, mass, mass_stride);
 #pragma unroll
     for (int j = 0; j < kSeg / kSelThreads; ++j) {
         const int64_t i = lo + tid + j * kSelThreads;
         if (i < len) {
-            const uint32_t key = key_of(pg, b, (int)i, len, m, n_first, n_recent, n_kv_heads, mass, mass_stride);
-            keys[(int64_t)b * stride + i] = key;
-            atomicAdd(&hist[key >> 21], 1);
+            keys[(int64_t)b * stride + i] = key[j];
+            atomicAdd(&hist[key[j] >> 21], 1);
         }
     }
     __syncthreads();
@@ -163,6 +183,12 @@ __global__ __launch_bounds__(kSelThreads) void evict_scan_kernel(const Paged pg,
     const int m = kept_of(keep, max_keep, b, len);
     const int64_t lo = (int64_t)part * kPart;
     if (lo >= len || m == 0) return;
+    uint32_t key[kPart / kSelThreads];
+#pragma unroll
+    for (int j = 0; j < kPart / kSelThreads; ++j) {
+        const int64_t i = lo + j * kSelThreads + tid;
+        key[j] = i < len ? keys[(int64_t)b * stride + i] : 0u;
+    }
     const int live = (len + kSeg - 1) / kSeg;
     int large = 0, small = 0;                                // word kBins / 2 - 1 - tid
 #pragma unroll 32
@@ -170,12 +196,6 @@ __global__ __launch_bounds__(kSelThreads) void evict_scan_kernel(const Paged pg,
         const uint32_t w = firsts[((int64_t)b * segs + s) * (kBins / 2) + kBins / 2 - 1 - tid];
         large += (int)(w >> 16);
         small += (int)(w & 0xffffu);
-    }
-    uint32_t key[kPart / kSelThreads];
-#pragma unroll
-    for (int j = 0; j < kPart / kSelThreads; ++j) {
-        const int64_t i = lo + j * kSelThreads + tid;
-        key[j] = i < len ? keys[(int64_t)b * stride + i] : 0u;
     }
     hist[tid] = hist[tid + kSelThreads] = 0;
     if (tid == 0) taken = 0;
@@ -216,6 +236,17 @@ __global__ __launch_bounds__(kSelThreads) void evict_pick_kernel(const Paged pg,
     if (m > 0) {
         const int live = (int)(((int64_t)len + kPart - 1) / kPart);
         const Picked first = picked[b];
+        // a wave a part; the first keys of its first one are asked for before it is known which count
+        constexpr int EARLY = 8;
+        const int wave = tid >> 6, lane = tid & 63;
+        const uint32_t *const from = aside + (int64_t)b * stride;
+        uint32_t early[EARLY];
+        int n_early = 0;
+        if (wave < live) {
+            n_early = n_aside[(int64_t)b * parts + wave];
+#pragma unroll
+            for (int j = 0; j < EARLY; ++j) early[j] = from[min((int64_t)wave * kPart + j * kWave + lane, (int64_t)len - 1)];
+        }
         int large = 0, small = 0;                            // word kBins / 2 - 1 - tid
 #pragma unroll 16
         for (int s = 0; s < live; ++s) {
@@ -229,14 +260,14 @@ __global__ __launch_bounds__(kSelThreads) void evict_pick_kernel(const Paged pg,
         key = first.key << 11 | digit;
         hist[tid] = hist[tid + kSelThreads] = 0;
         __syncthreads();
-        for (int p = tid >> 6; p < live; p += kSelWaves) {   // a wave a part
-            const int n = n_aside[(int64_t)b * parts + p];
-            const uint32_t *from = aside + (int64_t)b * stride + (int64_t)p * kPart;
+        auto count = [&](uint32_t k) { if (k >> 10 == key) atomicAdd(&hist[k & 1023u], 1); };
+#pragma unroll
+        for (int j = 0; j < EARLY; ++j)
+            if (j * kWave + lane < n_early) count(early[j]);
+        for (int p = wave; p < live; p += kSelWaves) {
+            const int n = p == wave ? n_early : n_aside[(int64_t)b * parts + p];
 #pragma unroll 8
-            for (int i = tid & 63; i < n; i += kWave) {
-                const uint32_t k = from[i];
-                if (k >> 10 == key) atomicAdd(&hist[k & 1023u], 1);
-            }
+            for (int i = (p == wave ? EARLY * kWave : 0) + lane; i < n; i += kWave) count(from[(int64_t)p * kPart + i]);
         }
         __syncthreads();
         find_digit(hist[kBins - 1 - 2 * tid], hist[kBins - 2 - 2 * tid], sums, found, digit, want);
@@ -402,8 +433,13 @@ extern "C" kvs_status kvs_evict_paged(const kvs_shape *shape, const kvs_paged_ca
     uint32_t *keys = (uint32_t *)(ws + l.keys), *firsts = (uint32_t *)(ws + l.firsts);
     const dim3 threads(kThreads), requests((unsigned)pg.batch);
     if (!l.segs) {
-        hipLaunchKernelGGL(evict_small_kernel, requests, dim3(kSelThreads), 0, hs, pg, shape->n_kv_heads, keep, (int)max_keep, n_first, n_recent, mass, mass_stride, keys, l.stride, picked,
-                           counts, (int)l.subs, new_len);
+#define KVS_SMALL(KPT)                                                                                                                                          \
+    hipLaunchKernelGGL(evict_small_kernel<KPT>, requests, dim3(kSelThreads), 0, hs, pg, shape->n_kv_heads, keep, (int)max_keep, n_first, n_recent, mass, mass_stride, \
+                       keys, l.stride, picked, counts, (int)l.subs, new_len)
+        if (pg.max_ctx <= 4 * kSelThreads) KVS_SMALL(4);
+        else if (pg.max_ctx <= 8 * kSelThreads) KVS_SMALL(8);
+        else KVS_SMALL(16);
+#undef KVS_SMALL
     } else {
         uint32_t *aside = (uint32_t *)(ws + l.aside), *seconds = (uint32_t *)(ws + l.seconds);
         int32_t *n_aside = (int32_t *)(ws + l.n_aside);

@@ -153,3 +153,15 @@ def test_rows_behind_32_bits():
     for j, i in enumerate(rows):
         p, q = int(table[0, i // 16]), int(to[0, j // 16])
         assert torch.equal(k[q, j % 16], k[p, i % 16]) and torch.equal(v[q, j % 16], v[p, i % 16])
+
+
+@pytest.mark.parametrize("hk,d", [(1, 64), (5, 64)])
+@pytest.mark.parametrize("n", [4096, 4097, 8192, 8193, 16384, 16385])
+def test_contexts_at_the_ends_of_the_selecting_kernels(hk, d, n):
+    _check(hk, hk, d, BF16, 64, [n, n - 1, 7], [700, 333, 5], 3, 100, seed=n + hk)
+
+
+def test_keys_of_many_parts():
+    """More parts than a workgroup has waves, and more keys of one first digit than are asked for early."""
+    _check(1, 1, 64, BF16, 256, [140000], [3000], 4, 50, seed=11)
+    _check(1, 1, 64, BF16, 256, [140000], [2500], 4, 50, seed=12, weigh=lambda m: m.clamp(1.0, 1.2).mul(64).round())
