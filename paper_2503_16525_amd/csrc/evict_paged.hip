@@ -8,7 +8,7 @@
 //   digits; a workgroup a request finds the rest among those; a fourth counts what stays of every 256 rows.
 //   The last launch moves: a workgroup for every 256 rows ranks its own behind those before it and copies them.
 // What bounds it: the copy, at most; the keys' passes are a few dependent trips to memory each.  (131072 rows of 4 heads to 65536: keys 4.8 us, first
-// digits 7.5, the rest 6.2, counts 4.7, the copy of 268 MB 56, 4.8 TB/s, 90 with the launches' gaps; 4097 rows to 3584 8.6 and 7.0.)
+// digits 7.5, the rest 6.2, counts 4.6, the copy of 268 MB 52, 5.1 TB/s, 86 with the launches' gaps; 4097 rows to 3584 8.3 and 7.5.)
 #include "paged.h"
 
 namespace kvs {
@@ -458,8 +458,9 @@ extern "C" kvs_status kvs_evict_paged(const kvs_shape *shape, const kvs_paged_ca
     if (max_keep == 0 || (!new_table && !new_mass && !kept)) return KVS_OK;
     const int ppr = (int)(shape->n_kv_heads * shape->head_dim * (int64_t)elem_bytes(shape->dtype) / 16);
     const int ppl = (ppr + kWave - 1) / kWave;
-    // Short contexts do not fill the chip with a workgroup for every kSub rows: several rank the same rows then, and copy a part each.
-    int64_t parts = 1024 / (l.subs * pg.batch);
+    // Short contexts do not fill the chip with a workgroup for every kSub rows: several rank the same rows then, and copy a part each.  Twice as
+    // many as are there at once let one rank while another copies (131072 rows: 1024 workgroups 78.0 us in all, 2048 74.1, 4096 73.8).
+    int64_t parts = 4096 / (l.subs * pg.batch);
     parts = parts < 1 || !new_table ? 1 : parts > 8 ? 8 : parts;
 #define KVS_MOVE(P, R)                                                                                                                            \
     hipLaunchKernelGGL((evict_move_kernel<P, R>), dim3((unsigned)l.subs, (unsigned)pg.batch, (unsigned)parts), threads, 0, hs, pg, shape->n_kv_heads, ppr, keys, l.stride, picked, counts, (int)l.subs, \
