@@ -13,9 +13,9 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libkvshare_hip.so")
-# the same library with the large-launch attention kernel pinned at compile time: only the test
-# suite loads it, to run that kernel at sizes the oracle can follow (the shipped library has no
-# run-time switch)
+# the same library with the large-launch attention kernel pinned at compile time, and with a switch that sends paged attention
+# to its kernel of many rows: only the test suite loads it, to run those kernels at sizes the oracle can follow
+# (the shipped library has no run-time switch)
 LIB_BIGATTN_PATH = os.path.join(PKG, "libkvshare_hip_bigattn.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -71,14 +71,14 @@ def _link(objs, lib: str, force: bool) -> None:
 def build(force: bool = False, jobs: int = 8) -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
     srcs = sources()
-    pinned = os.path.join(CSRC, "attention_mfma.hip")      # holds the choice between the attention kernels
+    # the files that hold the choices between the attention kernels
+    pinned = {"attention_mfma.hip": "-DKVS_ATTN_FORCE=2", "attention_paged.hip": "-DKVS_PAGED_TEST", "attention_paged_large.hip": "-DKVS_PAGED_TEST"}
     with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as ex:
-        big = ex.submit(_compile, pinned, force, ("-DKVS_ATTN_FORCE=2",), ".bigattn")
+        big = {name: ex.submit(_compile, os.path.join(CSRC, name), force, (define,), ".bigattn") for name, define in pinned.items()}
         objs = list(ex.map(lambda s: _compile(s, force), srcs))
-        big_obj = big.result()
+        big_objs = {os.path.join(OBJ_DIR, name + ".o"): obj.result() for name, obj in big.items()}
     _link(objs, LIB_PATH, force)
-    plain = os.path.join(OBJ_DIR, os.path.basename(pinned) + ".o")
-    _link([big_obj if o == plain else o for o in objs], LIB_BIGATTN_PATH, force)
+    _link([big_objs.get(o, o) for o in objs], LIB_BIGATTN_PATH, force)
     return LIB_PATH
 
 

@@ -49,12 +49,19 @@ __device__ __forceinline__ PagedPlace place_of(uint32_t wg, int units, int piece
 }
 
 // 256 rows a workgroup (attention_paged_large.hip): whether a call can go there, how its keys are cut and about how long that takes.
-struct PagedLargePlan { int32_t pieces, tiles; int64_t units; double us; };
+struct PagedLargePlan { int32_t pieces, tiles; int64_t units; double us; bool dealt; };
 bool attention_paged_takes_large(const kvs_shape *shape, const Paged &pg, const PagedCall &call, float scale, size_t workspace_bytes, PagedLargePlan *plan);
 kvs_status launch_attention_paged_large(const kvs_shape *shape, const kvs_paged_cache *cache, const Paged &pg, const PagedLargePlan &plan, const void *q, float scale,
                                         void *out, float *lse_out, void *workspace, hipStream_t hs);
 size_t attention_paged_large_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t n_new);
 constexpr int kPagedLargeRows = 256;
+// The test suite builds a second library, in which every call that the kernel of many rows can take goes there, its keys in so many pieces
+// (0: as estimated).  The shipped one has no switch.
+#ifdef KVS_PAGED_TEST
+extern int32_t paged_forced_pieces;
+#else
+constexpr int32_t paged_forced_pieces = 0;
+#endif
 // The rows of those of its workgroups that say so once more, with the other kernel (attention_paged.hip); odd: one word a workgroup.
 kvs_status launch_again_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const Paged &pg, const PagedLargePlan &plan, const int32_t *odd, const void *q, float scale,
                               void *out, float *lse_out, hipStream_t hs);

@@ -642,6 +642,17 @@ Plan plan_pieces(const kvs_shape *shape, const Paged &pg, const PagedCall &call,
     return best;
 }
 
+// Which kernel a call goes to: the one that is expected to be faster.
+struct Choice { bool large; Plan plan; PagedLargePlan many; };
+Choice choose(const kvs_shape *shape, const Paged &pg, float scale, size_t workspace_bytes)
+{
+    const PagedCall call = describe(shape, pg);
+    Choice c;
+    c.plan = plan_pieces(shape, pg, call, workspace_bytes);
+    c.large = attention_paged_takes_large(shape, pg, call, scale, workspace_bytes, &c.many) && (c.many.us < c.plan.us || paged_forced_pieces);
+    return c;
+}
+
 template <int DTYPE, int D, int PARTS>
 kvs_status launch(const kvs_shape *shape, const kvs_paged_cache *c, const Paged &pg, int64_t units, const Plan &plan, const void *q, float scale,
                   void *out, float *lse_out, void *workspace, hipStream_t hs)
@@ -784,11 +795,9 @@ extern "C" kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_page
         return fail(KVS_EINVAL, "%s: lse_out overlaps q_new or out", me);
     hipStream_t hs = (hipStream_t)stream;
     const int grp = shape->n_q_heads / shape->n_kv_heads;
-    const PagedCall call = describe(shape, pg);
-    const Plan plan = plan_pieces(shape, pg, call, workspace_bytes);
-    PagedLargePlan large;
-    if (attention_paged_takes_large(shape, pg, call, scale, workspace_bytes, &large) && large.us < plan.us)
-        return launch_attention_paged_large(shape, cache, pg, large, q_new, scale, out, lse_out, workspace, hs);
+    const Choice choice = choose(shape, pg, scale, workspace_bytes);
+    if (choice.large) return launch_attention_paged_large(shape, cache, pg, choice.many, q_new, scale, out, lse_out, workspace, hs);
+    const Plan &plan = choice.plan;
     const int64_t units = most_blocks(pg, grp, kRows);
     if (units * plan.pieces * shape->n_kv_heads > kMostWgs || (int64_t)pg.n_new * shape->n_q_heads * (plan.pieces > 1 ? 4 : 0) > kMostWgs)
         return fail(KVS_EINVAL, "%s: too many rows in one call", me);
@@ -802,3 +811,25 @@ extern "C" kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_page
     return wide ? KVS_AP(KVS_BF16, 128, 1) : KVS_AP(KVS_BF16, 64, 1);
 #undef KVS_AP
 }
+
+#ifdef KVS_PAGED_TEST
+namespace kvs { int32_t paged_forced_pieces = 0; }
+
+extern "C" KVS_API void kvs_test_force_pieces(int32_t pieces) { kvs::paged_forced_pieces = pieces; }
+
+// What a call would do, without one (no tensor is read): whether it goes to the kernel of many rows, into how many pieces its keys are cut, whether
+// row tiles are dealt there.
+extern "C" KVS_API kvs_status kvs_test_choice(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages, const int32_t *cu_new, const int32_t *sel_pos,
+                                              int64_t n_new, float scale, int32_t window, int32_t n_first, size_t workspace_bytes, int32_t *taken)
+{
+    using namespace kvs;
+    Paged pg;
+    kvs_status st = check_paged("kvs_test_choice", shape, cache, pages, &pg);
+    if (st != KVS_OK || (st = check_new_tokens("kvs_test_choice", shape, pages, cu_new, sel_pos, n_new, window, n_first, &pg)) != KVS_OK) return st;
+    const Choice c = choose(shape, pg, scale, workspace_bytes);
+    taken[0] = c.large;
+    taken[1] = c.large ? c.many.pieces : c.plan.pieces;
+    taken[2] = c.large && c.many.dealt;
+    return KVS_OK;
+}
+#endif

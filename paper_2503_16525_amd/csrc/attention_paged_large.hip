@@ -538,7 +538,7 @@ bool attention_paged_takes_large(const kvs_shape *shape, const Paged &pg, const 
     plan->us = 1e30;
     for (int64_t p = 1; p <= kMostPieces && (p == 1 || (fits(p) && wgs * p <= kMostCutWgs)); ++p) {
         const int64_t each = (tiles + p - 1) / p;
-        if (each > kMostTiles) continue;
+        if (each > kMostTiles || (paged_forced_pieces && p != paged_forced_pieces)) continue;
         if (p > 1 && each < kLeastTiles) break;
         // Rounds of one workgroup a compute unit: 0.90 us a tile and 6 to begin and end; 3 for the last launch; a merge.  (us, estimate and
         // measured: 256 tokens of 32 heads over 16384 keys in one piece 471, 437; eight 91, 93; ten 139, 134; 500 of 28 heads over 12000 in four 115, 113.)
@@ -551,6 +551,8 @@ bool attention_paged_takes_large(const kvs_shape *shape, const Paged &pg, const 
     if (plan->us == 1e30 || units * plan->pieces * shape->n_kv_heads > kMostWgs) return false;
     plan->tiles = (int32_t)((tiles + plan->pieces - 1) / plan->pieces);
     plan->units = units;
+    // (The rows of one request: of several, whose contexts differ, every tile finds its place as one becomes free.)
+    plan->dealt = plan->pieces == 1 && pg.batch == 1 && units * shape->n_kv_heads > 256 && 256 % shape->n_kv_heads == 0;
     return true;
 }
 
@@ -573,13 +575,11 @@ kvs_status launch_attention_paged_large(const kvs_shape *shape, const kvs_paged_
     int32_t *const odd = (int32_t *)workspace;
     const PagedParts parts = paged_parts((char *)workspace + odd_bytes(wgs), (int64_t)pg.n_new * shape->n_q_heads * plan.pieces);
     const int lds = PLACES_AT + (8 * plan.tiles + 15) / 16 * 16;
-    // (The rows of one request: of several, whose contexts differ, every tile finds its place as one becomes free.)
-    const bool dealt = plan.pieces == 1 && pg.batch == 1 && wgs > 256 && 256 % shape->n_kv_heads == 0;
 #define KVS_LARGE(DEAL, N)                                                                                                                                      \
     hipLaunchKernelGGL(attention_paged_large_kernel<DEAL>, dim3((unsigned)(N)), dim3(NT), lds, hs, pg, shape->n_q_heads, shape->n_kv_heads, (int)plan.units,    \
                        plan.pieces, plan.tiles < kLeastTiles ? plan.tiles : kLeastTiles, (const char *)cache->k, (const char *)cache->v, (const uint16_t *)q,   \
                        scale * 1.4426950408889634f, (uint16_t *)out, lse_out, parts.o, parts.ml, odd)
-    if (dealt) KVS_LARGE(true, 256);
+    if (plan.dealt) KVS_LARGE(true, 256);
     else KVS_LARGE(false, wgs);
 #undef KVS_LARGE
     if ((st = check_launch("kvs_attention_paged")) != KVS_OK) return st;
