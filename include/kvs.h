@@ -601,7 +601,7 @@ KVS_API kvs_status kvs_store_paged(const kvs_shape *shape, const kvs_paged_cache
  *            call has ended on its stream.
  * bf16: fp32 accumulation and softmax; the weights enter the second product as two bf16 numbers that hold 16 of their bits where
  * there are no more than 32 rows (tokens times query heads of a KV head) a request on average, rounded to one elsewhere.  fp32
- * throughout otherwise.  Sums of values beyond 2^110 may become infinite.  Equal calls give equal bits.
+ * throughout otherwise.  Sums of values beyond 2^110 may become infinite, values below 2^-100 may lose bits.  Equal calls give equal bits.
  */
 KVS_API kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages,
                                        const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new, const void *q_new, float scale,

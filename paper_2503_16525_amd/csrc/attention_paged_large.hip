@@ -11,10 +11,12 @@
 // K and V go straight into LDS, rings of four and eight tiles; a tile is asked for four steps ahead, and the one barrier of a
 // step is where each wave waits for its own loads of the tile after next.
 //
-// The softmax's reference is taken from a row's first tile, raised by 60 so that sums stay far from both ends of the exponents, and
-// moves, to 30 above the tile's largest score, only where a sum passes 2^64: then the tile's weights, which have not met V yet, are made again, and sums and
-// accumulators come down with it.  A row that has seen nothing yet has the lowest reference and a sum of 0, so that its first
-// score moves it.
+// The softmax's reference is the largest score of a row's first tile, and moves only where a sum passes 2^64, to 3 above the tile's largest score or by 66 if
+// that is more: then the tile's weights, which have not met V yet, are made again, and sums and accumulators come down with it.  So a row's largest
+// weight is never far below 1: products with a V down to 2^-100 keep their bits, and of two pieces whose references are so far apart that the merge gives one of them
+// nothing, that one had nothing to give (at 2^-58 of the other's weight).  Raised above the first scores by 60, as weights would allow, neither held: V
+// of 2^-70 lost bits, V of 2^-90 was 0, and pieces with a quarter of another's weight were lost.  A row that has seen nothing yet has the lowest reference and a sum
+// of 0, so that its first score moves it.
 //
 // A weight of 0 does not hide a V that is infinite or NaN.  A workgroup whose sums are no numbers, or that met an entry of the table
 // that names no page, says so, and a last launch does its rows once more with the kernel of attention_paged.hip, which
@@ -49,7 +51,6 @@ constexpr int PLACES_AT = RING_B + 48;
 constexpr int kMostTiles = 6144;       // of a piece: 48 KB of places
 constexpr int kLeastTiles = 8;         // of a piece
 constexpr int kMostPieces = 32, kMostCutWgs = 512;
-constexpr float kRefShift = 60.0f;
 constexpr float kSumLimit = 1.8446744e19f;   // 2^64
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4_t v) { return __builtin_bit_cast(bf16x8, v); }
@@ -322,9 +323,10 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
             floatx16 &m = s[nb];
             const float other = __shfl_xor(l_run[nb], 32);
             const bool move = l_run[nb] >= kSumLimit || other >= kSumLimit;
-            // (30 and 80, so that a sum of up to 2^64 comes down by no more than 2^126, where the exponential would make it 0, unless
-            // it is below 2^-32 of the tile's largest weight.  A sum can also pass 2^64 by a weight of little more than nothing.)
-            const float to = move ? fmaxf(row_max(m) + 30.f, m_ref[nb] + 80.f) : m_ref[nb];
+            // (A sum of up to 2^64 that comes down by more than 2^126, where the exponential makes it 0, is below 2^-59 of the tile's largest
+            // weight.  A sum can also pass 2^64 by a weight of little more than nothing.  0 and 64 would do as well: 2048 tokens over 32768 keys 1016 us
+            // for 985, by how the compiler orders the whole kernel.)
+            const float to = move ? fmaxf(row_max(m) + 3.f, m_ref[nb] + 66.f) : m_ref[nb];
             const float down = move ? __builtin_amdgcn_exp2f(m_ref[nb] - to) : 1.f;
             m_ref[nb] = to;
             l_run[nb] = l_before[nb] * down;
@@ -425,7 +427,7 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const float top = row_max(s_cur[nb]);
-            m_ref[nb] = top > kLowest ? top + kRefShift : kLowest;       // (NaN: the lowest, and the weights say so)
+            m_ref[nb] = top > kLowest ? top : kLowest;       // (NaN: the lowest, and the weights say so)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s_cur[nb][r] = begin < t_lo ? -INFINITY : s_cur[nb][r];
         }

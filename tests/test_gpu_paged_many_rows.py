@@ -129,6 +129,49 @@ def test_a_reference_that_moves_keeps_what_came_before(plateau, pieces):
         _run(c, pieces, f"a plateau of {plateau}, then {rise} more")
 
 
+@pytest.mark.parametrize("first,second", [(60, 63), (63, 67), (63, 130), (120, 124), (123, 126), (123, 127), (123, 130), (123, 133), (200, 203), (127, 123)])
+def test_pieces_whose_first_tiles_lie_far_apart(first, second):
+    """Two pieces.  The first one's scores begin at 0 and rise to `first` powers of two in one key; the second one's begin with a tile of
+    one key at `second`: each counts by its largest score, wherever its reference stands."""
+    n, half = 1100, 576                                      # 18 tiles of 32 keys each
+
+    def change(y, b, is_v):
+        if is_v:
+            y = y.abs() + 1                                  # V of one sign, times 8 where the scores are lower
+            y[200] *= 8
+            return y
+        level = torch.zeros((n,))
+        level[200], level[half + 3] = first, second
+        k = torch.zeros_like(y)
+        k[:, 0, 0], k[:, 0, 1] = (level / 64).floor(), level % 64
+        return k
+    c = R.Case(4, 1, 128, BF16, 16, [(n, 20)], seed=8, change=change, scale=0.6931471805599453)
+    c.q[:] = 0
+    c.q[:, :, 0], c.q[:, :, 1] = 64, 1
+    _run(c, 2, f"{first} beside {second}")
+
+
+@pytest.mark.parametrize("pieces", [0, 1, 3])
+@pytest.mark.parametrize("power", [-100, -90, -70, 60, 100])
+def test_small_and_large_values(power, pieces):
+    """V of a magnitude far from 1, by this kernel and (0 pieces) by the one that takes such a call otherwise: what comes out is as near as ever, relative to
+    what goes in (compared after a multiplication by the power of two, so that no absolute floor helps)."""
+    def level(y, b, is_v):
+        if is_v:
+            return y * 2.0 ** power
+        y = y.clone()
+        y[100:700] *= 6.0                                    # references that move, in some rows often
+        return y
+    for scale, change in ((None, lambda y, b, is_v: y * 2.0 ** power if is_v else y), (1.0, level)):
+        c = R.Case(8, 2, 128, BF16, 16, [(900, 300), (40, 40)], seed=power % 17, change=change, scale=scale)
+        out, lse, mag, dots = R.attention(c)
+        with M.forced(pieces) as lib:
+            if pieces:
+                _there(lib, c, pieces, False)
+            got, got_lse = _attend(c)
+        R.check_attention(c, got.double() * 2.0 ** -power, got_lse, (out * 2.0 ** -power, lse, mag * 2.0 ** -power, dots), 1, f"V of 2^{power}")
+
+
 @pytest.mark.parametrize("window,n_first,pieces", [(0, 0, 1), (0, 0, 3), (48, 33, 1), (89, 33, 1)])
 def test_what_a_row_does_not_see_does_not_reach_it(window, n_first, pieces):
     odd = [33, 40, 41, 64, 95, 96, 500, 511, 512, 700]
