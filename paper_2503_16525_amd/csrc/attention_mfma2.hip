@@ -72,6 +72,7 @@ constexpr int V_RING = 8;                    // >= AHEAD + 2
 static_assert(K_RING >= AHEAD && V_RING >= AHEAD + 2, "ring depth");
 constexpr int LDS_BYTES = (K_RING + V_RING) * TILE_B;
 constexpr float kRefShift = 60.0f;      // base-2 offset of the fixed softmax reference above the first tile's maximum
+constexpr float kMoveShift = 30.0f;     // and of one that moves (RECENTRE) above the tile's
 constexpr float kSumLimit = 1.8446744e19f;   // 2^64: a sum of weights beyond it moves the reference (RECENTRE)
 constexpr float kFarRef = 65536.0f;          // references below it move by `up` to within 2^-8, and fp32 products up to it are that good
 constexpr float kLeastSum = 5.421011e-20f;   // 2^-64: less than any row's sum whose references stayed within kFarRef
@@ -597,7 +598,8 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
 
     // RECENTRE: the reference moves where a row's sum outgrows it.  Looked at after every tile, before the tile's weights are
     // multiplied with V: the row's reference goes up by a whole number (at least 100, and past the tile's largest logit by
-    // kRefShift), its sum without the tile and its accumulators come down by that power of two, and the tile's weights
+    // kMoveShift, so that a sum of up to 2^64 comes down by more than 2^126, where the exponential makes it 0, only if it is below
+    // 2^-32 of the tile's largest weight; by kRefShift it was up to a quarter of what the row has), its sum without the tile and its accumulators come down by that power of two, and the tile's weights
     // are computed again, from scores that are still there.  (A NaN moves nothing.)  References beyond kFarRef are not to be
     // trusted: adding `up` to them, or to one that far off, loses what it adds.  Their workgroups end in the exact maxima's pass.
     auto outgrown = [&](int first) __attribute__((always_inline)) -> bool {
@@ -625,7 +627,7 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
 #pragma unroll
             for (int r = 0; r < 16; ++r) m[r] = jt * BN + 16 * (r >> 3) + 8 * hf + (r & 7) > pos[nb] ? -INFINITY : m[r];
             const float other = __shfl_xor(l_run[nb], 32);
-            const float up = !(l_run[nb] >= kSumLimit || other >= kSumLimit) ? 0.f : fmaxf(ceilf(row_max(m, f) + kRefShift - m_ref[nb]), 100.f);
+            const float up = !(l_run[nb] >= kSumLimit || other >= kSumLimit) ? 0.f : fmaxf(ceilf(row_max(m, f) + kMoveShift - m_ref[nb]), 100.f);
             const float down = __builtin_amdgcn_exp2f(-up);
             m_ref[nb] += up;
             l_run[nb] = l_before[nb] * down;
