@@ -74,6 +74,7 @@ constexpr int LDS_BYTES = (K_RING + V_RING) * TILE_B;
 constexpr float kRefShift = 60.0f;      // base-2 offset of the fixed softmax reference above the first tile's maximum
 constexpr float kMoveShift = 30.0f;     // and of one that moves (RECENTRE) above the tile's
 constexpr float kSumLimit = 1.8446744e19f;   // 2^64: a sum of weights beyond it moves the reference (RECENTRE)
+constexpr float kGrownSum = 0x1p40f;
 constexpr float kFarRef = 65536.0f;          // references below it move by `up` to within 2^-8, and fp32 products up to it are that good
 constexpr float kLeastSum = 5.421011e-20f;   // 2^-64: less than any row's sum whose references stayed within kFarRef
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4_t v) { return __builtin_bit_cast(bf16x8, v); }
@@ -889,6 +890,23 @@ __global__ __launch_bounds__(NT, 1) void attn_mfma2_kernel(
     }
 
     // ---- epilogue: normalise, convert, store ----------------------------------------------------------
+    // A piece's reference is its first tile's largest logit, raised, and its sum may be up to 2^100.  The merge goes by the references: a sum that
+    // has grown past 2^40 is brought down by 2^80, its reference goes up by as much, and then a piece whose reference is so far below
+    // another's that its weight is 0 had less than 2^-26 of the row.  (Seldom: logits 70 above the first tile's, in natural units.)
+    if (SPLIT && __builtin_amdgcn_ballot_w64(fmaxf(l_tot[0], l_tot[1]) > kGrownSum) != 0) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const bool grown = l_tot[nb] > kGrownSum;
+            const float down = grown ? 0x1p-80f : 1.f;
+            m_ref[nb] += grown ? 80.f : 0.f;
+            l_tot[nb] *= down;
+            l_exact[nb] *= down;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o_acc[db][nb][r] *= down;
+        }
+    }
     if (SPLIT) __syncthreads();   // the rows leave through LDS, where (after the second pass) other waves may still be reading their last tile
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {

@@ -52,3 +52,19 @@ def test_a_reference_that_moves_keeps_what_came_before(rise):
     v = torch.randn((n, 8, 128), generator=gen, device=DEV).abs() + 1
     v[1100] = -v[1100]
     _run(64, 8, n, torch.arange(n - k * 30, n, 30, device=DEV, dtype=torch.int32), level, v, rise)
+
+
+@pytest.mark.parametrize("hq,hk,n,k", [(32, 8, 8192, 738), (28, 4, 12000, 481), (32, 8, 3000, 200)])
+@pytest.mark.parametrize("first,others", [(150, 130), (150, 125), (99, 60), (140, 128), (60, 190), (105, 20)])
+def test_pieces_whose_first_tiles_lie_far_apart(hq, hk, n, k, first, others):
+    """Launches that are cut into pieces: the first piece's logits begin at 0 and rise to `first` in one key, those of the context's second half
+    are all `others`.  Each piece counts by what it holds, wherever its reference stands."""
+    print(f"{k} of {n} on {hq}:{hk}, {first} beside {others}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(first)
+    level = torch.zeros((n,), device=DEV)
+    level[100], level[n // 2:] = first, others
+    v = torch.randn((n, hk, 128), generator=gen, device=DEV).abs() + 1
+    v[100] = -v[100]
+    pos = (torch.arange(k, device=DEV) * n // k).int()
+    _run(hq, hk, n, pos, level, v, first)
+    _run(hq, hk, n, pos, level, v, first, workspace=False)
