@@ -541,7 +541,7 @@ KVS_API kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8 *c
  * The page table and the lengths are read on the device, when the kernels run: a captured call can be replayed after they have
  * changed.  max_ctx is what the host promises about them: no context is longer.  Launches are sized by it, so it should not be
  * far above; of a longer context the first max_ctx rows are taken, and of one longer than the table is wide what the table
- * names.  A negative length is 0.  An entry of the table outside [0, n_pages) names no page: its rows are not stored to, seen or
+ * names (its last tokens then stand behind those: they overwrite no row, and see what the last one taken sees).  A negative length is 0.  An entry of the table outside [0, n_pages) names no page: its rows are not stored to, seen or
  * copied.  Entries behind a context's last page are not used.
  *
  * Tokens of a call belong to the requests in order: those of request b are [cu_new[b], cu_new[b+1]) (device memory, at

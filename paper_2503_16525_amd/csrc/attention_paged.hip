@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kThreads, DTYPE == KVS_F32 && D == 128 ? 1 : 2) voi
         if (!find_block<kRows>(pg, grp, unit, found)) return;
     }
     const int b = __builtin_amdgcn_readfirstlane(found.b), blk = __builtin_amdgcn_readfirstlane(found.blk), tok0 = __builtin_amdgcn_readfirstlane(found.tok0);
-    const int n_tok = __builtin_amdgcn_readfirstlane(found.n_tok), len = __builtin_amdgcn_readfirstlane(found.len);
+    const int n_tok = __builtin_amdgcn_readfirstlane(found.n_tok), len = __builtin_amdgcn_readfirstlane(found.len), end = __builtin_amdgcn_readfirstlane(found.end);
     const int rows = n_tok * grp;
 
     // Without a window the first piece's tiles do not depend on the length, and their places are asked for beside it.
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(kThreads, DTYPE == KVS_F32 && D == 128 ? 1 : 2) voi
     // ---- this lane's row (both half-waves hold the same 32) ------------------------------------------------
     const int rq = min(max(row0 + ln, 0), rows - 1);
     const int t_own = rq / grp, hh = rq - t_own * grp;
-    const int pos = position_of(pg, tok0, n_tok, t_own, len);
+    const int pos = position_of(pg, tok0, n_tok, t_own, len, end);
     int pmin = pos, pmax = pos, plow = pos < 0 ? 0x7fffffff : pos;        // plow: of those that see anything
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
         return;
     }
     const int b = __builtin_amdgcn_readfirstlane(mine.b), blk = __builtin_amdgcn_readfirstlane(mine.blk), tok0 = __builtin_amdgcn_readfirstlane(mine.tok0);
-    const int n_tok = __builtin_amdgcn_readfirstlane(mine.n_tok), len = __builtin_amdgcn_readfirstlane(mine.len);
+    const int n_tok = __builtin_amdgcn_readfirstlane(mine.n_tok), len = __builtin_amdgcn_readfirstlane(mine.len), end = __builtin_amdgcn_readfirstlane(mine.end);
     const int rows = n_tok * grp;
     // Row tiles end with their request's rows: the one partly filled is the first, whose rows see least.
     const int row0 = blk * ROWS - ((rows + ROWS - 1) / ROWS * ROWS - rows);
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(NT, 1) void attention_paged_large_kernel(
         const int rq = row0 + block_row(nb) + ln;
         row_ok[nb] = rq >= 0;
         const int t = max(rq, 0) / grp;
-        pos[nb] = position_of(pg, tok0, n_tok, t, len);
+        pos[nb] = position_of(pg, tok0, n_tok, t, len, end);
         row_idx[nb] = (int64_t)(tok0 + t) * n_q_heads + g * grp + (max(rq, 0) - t * grp);
         pmin = min(pmin, pos[nb]);
         pmax = max(pmax, pos[nb]);

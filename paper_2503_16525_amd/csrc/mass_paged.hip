@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
     const int kb = rest % key_blocks;
     rest /= key_blocks;
     const int piece = rest % pieces, b = rest / pieces;
-    const int len = len_of(pg, b);
+    const int end = end_of(pg, b), len = min(end, pg.max_ctx);
     const int wg_lo = kb * kWgKeys<DTYPE>;
     if (wg_lo >= len) return;
     const int my_lo = wg_lo + wave * NB * 32, my_hi = min(my_lo + NB * 32, len) - 1;   // the wave's keys
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_paged_kernel(
         lse_next = 0.f;
         if (info.t < n_tok) {
             lse_next = lse[(int64_t)(tok0 + info.t) * n_q_heads + g * grp + info.h] * 1.4426950408889634f;
-            pos_next = position_of(pg, tok0, n_tok, info.t, len);
+            pos_next = position_of(pg, tok0, n_tok, info.t, len, end);
             if (lse_next == -INFINITY) pos_next = -1;        // saw nothing
         }
         info.t += info_dt;
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_few_kernel(
     const int g = (int)(blockIdx.x % (uint32_t)n_kv_heads);
     const int rest = (int)(blockIdx.x / (uint32_t)n_kv_heads);
     const int b = rest % pg.batch, piece = rest / pg.batch;
-    const int len = len_of(pg, b);
+    const int end = end_of(pg, b), len = min(end, pg.max_ctx);
     const int tiles = (len + 31) / 32;
     const int p_lo = (int)min((int64_t)piece * piece_tiles, (int64_t)tiles), p_hi = (int)min((int64_t)p_lo + piece_tiles, (int64_t)tiles);
     if (p_lo >= p_hi) return;
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_few_kernel(
         for (int c = 0; c < NS; ++c) qreg[c] = u32x4_t{0u, 0u, 0u, 0u};
         if (rows) {
             const int64_t row = (int64_t)(tok0 + t_own) * n_q_heads + g * grp + h_own;
-            pos = rq < rows ? position_of(pg, tok0, n_tok, t_own, len) : -1;
+            pos = rq < rows ? position_of(pg, tok0, n_tok, t_own, len, end) : -1;
             lse2 = lse[row] * 1.4426950408889634f;
             if (lse2 == -INFINITY) pos = -1;                 // saw nothing
 #pragma unroll

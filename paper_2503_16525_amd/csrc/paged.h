@@ -29,7 +29,8 @@ size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, in
 size_t mass_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new);
 size_t evict_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx);
 
-__device__ __forceinline__ int len_of(const Paged &pg, int b) { return min(max(pg.ctx_len[b], 0), pg.max_ctx); }
+__device__ __forceinline__ int end_of(const Paged &pg, int b) { return max(pg.ctx_len[b], 0); }        // where new tokens end
+__device__ __forceinline__ int len_of(const Paged &pg, int b) { return min(end_of(pg, b), pg.max_ctx); } // rows that are taken
 
 // The tokens of request b: [lo, lo + n) of the call's.
 __device__ __forceinline__ void tokens_of(const Paged &pg, int b, int &lo, int &n)
@@ -39,10 +40,11 @@ __device__ __forceinline__ void tokens_of(const Paged &pg, int b, int &lo, int &
     n = min(max(pg.cu_new[b + 1], lo), pg.n_new) - lo;
 }
 
-// Position of token i of a request's n, -1 where it sees nothing, at most the context's last.
-__device__ __forceinline__ int position_of(const Paged &pg, int lo, int n, int i, int len)
+// Position of token i of a request's n, -1 where it sees nothing, at most the last that is taken.  (Of a context that is longer than was
+// promised the last tokens stand behind that, not in the place of rows that are there.)
+__device__ __forceinline__ int position_of(const Paged &pg, int lo, int n, int i, int len, int end)
 {
-    const int p = pg.sel_pos ? pg.sel_pos[lo + i] : len - n + i;
+    const int p = pg.sel_pos ? pg.sel_pos[lo + i] : end - n + i;
     return p < 0 ? -1 : min(p, len - 1);
 }
 
@@ -56,24 +58,25 @@ __device__ __forceinline__ int granule_of(const Paged &pg, int b, int gi)
 }
 
 // A call's rows (tokens times the query heads that share a KV head) in blocks of R rows, none of which holds two requests: which request
-// block u belongs to, which of its blocks it is, the request's tokens [tok0, tok0 + n_tok) and context length.  All lanes of a wave ask
+// block u belongs to, which of its blocks it is, the request's tokens [tok0, tok0 + n_tok), context length and end.  All lanes of a wave ask
 // for the same block; 64 requests a step, whose offsets and lengths come in one trip to memory.
-struct Block { int b, blk, tok0, n_tok, len; };
+struct Block { int b, blk, tok0, n_tok, len, end; };
 template <int R>
 __device__ __forceinline__ bool find_block(const Paged &pg, int grp, int u, Block &out)
 {
     if (!pg.cu_new) {
         const int per = (grp + R - 1) / R, b = u / per;
         if (b >= pg.batch) return false;
-        out = {b, u - b * per, b, 1, len_of(pg, b)};
+        const int end = end_of(pg, b);
+        out = {b, u - b * per, b, 1, min(end, pg.max_ctx), end};
         return true;
     }
     const int lane = threadIdx.x & 63;
     int base = 0;
     for (int b0 = 0; b0 < pg.batch; b0 += 64) {
-        int lo = 0, n = 0, len = 0;
+        int lo = 0, n = 0, end = 0;
         if (b0 + lane < pg.batch) {
-            len = len_of(pg, b0 + lane);
+            end = end_of(pg, b0 + lane);
             tokens_of(pg, b0 + lane, lo, n);
         }
         const int mine = (n * grp + R - 1) / R;
@@ -86,7 +89,8 @@ __device__ __forceinline__ bool find_block(const Paged &pg, int grp, int u, Bloc
         const unsigned long long past = __ballot(base + upto > u);
         if (past) {
             const int at = __ffsll((long long)past) - 1;
-            out = {b0 + at, u - base - __builtin_amdgcn_readlane(upto - mine, at), __builtin_amdgcn_readlane(lo, at), __builtin_amdgcn_readlane(n, at), __builtin_amdgcn_readlane(len, at)};
+            end = __builtin_amdgcn_readlane(end, at);
+            out = {b0 + at, u - base - __builtin_amdgcn_readlane(upto - mine, at), __builtin_amdgcn_readlane(lo, at), __builtin_amdgcn_readlane(n, at), min(end, pg.max_ctx), end};
             return true;
         }
         base += __builtin_amdgcn_readlane(upto, 63);

@@ -53,8 +53,8 @@ __global__ __launch_bounds__(kThreads) void store_paged_kernel(const Paged pg, i
         int lo, n;
         tokens_of(pg, b, lo, n);
         if (s < lo || s >= lo + n) continue;                   // a token of no request
-        const int len = len_of(pg, b);
-        const int p = pg.sel_pos ? pg.sel_pos[s] : len - n + (s - lo);
+        const int end = end_of(pg, b), len = min(end, pg.max_ctx);
+        const int p = pg.sel_pos ? pg.sel_pos[s] : end - n + (s - lo);
         if (p < 0 || p >= len) continue;
         if (pg.sel_pos && s + 1 < lo + n && pg.sel_pos[s + 1] == p) continue;      // the last one counts
         const int at = granule_of(pg, b, p / kGranule);
