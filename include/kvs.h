@@ -574,9 +574,9 @@ typedef struct {
  * tokens of a request have the same position the last one counts (an ascending list may repeat itself); the same position further
  * apart, and one row of the pool reached through two requests, are a race.
  *
- * k_new, v_new [dev] [n_new, n_kv_heads, head_dim]
+ * k_new, v_new [dev] [n_new, n_kv_heads, head_dim], not in the cache
  * mass         [dev] fp32 [batch, n_kv_heads, mass_stride] or NULL: set to 0 at the positions stored to (kvs_mass_paged;
- *              mass_stride at least max_ctx)
+ *              mass_stride at least max_ctx).  No overlap
  */
 KVS_API kvs_status kvs_store_paged(const kvs_shape *shape, const kvs_paged_cache *cache, const kvs_page_table *pages,
                                    const int32_t *cu_new, const int32_t *sel_pos, int64_t n_new,

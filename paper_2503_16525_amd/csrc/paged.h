@@ -3,6 +3,8 @@
 
 #include "kvs_internal.h"
 
+#include <initializer_list>
+
 namespace kvs {
 
 // A call's requests as its kernels see them.  Lengths, offsets, positions and page ids come from device memory and are not
@@ -25,6 +27,16 @@ inline bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes
 {
     return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }
+// What a call writes may lie over nothing that it reads.  (NULL and nothing overlap nothing.)
+struct Span { const void *at; size_t bytes; const char *name; };
+inline kvs_status check_apart(const char *me, std::initializer_list<Span> written, std::initializer_list<Span> read)
+{
+    for (const Span &w : written)
+        for (const Span &r : read)
+            if (w.at && r.at && w.bytes && r.bytes && overlap(w.at, w.bytes, r.at, r.bytes)) return fail(KVS_EINVAL, "%s: %s overlaps %s", me, w.name, r.name);
+    return KVS_OK;
+}
+inline size_t pool_bytes(const kvs_shape *shape, const kvs_paged_cache *c) { return (size_t)c->n_pages * c->page * shape->n_kv_heads * shape->head_dim * elem_bytes(shape->dtype); }
 size_t attention_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new);
 size_t mass_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx, int64_t n_new);
 size_t evict_paged_workspace_bytes(const kvs_shape *shape, int32_t batch, int64_t max_ctx);

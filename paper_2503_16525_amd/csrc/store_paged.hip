@@ -89,6 +89,13 @@ extern "C" kvs_status kvs_store_paged(const kvs_shape *shape, const kvs_paged_ca
     if (n_new == 0 || pages->batch == 0) return KVS_OK;
     if (!k_new || !v_new) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
     if (!aligned16(k_new) || !aligned16(v_new)) return fail(KVS_EINVAL, "%s: K/V pointers must be 16-byte aligned", me);
+    const size_t pool = pool_bytes(shape, cache), rows = (size_t)n_new * shape->n_kv_heads * shape->head_dim * elem_bytes(shape->dtype), batch = (size_t)pages->batch;
+    const size_t masses = batch * shape->n_kv_heads * (size_t)mass_stride * sizeof(float);
+    st = check_apart(me, {{cache->k, pool, "the cache's K"}, {cache->v, pool, "the cache's V"}, {mass, masses, "mass"}},
+                     {{k_new, rows, "k_new"}, {v_new, rows, "v_new"}, {pages->table, batch * pages->width * 4, "the page table"}, {pages->ctx_len, batch * 4, "ctx_len"},
+                      {cu_new, (batch + 1) * 4, "cu_new"}, {sel_pos, (size_t)n_new * 4, "sel_pos"}});
+    if (st == KVS_OK) st = check_apart(me, {{mass, masses, "mass"}}, {{cache->k, pool, "the cache's K"}, {cache->v, pool, "the cache's V"}});
+    if (st != KVS_OK) return st;
     const int ppr = (int)(shape->n_kv_heads * shape->head_dim * (int64_t)elem_bytes(shape->dtype) / 16);
     const int ppl = (ppr + kWave - 1) / kWave;
 #define KVS_STORE(P, R)                                                                                                                       \
