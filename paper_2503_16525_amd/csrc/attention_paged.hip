@@ -793,6 +793,11 @@ extern "C" kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_page
     if (overlap(q_new, bytes, out, bytes)) return fail(KVS_EINVAL, "%s: out overlaps q_new", me);
     if (lse_out && (overlap(lse_out, heads * sizeof(float), q_new, bytes) || overlap(lse_out, heads * sizeof(float), out, bytes)))
         return fail(KVS_EINVAL, "%s: lse_out overlaps q_new or out", me);
+    const size_t pool = pool_bytes(shape, cache), batch = (size_t)pages->batch;
+    st = check_apart(me, {{out, bytes, "out"}, {lse_out, heads * sizeof(float), "lse_out"}},
+                     {{cache->k, pool, "the cache's K"}, {cache->v, pool, "the cache's V"}, {pages->table, batch * pages->width * 4, "the page table"}, {pages->ctx_len, batch * 4, "ctx_len"},
+                      {cu_new, (batch + 1) * 4, "cu_new"}, {sel_pos, (size_t)n_new * 4, "sel_pos"}});
+    if (st != KVS_OK) return st;
     hipStream_t hs = (hipStream_t)stream;
     const int grp = shape->n_q_heads / shape->n_kv_heads;
     const Choice choice = choose(shape, pg, scale, workspace_bytes);

@@ -51,3 +51,13 @@ def test_store(lib, written, read):
 @pytest.mark.parametrize("pool", ["k", "v"])
 def test_store_mass_in_the_cache(lib, pool):
     _refused(lib, "store", pool, "mass")
+
+
+@pytest.mark.parametrize("read", ["q", "k", "v", "table", "ctx_len", "cu_new", "sel_pos"])
+@pytest.mark.parametrize("written", ["out", "lse_out"])
+def test_attention(lib, written, read):
+    _refused(lib, "attention", written, read)
+
+
+def test_attention_outputs_over_each_other(lib):
+    _refused(lib, "attention", "out", "lse_out")
