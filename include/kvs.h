@@ -620,8 +620,8 @@ KVS_API kvs_status kvs_attention_paged(const kvs_shape *shape, const kvs_paged_c
  *
  * lse            [dev] fp32[n_new, n_q_heads]
  * decay          finite, at least 0
- * mass, mass_out [dev] fp32 [batch, n_kv_heads, mass_stride], mass_stride at least max_ctx.  mass may be mass_out, or NULL (zeros); they
- *                may not overlap otherwise
+ * mass, mass_out [dev] fp32 [batch, n_kv_heads, mass_stride], mass_stride at least max_ctx.  mass may be mass_out, or NULL (zeros);
+ *                mass_out may not overlap it otherwise, nor anything else that is read
  * workspace      [dev] optional, 256-byte aligned, kvs_workspace_size("mass_paged", shape, batch, max_ctx, n_new) bytes:
  *                chunks over short contexts cut their rows into pieces and add them up
  * fp32 sums in a fixed order (bit-reproducible for equal workspaces); bf16 products are accumulated in fp32.

@@ -596,6 +596,12 @@ extern "C" kvs_status kvs_mass_paged(const kvs_shape *shape, const kvs_paged_cac
     if (mass && mass != mass_out && overlap(mass, mass_bytes, mass_out, mass_bytes)) return fail(KVS_EINVAL, "%s: mass_out overlaps mass without being it", me);
     if (n_new > 0 && (!q_new || !lse)) return fail(KVS_EINVAL, "%s: NULL tensor pointer", me);
     if (!aligned16(q_new)) return fail(KVS_EINVAL, "%s: Q must be 16-byte aligned", me);
+    const size_t pool = pool_bytes(shape, cache), heads = (size_t)n_new * shape->n_q_heads, batch = (size_t)pages->batch;
+    st = check_apart(me, {{mass_out, mass_bytes, "mass_out"}},
+                     {{q_new, heads * shape->head_dim * elem_bytes(shape->dtype), "q_new"}, {lse, heads * sizeof(float), "lse"}, {cache->k, pool, "the cache's K"},
+                      {cache->v, pool, "the cache's V"}, {pages->table, batch * pages->width * 4, "the page table"}, {pages->ctx_len, batch * 4, "ctx_len"},
+                      {cu_new, (batch + 1) * 4, "cu_new"}, {sel_pos, (size_t)n_new * 4, "sel_pos"}});
+    if (st != KVS_OK) return st;
     const bool wide = shape->head_dim == 128;
     hipStream_t hs = (hipStream_t)stream;
     if (few_rows(shape, pg.batch, n_new)) {

@@ -61,3 +61,11 @@ def test_attention(lib, written, read):
 
 def test_attention_outputs_over_each_other(lib):
     _refused(lib, "attention", "out", "lse_out")
+
+
+@pytest.mark.parametrize("read", ["q", "lse", "mass", "k", "v", "table", "ctx_len", "cu_new", "sel_pos"])
+def test_mass(lib, read):
+    if read != "mass":                                       # (mass may be mass_out itself)
+        _refused(lib, "mass", "mass_out", read)
+    for at in (AT["mass_out"] - (SIZES[read] - 1) // 16 * 16, AT["mass_out"] + 16, AT["mass_out"] + SIZES["mass_out"] - 16):
+        assert _call(lib, "mass", **{read: at}) == B.EINVAL and b"overlaps" in lib.kvs_last_error()
