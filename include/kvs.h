@@ -648,7 +648,8 @@ KVS_API kvs_status kvs_mass_paged(const kvs_shape *shape, const kvs_paged_cache 
  *           [0, n_pages) take nothing
  * kept      [dev] int32[batch, max_keep] or NULL: the kept rows' positions, ascending; entries from m on stay as they are
  * new_len   [dev] int32[batch] or NULL: m.  May be ctx_len
- * new_mass  [dev] fp32 [batch, n_kv_heads, max_keep] or NULL: the kept rows' mass; entries from m on stay as they are.  No overlap with mass
+ * new_mass  [dev] fp32 [batch, n_kv_heads, max_keep] or NULL: the kept rows' mass; entries from m on stay as they are.  Nothing that is written
+ *           may overlap anything else
  * workspace [dev] kvs_workspace_size("evict_paged", shape, batch, max_ctx, 0) bytes, 256-byte aligned, required
  * Exact and deterministic.
  */

@@ -424,6 +424,16 @@ extern "C" kvs_status kvs_evict_paged(const kvs_shape *shape, const kvs_paged_ca
     const size_t lines = (size_t)pages->batch * shape->n_kv_heads * sizeof(float);
     if (new_mass && overlap(mass, lines * mass_stride, new_mass, lines * max_keep)) return fail(KVS_EINVAL, "%s: new_mass overlaps mass", me);
     if (!workspace || workspace_bytes < evict_paged_workspace_bytes(shape, pages->batch, pg.max_ctx)) return fail(KVS_EWORKSPACE, "%s: workspace too small", me);
+    const size_t pool = pool_bytes(shape, cache), ints = (size_t)pages->batch * 4;
+    const Span out_mass = {new_mass, lines * max_keep, "new_mass"}, out_kept = {kept, ints * max_keep, "kept"}, out_len = {new_len, ints, "new_len"};
+    const Span k = {new_table ? cache->k : nullptr, pool, "the cache's K"}, v = {new_table ? cache->v : nullptr, pool, "the cache's V"};
+    const Span in_mass = {mass, lines * mass_stride, "mass"}, in_keep = {keep, ints, "keep"}, table = {pages->table, ints * pages->width, "the page table"},
+               into = {new_table, ints * new_width, "new_table"}, length = {new_len == pages->ctx_len ? nullptr : pages->ctx_len, ints, "ctx_len"};
+    st = check_apart(me, {out_mass, out_kept, k, v}, {in_mass, in_keep, table, into, {pages->ctx_len, ints, "ctx_len"}});
+    if (st == KVS_OK) st = check_apart(me, {out_len}, {in_mass, in_keep, table, into, length, out_mass, out_kept, k, v});
+    if (st == KVS_OK) st = check_apart(me, {out_kept, out_mass}, {k, v});
+    if (st == KVS_OK) st = check_apart(me, {out_kept}, {out_mass});
+    if (st != KVS_OK) return st;
     hipStream_t hs = (hipStream_t)stream;
     if (pg.max_ctx == 0) max_keep = 0;
     const Layout l = layout_of(pg.batch, pg.max_ctx);

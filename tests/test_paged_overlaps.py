@@ -69,3 +69,23 @@ def test_mass(lib, read):
         _refused(lib, "mass", "mass_out", read)
     for at in (AT["mass_out"] - (SIZES[read] - 1) // 16 * 16, AT["mass_out"] + 16, AT["mass_out"] + SIZES["mass_out"] - 16):
         assert _call(lib, "mass", **{read: at}) == B.EINVAL and b"overlaps" in lib.kvs_last_error()
+
+
+@pytest.mark.parametrize("read", ["mass", "keep", "table", "ctx_len", "new_table"])
+@pytest.mark.parametrize("written", ["k", "v", "kept", "new_len", "new_mass"])
+def test_evict(lib, written, read):
+    if (written, read) != ("new_len", "ctx_len"):
+        _refused(lib, "evict", written, read)
+
+
+@pytest.mark.parametrize("one,other", [("k", "kept"), ("v", "kept"), ("k", "new_mass"), ("v", "new_mass"), ("k", "new_len"), ("v", "new_len"), ("kept", "new_mass"), ("kept", "new_len"), ("new_mass", "new_len")])
+def test_evict_outputs_over_each_other(lib, one, other):
+    _refused(lib, "evict", one, other)
+
+
+def test_evict_lengths_in_place(lib):
+    """new_len may be ctx_len itself, and lie across it in no other way."""
+    for by in (-12, -4, 4, 12):
+        assert _call(lib, "evict", new_len=AT["ctx_len"] + by) == B.EINVAL and b"new_len overlaps ctx_len" in lib.kvs_last_error()
+    assert _call(lib, "evict", new_len=AT["ctx_len"], kept=AT["mass"]) == B.EINVAL and b"kept overlaps mass" in lib.kvs_last_error()
+    assert _call(lib, "evict", new_len=AT["ctx_len"], kept=AT["ctx_len"]) == B.EINVAL and b"kept overlaps ctx_len" in lib.kvs_last_error()
