@@ -546,8 +546,8 @@ KVS_API kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8 *c
  *
  * Tokens of a call belong to the requests in order: those of request b are [cu_new[b], cu_new[b+1]) (device memory, at
  * least 0, non-decreasing, at most n_new; offsets that break this give unspecified results, and no access outside the tensors).
- * Tokens outside [cu_new[0], cu_new[batch]) belong to none: nothing of theirs is read or written, so a captured call may hold
- * more places than tokens.  cu_new == NULL: one token a request (n_new == batch).  Token i of a request's n stands at position
+ * Tokens outside [cu_new[0], cu_new[batch]) belong to none: nothing of theirs is written, and what their rows hold reaches nothing (the rows
+ * may be read), so a captured call may hold more places than tokens.  cu_new == NULL: one token a request (n_new == batch).  Token i of a request's n stands at position
  * sel_pos[cu_new[b] + i], or, with sel_pos == NULL, at ctx_len[b] - n + i: the context's last rows.  A negative position sees
  * nothing; one behind the context sees what its last row sees.
  *

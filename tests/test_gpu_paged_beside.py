@@ -3,6 +3,7 @@ they may write over what they read: accepted, and right."""
 import pytest
 import torch
 
+import paged_many as M
 import paged_ref as R
 from paper_2503_16525_amd import binding as B
 from test_gpu_paged_attention import _parts
@@ -72,3 +73,35 @@ def test_side_by_side(dtype):
             assert torch.equal(new_mass[b, :, :m], mass[b][:, want_rows])
             for j, i in enumerate(want_rows):
                 assert torch.equal(c.k[int(new_table[b, j // page]), j % page], before[int(c.table[b, i // page]), i % page])
+
+
+@pytest.mark.parametrize("dtype,pieces", [(torch.bfloat16, None), (torch.bfloat16, 1), (torch.bfloat16, 2), (torch.float32, None)])
+def test_places_that_hold_no_token(dtype, pieces):
+    """Before the first and behind the last request's tokens: NaN and infinities in them reach nothing, and nothing of theirs is written.  By the kernels of
+    few and of many rows a request, and (pieces) by attention's for many rows a key."""
+    for reqs in ([(600, 300), (64, 5), (0, 0), (33, 33)], [(600, 1), (64, 2), (33, 1), (40, 3)]):
+        c = R.Case(8, 2, 128, dtype, 16, reqs, seed=6, places=(70, 90))
+        ref = R.attention(c)
+        lse = torch.nan_to_num(ref[1], nan=0.0).float()
+        old = torch.rand((len(reqs), 2, 600), generator=c.gen).cuda()
+        want = R.mass(c, lse, old, 1.0)
+        k_new, v_new = (torch.randn((c.n, 2, 128), generator=c.gen).to(dtype).cuda() for _ in range(2))
+        for x in (c.q, k_new, v_new, lse):
+            x[:c.cu[0]], x[c.cu[-1]:] = float("nan"), float("inf")
+        cache, pages = c.on()
+        out, got_lse = torch.full_like(c.q, 7.0), torch.full((c.n, 8), 7.0, device="cuda")
+        ws = torch.empty((max(B.kvs_workspace_size(x, c.shape, len(reqs), 600, c.n) for x in ("attention_paged", "mass_paged")),), dtype=torch.uint8, device="cuda")
+        with M.forced(pieces or 0) as lib:
+            assert not pieces or M.choice(lib, c.shape, 16, len(reqs), 600, c.n)[:2] == (True, pieces)
+            B.kvs_attention_paged(c.shape, cache, pages, c.cu_new, None, c.q, c.scale, 0, 0, out, got_lse, ws)
+        R.check_attention(c, out, got_lse, ref, 1 if pieces else _parts(c), "places")
+        for s in (slice(0, c.cu[0]), slice(c.cu[-1], c.n)):
+            assert (out[s] == 7).all() and (got_lse[s] == 7).all()
+        got = old.clone()
+        B.kvs_mass_paged(c.shape, cache, pages, c.cu_new, None, c.q, lse, c.scale, 0, 0, 1.0, got, got, ws)
+        R.check_mass(c, got, want, lse[c.cu[0]:c.cu[-1]], "places")
+        B.kvs_store_paged(c.shape, cache, pages, c.cu_new, None, k_new, v_new)
+        for b in range(len(reqs)):
+            rows = c.slots[b].cuda()
+            assert torch.isfinite(c.k.view(-1, 2, 128)[rows]).all()
+            assert torch.equal(c.v.view(-1, 2, 128)[rows[c.pos[b]]], v_new[c.cu[b]:c.cu[b + 1]])
