@@ -210,7 +210,8 @@ KVS_API kvs_status kvs_scatter_kv(const kvs_shape *shape, int64_t n_rows,
  *         asked for stays below 0.56 GB for one request (528 bytes a row and piece).
  * bf16 inputs (head_dim 128, scale > 0) are contracted on the matrix cores with fp32 accumulation
  * and an fp32 softmax, the softmax weights entering the second product as bf16; every other case
- * is computed in fp32 throughout, on the fp32 matrix instruction.
+ * is computed in fp32 throughout, on the fp32 matrix instruction.  In bf16 launches of many rows weights lie around 2^-60 while a row's
+ * first logits are its largest: values below 2^-60 may lose bits there, and sums of values beyond 2^27 may become infinite.
  */
 KVS_API kvs_status kvs_partial_attention(const kvs_shape *shape, int32_t batch,
                                  const int64_t *ctx_off, const int64_t *ctx_len,
@@ -525,7 +526,7 @@ KVS_API kvs_status kvs_deviation_kv8(const kvs_shape *shape, const kvs_cache8 *c
  * bf16: softmax weights enter the second product times V's scales, as two bf16 numbers that hold 16 of their bits where no
  * request has more than 32 rows a KV head (tokens times the query heads that share it), rounded to one elsewhere.
  * fp32: Q and these products enter as three bf16 numbers each, which together hold all their bits, and everything else is
- * fp32.  Sums of values beyond 2^110 may become infinite.
+ * fp32.  Sums of values beyond 2^110 may become infinite; in bf16 launches of many rows beyond 2^27, and values below 2^-60 may lose bits.
  */
 KVS_API kvs_status kvs_attention_kv8(const kvs_shape *shape, const kvs_cache8 *cache, int32_t batch,
                                      const int64_t *ctx_off, const int64_t *ctx_len, const int64_t *cu_sel,

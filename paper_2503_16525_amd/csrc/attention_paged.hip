@@ -12,7 +12,8 @@
 //
 // The four waves of a workgroup take the same 32 rows and every fourth tile, each with an LDS slot for K and one for V that its
 // loads go to directly (global to LDS, 16 bytes a lane, no registers), without a barrier: K of the next tile is asked for once
-// this tile's has been read, V likewise, so that a tile's worth of loads is under way all the time, and two workgroups share a CU.
+// this tile's has been read, V likewise, so that a tile's worth of loads is under way all the time, and two workgroups share a CU (fp32 at
+// 128 channels: one, whose slots take 128 KB).
 // At the end the waves meet in LDS.  Launches of too few workgroups cut the keys into pieces, which a second kernel merges.
 //
 // Measured (bf16, 128 channels, one token a request, 28 or 32 query heads).  Memory bounds the long ones: 131072 keys of 4 KV heads, 268 MB, 44.5 us and
@@ -54,8 +55,10 @@ __device__ __forceinline__ float max_of_halves(float x)      // of lanes i and i
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// PARTS: bf16 numbers that a weight enters the second product as: one, or two that hold 16 of its bits (fp32: the weights are what they are).
-// Two goes with few rows a request: K and V are then read once, and their loads say so (64 contexts of 4096 to 16384 487 -> 443 us, 131072
+// PARTS: bf16 numbers that a weight enters the second product as: one, or two that hold 16 of its bits (fp32: the weights are what they are).  One is
+// off by up to 2^-8 (rounding the output to bf16 is off by as much); a second one would be half as many products again, which bound launches of many rows,
+// and is nearly free where memory does.
+// So two go with few rows a request: K and V are then read once, and their loads say so (64 contexts of 4096 to 16384 487 -> 443 us, 131072
 // keys 59 -> 53; where several blocks share the keys through L2, 24 tokens over each of 8 contexts, 83 -> 100).
 // AGAIN: the rows of row tiles of 256 whose kernel asks for it (`odd`, a word a workgroup of its), eight blocks each.
 template <int DTYPE, int D, int PARTS, bool AGAIN>
@@ -608,7 +611,8 @@ constexpr int kLeastTiles = kWaves;    // of a piece: one for each wave
 constexpr int64_t kMostCutWgs = 4 * kPlaces;
 
 // In microseconds, as measured: a step of four tiles, one a wave, takes 1.0, 1.5 beside a second workgroup on the compute unit, and workgroups
-// beyond 512 wait for the first; the cache comes at 5.1 TB/s, and the two hide each other less the closer they are; where reading bounds the call
+// beyond 512 wait for the first (fp32 at 128 channels has 256 places and is planned the same; 8192 keys of 8 heads 26 us, 256 tokens of 32 heads over
+// 4096 162); the cache comes at 5.1 TB/s, and the two hide each other less the closer they are; where reading bounds the call
 // or there are rounds, contexts of a batch that are longer than others hold the end up by a third of a piece, and the average one is shorter
 // than the longest; 6 for the launch and a workgroup's beginning and end, 4 for a merge's.  Over 39 calls of 1 to 6000 tokens and 500 to 60000
 // keys the kernel and number of pieces that this takes are within 10 % of the best there is in 35, within 22 % in all.

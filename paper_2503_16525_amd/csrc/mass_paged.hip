@@ -546,8 +546,8 @@ kvs_status launch_few(const kvs_shape *shape, const kvs_paged_cache *c, const Pa
     if (st != KVS_OK) return st;
     const int64_t units = (int64_t)pg.batch * shape->n_kv_heads, tiles = (pg.max_ctx + 31) / 32;
     // One workgroup for each place on the chip, and none of more than 128 tiles.  (512, 1024, 2048 workgroups, us: 8 contexts of 2000 to 8000 of
-    // 8 heads 22.2, 23.1, 24.3; 4 of 10000 to 40000 of 4 30.8, 32.9, 34.8; 64 of 100 to 400 of 8 13.2, 15.2, 15.3; 64 of 4096 to 16384 280 each,
-    // 313 with pieces as long as they come.)
+    // 8 heads 22.2, 23.1, 24.3; 4 of 10000 to 40000 of 4 30.8, 32.9, 34.8; 64 of 100 to 400 of 8 13.2, 15.2, 15.3; 64 of 4096 to 16384, before loads said that keys
+    // are read once, 280 each (now 258 to 266), 313 with pieces as long as they come.)
     int64_t pieces = (512 + units - 1) / units;
     if (pieces < (tiles + 127) / 128) pieces = (tiles + 127) / 128;
     int64_t piece_tiles = (tiles + pieces - 1) / pieces;
